@@ -241,6 +241,76 @@ int laser_kv_seq_set_len(laser_kv* kv, int seq, int len, void* stream);
 int laser_kv_read_lens(laser_kv* kv, const int32_t* seq_ids /*[host] B*/, int B,
                        int32_t* lens_out /*[host] B*/, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Caches and weights in four bits. A code c = 0..15 stands for m + s c, with a scale s and an offset m (fp16) that a group of
+ * elements shares.
+ *
+ * laser_kv_create_4bit: a cache whose keys and values are held that way, 32 channels of a token and head to a group (1.25
+ * bytes per token, layer and channel instead of 5). n_heads is the number of key/value heads. All laser_kv_* calls take such a handle;
+ * laser_verify_step, laser_verify_tree and laser_generate do too (on the general path, whose attention is then laser_kv_attend's),
+ * and results carry the cache's rounding: about 7 % of a key's or value's spread. Beside the pages it holds 17 MB (9 at head_dim 64) of workspace.
+ * Stored for a group x: s = fp16((max - min) / 15), m = fp16(min), c = (x - m) / s rounded to nearest even within 0..15 (s = 0: c = 0), from
+ * 64-bit intermediate values (s and m rounded to fp32 and from there to fp16); magnitudes beyond 65504 saturate. A key or value that is not finite makes its token's
+ * key in that head NaN (its value as if that element were 0): rows that see the token get NaN from that head, other rows are not touched. */
+int laser_kv_create_4bit(const laser_kv_desc* desc, void* stream, laser_kv** out);
+
+/* Element types of laser_kv_append, laser_kv_attend, laser_kv_read and laser_w4_matmul. */
+#define LASER_F16  0
+#define LASER_BF16 1
+#define LASER_F32  2
+
+/* Keys, values, queries or results of B sequences with R rows each: [dev] element (b, r, h, c) lies at
+ * data + b * seq + r * row + h * head + c (strides in elements, >= 0). Needs the alignment of its elements only. */
+typedef struct laser_heads { void* data; int64_t seq, row, head; } laser_heads;
+
+/* laser_rope_table: table [dev] float[max_pos][rope_dim / 2][2] = (cos, sin) of position * base^(-2 i / rope_dim), angles in 64 bits. */
+int laser_rope_table(float* table, int max_pos, int rope_dim, double base, void* stream);
+
+/* laser_kv_append: the keys and values of a step's rows into a 4-bit cache, with the position rotation applied on the way.
+ * Row r of sequence b goes to slot len + r, and len does not change: laser_kv_commit (laser_kv_commit_tree) makes rows permanent, and
+ * the next append overwrites what was not committed. Its position is len + r or, with tree_parent, len + its depth in the token tree.
+ *   seq_ids     [host] int32[B]       all different; slots need (host bound of len) + R reserved tokens, else LASER_E_OOM_PAGES
+ *   n_rows      [dev]  int32[B] or NULL (R each): rows a sequence has, cut to 0..R; nothing is read or written for the others
+ *   tree_parent [dev]  int32[B][R-1] or NULL (chains): as for laser_verify_tree
+ *   R           1..LASER_MAX_DRAFT + 1
+ *   k, v        key/value heads of the cache; q, q_out: n_heads query heads, rotated into q_out (which may be q); n_heads 0: none
+ *   rope        [dev] float[max_pos][rope_dim / 2][2] (laser_rope_table), 8-byte aligned; channel i < rope_dim / 2 is paired with i + rope_dim / 2,
+ *               channels from rope_dim on are not rotated. rope_dim: 0 (no rotation), head_dim, or 64 of 128. Positions must stay below
+ *               max_pos (checked against the host's bound of len, LASER_E_LIMIT; a replayed graph's are cut to it).
+ * seq_ids and the reservations are part of the launch: a captured append keeps those of its capture, and leaves out rows for which
+ * a length that has grown under replays has no reserved slot. */
+int laser_kv_append(laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* n_rows, const int32_t* tree_parent, int B, int R,
+                    int dtype, const laser_heads* k, const laser_heads* v, const laser_heads* q, const laser_heads* q_out, int n_heads,
+                    const float* rope, int rope_dim, int max_pos, void* stream);
+
+/* laser_kv_attend: out = softmax(scale q . k) v of a step's rows over a 4-bit cache: row r of sequence b attends to the committed
+ * slots 0..len-1 and, of its own step's slots len..len+R-1 (laser_kv_append), to itself and its ancestors (tree_parent; NULL: rows 0..r).
+ * n_heads query heads, a multiple of the cache's: query head j uses key/value head j / (n_heads / cache heads).
+ * Other arguments as for laser_kv_append; rows beyond n_rows are left as they are. out has q's type and may be q. Sums, softmax and
+ * scores are fp32. Contexts are split over workgroups by the host's bounds of len: results may differ in the last bits between launches
+ * whose bounds differ, and are the same for the same ones. Uses the handle's workspace. */
+int laser_kv_attend(laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* n_rows, const int32_t* tree_parent, int B, int R,
+                    int n_heads, int dtype, const laser_heads* q, float scale, const laser_heads* out, void* stream);
+
+/* laser_kv_read: the keys (rotated) and values that n tokens of a 4-bit cache stand for, from slot start on (-1: from each sequence's
+ * committed length on, i.e. the rows of the last append). All slots must be reserved. */
+int laser_kv_read(laser_kv* kv, int layer, const int32_t* seq_ids, int B, int start, int n, int dtype, const laser_heads* k,
+                  const laser_heads* v, void* stream);
+
+/* Weights in four bits: W[n][i] = m[n][i / group] + s[n][i / group] c[n][i], group 32, 64 or 128; Kd a multiple of group, N >= 1.
+ * laser_w4_create lays codes, scales and offsets out for the products (the handle keeps its own copy; synchronises `stream`):
+ *   codes   [dev] uint8[N][Kd / 2]      two to a byte, the first in the low four bits
+ *   scales  [dev] fp16[N][Kd / group];  offsets [dev] fp16[N][Kd / group]   (a zero point z is an offset of -s z)
+ * laser_w4_quantize makes them from bf16 weights [N][Kd], by the rule of laser_kv_create_4bit. */
+typedef struct laser_w4 laser_w4;
+int laser_w4_create(const uint8_t* codes, const uint16_t* scales, const uint16_t* offsets, int N, int Kd, int group, void* stream, laser_w4** out);
+int laser_w4_destroy(laser_w4* w);
+int laser_w4_quantize(const uint16_t* w, int N, int Kd, int group, uint8_t* codes, uint16_t* scales, uint16_t* offsets, void* stream);
+/* laser_w4_matmul: out[r][n] = sum over i of x[r][i] W[n][i] for M rows; x and out in `dtype` (LASER_F16 or LASER_BF16), rows
+ * x_stride >= Kd and out_stride >= N elements apart, aligned to their elements. fp32 sums. Keeps no workspace: calls on several
+ * streams may share a handle. Made for few rows (every weight is read once up to 80 rows, again for every 80 further ones). */
+int laser_w4_matmul(const laser_w4* w, const void* x, int64_t x_stride, int M, int dtype, void* out, int64_t out_stride, void* stream);
+
 /* laser_verify_step (Eq. 3 / Eq. 6 forward, Eq. 4 / 7 / 8 acceptance, correction rule of Sec. 2.1).
  * For sequence b, rows r = 0..K hold the tokens [pending[b], drafts[b][0..K-1]] at positions
  * len+r; their keys/values go to cache slots len..len+K; row r attends to slots 0..len+r. The

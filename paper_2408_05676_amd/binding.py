@@ -38,6 +38,14 @@ class _KVDesc(C.Structure):
                                          "max_seqs", "max_pages_per_seq")]
 
 
+class _Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("seq", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+F16, BF16, F32 = 0, 1, 2                                                         # LASER_F16 .. of include/laser.h
+_DTYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+
 def lib():
     """Load liblaser.so once and declare the prototypes."""
     global _LIB
@@ -63,6 +71,16 @@ def lib():
         "laser_model_create": [C.POINTER(_ModelDesc), vp, C.POINTER(vp)],
         "laser_model_destroy": [vp],
         "laser_kv_create": [C.POINTER(_KVDesc), vp, C.POINTER(vp)],
+        "laser_kv_create_4bit": [C.POINTER(_KVDesc), vp, C.POINTER(vp)],
+        "laser_rope_table": [vp, i32, i32, C.c_double, vp],
+        "laser_kv_append": [vp, i32, vp, vp, vp, i32, i32, i32, C.POINTER(_Heads), C.POINTER(_Heads), C.POINTER(_Heads), C.POINTER(_Heads),
+                            i32, vp, i32, i32, vp],
+        "laser_kv_attend": [vp, i32, vp, vp, vp, i32, i32, i32, i32, C.POINTER(_Heads), f32, C.POINTER(_Heads), vp],
+        "laser_kv_read": [vp, i32, vp, i32, i32, i32, i32, C.POINTER(_Heads), C.POINTER(_Heads), vp],
+        "laser_w4_create": [vp, vp, vp, i32, i32, i32, vp, C.POINTER(vp)],
+        "laser_w4_destroy": [vp],
+        "laser_w4_quantize": [vp, i32, i32, i32, vp, vp, vp, vp],
+        "laser_w4_matmul": [vp, vp, i64, i32, i32, vp, i64, vp],
         "laser_kv_destroy": [vp],
         "laser_kv_seq_reserve": [vp, i32, i32, vp],
         "laser_kv_seq_release": [vp, i32, vp],
@@ -314,6 +332,192 @@ class KVCache:
         # at interpreter shutdown the HIP runtime may already be gone; the process frees everything
         if not sys.is_finalizing():
             self.close()
+
+
+class KVCache4(KVCache):
+    """laser_kv_create_4bit: a KVCache whose keys and values are held in four bits. n_heads: its key/value heads."""
+
+    def __init__(self, n_layers, n_heads, head_dim, n_pages, max_seqs, max_pages_per_seq, page_size=16, stream=None):
+        self.page_size, self.n_heads, self.head_dim, self.device = page_size, n_heads, head_dim, torch.cuda.current_device()
+        d = _KVDesc(n_layers, n_heads, head_dim, page_size, n_pages, max_seqs, max_pages_per_seq)
+        self._h = C.c_void_p()
+        _check(lib().laser_kv_create_4bit(C.byref(d), _stream(stream), C.byref(self._h)), "laser_kv_create_4bit")
+
+
+def _heads(t: torch.Tensor, name: str, B: int, R: int, H: int, dh: int, dtype) -> _Heads:
+    """A [B][R][H][dh] tensor, in any order of its first three dimensions, as laser_heads."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and tuple(t.shape) == (B, R, H, dh) and (t.stride(3) == 1 or t.numel() == 0)):
+        raise LaserError(f"{name} must be a CUDA tensor [{B}][{R}][{H}][{dh}] of {dtype} with contiguous channels")
+    _here(t, name)
+    return _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _here(t: torch.Tensor, name: str) -> None:
+    if t.device.index != torch.cuda.current_device():
+        raise LaserError(f"{name} is on {t.device}, not on the current device")
+
+
+def _out(shape, dtype, device, stream) -> torch.Tensor:
+    """A result's memory, allocated for the stream that writes it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(_stream(stream)))
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _step_args(kv, ids, n_rows, tree_parent, B, R):
+    if not isinstance(kv, KVCache4):
+        raise LaserError("kv must be a KVCache4")
+    if kv.device != torch.cuda.current_device():
+        raise LaserError(f"the cache is on device {kv.device}, not on the current one")
+    if ids.size != B:
+        raise LaserError(f"seq_ids must name {B} sequences")
+    if n_rows is not None:
+        if tuple(n_rows.shape) != (B,):
+            raise LaserError("n_rows must be [B]")
+        _here(n_rows, "n_rows")
+    if tree_parent is not None:
+        if tuple(tree_parent.shape) != (B, R - 1):
+            raise LaserError("tree_parent must be [B][R - 1]")
+        _here(tree_parent, "tree_parent")
+    return (None if n_rows is None else _dev(n_rows, torch.int32, "n_rows"),
+            None if tree_parent is None else _dev(tree_parent, torch.int32, "tree_parent"))
+
+
+def rope_table(max_pos: int, dim: int, base: float = 10000.0, stream=None) -> torch.Tensor:
+    """laser_rope_table: (cos, sin) float32 [max_pos][dim / 2][2]."""
+    t = _out((max_pos, dim // 2, 2), torch.float32, "cuda", stream)
+    _check(lib().laser_rope_table(t.data_ptr(), max_pos, dim, base, _stream(stream)), "laser_rope_table")
+    return t
+
+
+def kv_append(kv: KVCache4, layer: int, seq_ids, k: torch.Tensor, v: torch.Tensor, q=None, rope=None, tree_parent=None, n_rows=None,
+              q_out=None, stream=None):
+    """laser_kv_append: keys and values [B][R][heads][head_dim] of a step's rows into the cache, rotated by `rope`
+    (rope_table; None: not rotated). Returns the rotated queries (q [B][R][query heads][head_dim], may be q_out itself) or None."""
+    ids = _host_i32(seq_ids, "seq_ids")
+    if k.dim() != 4:
+        raise LaserError("k must be [B][R][heads][head_dim]")
+    B, R = k.shape[0], k.shape[1]
+    nr, tp = _step_args(kv, ids, n_rows, tree_parent, B, R)
+    dt = k.dtype
+    if dt not in _DTYPES:
+        raise LaserError(f"k: {dt} is not float16, bfloat16 or float32")
+    hk = _heads(k, "k", B, R, kv.n_heads, kv.head_dim, dt)
+    hv = _heads(v, "v", B, R, kv.n_heads, kv.head_dim, dt)
+    hq = ho = None
+    n_heads = 0
+    if q is not None:
+        if q.dim() != 4:
+            raise LaserError("q must be [B][R][heads][head_dim]")
+        n_heads = q.shape[2]
+        if q_out is None:
+            q_out = _out(q.shape, dt, q.device, stream)
+        hq, ho = _heads(q, "q", B, R, n_heads, kv.head_dim, dt), _heads(q_out, "q_out", B, R, n_heads, kv.head_dim, dt)
+    rope_p, rope_dim, max_pos = None, 0, 0
+    if rope is not None:
+        if rope.dim() != 3 or rope.shape[2] != 2:
+            raise LaserError("rope must be [max_pos][rope_dim / 2][2]")
+        _here(rope, "rope")
+        rope_p, max_pos, rope_dim = _dev(rope, torch.float32, "rope"), rope.shape[0], 2 * rope.shape[1]
+    _check(lib().laser_kv_append(kv._h, layer, ids.ctypes.data, nr, tp, B, R, _DTYPES[dt], hk, hv, hq, ho, n_heads, rope_p, rope_dim, max_pos,
+                                 _stream(stream)), "laser_kv_append")
+    return q_out
+
+
+def kv_attend(kv: KVCache4, layer: int, seq_ids, q: torch.Tensor, tree_parent=None, n_rows=None, scale=None, out=None, stream=None) -> torch.Tensor:
+    """laser_kv_attend: q [B][R][query heads][head_dim] -> the same shape. scale: 1 / sqrt(head_dim) unless given."""
+    ids = _host_i32(seq_ids, "seq_ids")
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise LaserError("q must be [B][R][heads][head_dim]")
+    B, R, H, dh = q.shape
+    nr, tp = _step_args(kv, ids, n_rows, tree_parent, B, R)
+    if q.dtype not in _DTYPES:
+        raise LaserError(f"q: {q.dtype} is not float16, bfloat16 or float32")
+    hq = _heads(q, "q", B, R, H, kv.head_dim, q.dtype)
+    if out is None:
+        out = _out(q.shape, q.dtype, q.device, stream)
+    ho = _heads(out, "out", B, R, H, kv.head_dim, q.dtype)
+    _check(lib().laser_kv_attend(kv._h, layer, ids.ctypes.data, nr, tp, B, R, H, _DTYPES[q.dtype], hq, dh ** -0.5 if scale is None else scale, ho,
+                                 _stream(stream)), "laser_kv_attend")
+    return out
+
+
+def kv_read(kv: KVCache4, layer: int, seq_ids, n: int, start: int = -1, dtype=torch.float16, out=None, stream=None):
+    """laser_kv_read: the keys and values [B][n][heads][head_dim] that tokens start .. start + n - 1 (-1: those behind the committed
+    length) stand for."""
+    ids = _host_i32(seq_ids, "seq_ids")
+    _step_args(kv, ids, None, None, ids.size, 1)
+    shape = (ids.size, n, kv.n_heads, kv.head_dim)
+    if out is None:
+        out = _out(shape, dtype, "cuda", stream), _out(shape, dtype, "cuda", stream)
+    k, v = out
+    if k.dtype not in _DTYPES:
+        raise LaserError(f"{k.dtype} is not float16, bfloat16 or float32")
+    _check(lib().laser_kv_read(kv._h, layer, ids.ctypes.data, ids.size, start, n, _DTYPES[k.dtype], _heads(k, "k", *shape, k.dtype),
+                               _heads(v, "v", *shape, k.dtype), _stream(stream)), "laser_kv_read")
+    return k, v
+
+
+def w4_quantize(w: torch.Tensor, group: int = 128, stream=None):
+    """laser_w4_quantize: bf16 [N][Kd] -> (codes uint8 [N][Kd / 2], scales and offsets fp16 [N][Kd / group])."""
+    p = _dev(w, torch.bfloat16, "w")
+    if w.dim() != 2:
+        raise LaserError("w must be [N][Kd]")
+    _here(w, "w")
+    N, Kd = w.shape
+    if group not in (32, 64, 128) or Kd % group:
+        raise LaserError(f"group {group}: 32, 64 or 128, and Kd {Kd} a multiple of it")
+    out = (_out((N, Kd // 2), torch.uint8, w.device, stream), *(_out((N, Kd // group), torch.float16, w.device, stream) for _ in range(2)))
+    _check(lib().laser_w4_quantize(p, N, Kd, group, *(t.data_ptr() for t in out), _stream(stream)), "laser_w4_quantize")
+    return out
+
+
+class W4:
+    """laser_w4_create / laser_w4_destroy: a matrix of 4-bit weights laid out for w4_matmul (see laser.h for the three arrays)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, offsets: torch.Tensor, stream=None):
+        self._h = C.c_void_p()
+        if codes.dim() != 2 or scales.dim() != 2 or scales.shape != offsets.shape or scales.shape[0] != codes.shape[0] or not scales.shape[1]:
+            raise LaserError("codes must be [N][Kd / 2], scales and offsets [N][Kd / group]")
+        for t, n in ((codes, "codes"), (scales, "scales"), (offsets, "offsets")):
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                _here(t, n)
+        self.N, self.Kd = codes.shape[0], 2 * codes.shape[1]
+        self.group = self.Kd // scales.shape[1]
+        if self.group * scales.shape[1] != self.Kd:
+            raise LaserError("Kd is not a multiple of the number of groups")
+        self.device = codes.device
+        _check(lib().laser_w4_create(_dev(codes, torch.uint8, "codes"), _dev(scales, torch.float16, "scales"), _dev(offsets, torch.float16, "offsets"),
+                                     self.N, self.Kd, self.group, _stream(stream), C.byref(self._h)), "laser_w4_create")
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h:
+            lib().laser_w4_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        # at interpreter shutdown the HIP runtime may already be gone; the process frees everything
+        if not sys.is_finalizing():
+            self.close()
+
+
+def w4_matmul(w: W4, x: torch.Tensor, out=None, stream=None) -> torch.Tensor:
+    """laser_w4_matmul: x [M][Kd] (float16 or bfloat16, contiguous within a row) -> [M][N] of the same type."""
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype in (torch.float16, torch.bfloat16) and x.dim() == 2 and x.shape[1] == w.Kd and x.stride(1) == 1):
+        raise LaserError(f"x must be a CUDA tensor [M][{w.Kd}] of float16 or bfloat16 with contiguous rows")
+    M = x.shape[0]
+    if out is None:
+        out = _out((M, w.N), x.dtype, x.device, stream)
+    if not (out.is_cuda and out.dtype == x.dtype and tuple(out.shape) == (M, w.N) and (out.stride(1) == 1 or w.N == 1)):
+        raise LaserError(f"out must be a CUDA tensor [{M}][{w.N}] of {x.dtype} with contiguous rows")
+    _here(x, "x")
+    if out.device != x.device or w.device != x.device:
+        raise LaserError(f"x, out and the weights are on {x.device}, {out.device} and {w.device}")
+    _check(lib().laser_w4_matmul(w._h, x.data_ptr(), x.stride(0) if M > 1 else w.Kd, M, _DTYPES[x.dtype], out.data_ptr(),
+                                 out.stride(0) if M > 1 else w.N, _stream(stream)), "laser_w4_matmul")
+    return out
 
 
 def verify_step(model: Model, kv: KVCache, seq_ids, pending: torch.Tensor, drafts: torch.Tensor,

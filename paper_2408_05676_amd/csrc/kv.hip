@@ -3,10 +3,13 @@
 #include <algorithm>
 #include <cstring>
 
+#include "four_bit.h"
 #include "mfma.h"
 #include "state.h"
 
 namespace laser {
+
+int kv4_import(KV* kv, int seq, int layer, const uint16_t* k, const uint16_t* v, int n_tokens, hipStream_t stream);
 
 int KV::stage_ids(const int32_t* host_ids, int B, hipStream_t stream, const int32_t** dev_out) {
     // The same ids on the same stream as the staging before (the steady state of a decoding loop, where verify and
@@ -136,7 +139,7 @@ __global__ __launch_bounds__(256) void kv_import_kernel(uint16_t* kpages, uint8_
 
 using namespace laser;
 
-extern "C" int laser_kv_create(const laser_kv_desc* desc, void* stream_, laser_kv** out) {
+static int create_impl(const laser_kv_desc* desc, bool four_bit, void* stream_, laser_kv** out) {
     LASER_REQUIRE(desc && out, LASER_E_INVALID_ARG, "NULL argument");
     hipStream_t stream = (hipStream_t)stream_;
     const laser_kv_desc& d = *desc;
@@ -150,9 +153,15 @@ extern "C" int laser_kv_create(const laser_kv_desc* desc, void* stream_, laser_k
     const size_t bt = (size_t)d.max_seqs * d.max_pages_per_seq;
     auto fail = [&](int rc) { laser_kv_destroy(reinterpret_cast<laser_kv*>(kv)); return rc; };
 #define KV_TRY(expr) do { hipError_t e_ = (expr); if (e_ != hipSuccess) { set_error("%s: %s", #expr, hipGetErrorString(e_)); return fail(LASER_E_HIP); } } while (0)
-    KV_TRY(hipMalloc((void**)&kv->kpages, pool_elems * 2));
-    KV_TRY(hipMalloc((void**)&kv->klpages, pool_elems));
-    KV_TRY(hipMalloc((void**)&kv->vpages, pool_elems * 2));
+    const size_t bytes4 = pool_elems / ((size_t)kPageSize * d.head_dim) * page4_bytes(d.head_dim);
+    if (four_bit) {
+        KV_TRY(hipMalloc((void**)&kv->pages4, bytes4));
+        KV_TRY(hipMalloc((void**)&kv->part4, kv4_part_floats(d.head_dim) * 4));
+    } else {
+        KV_TRY(hipMalloc((void**)&kv->kpages, pool_elems * 2));
+        KV_TRY(hipMalloc((void**)&kv->klpages, pool_elems));
+        KV_TRY(hipMalloc((void**)&kv->vpages, pool_elems * 2));
+    }
     KV_TRY(hipMalloc((void**)&kv->block_table, bt * 4));
     KV_TRY(hipMalloc((void**)&kv->len, (size_t)d.max_seqs * 4));
     KV_TRY(hipMalloc((void**)&kv->ids_dev, (size_t)kIdSlots * d.max_seqs * 4));
@@ -160,9 +169,12 @@ extern "C" int laser_kv_create(const laser_kv_desc* desc, void* stream_, laser_k
     for (int i = 0; i < kIdSlots; ++i) KV_TRY(hipEventCreateWithFlags(&kv->ids_ev[i], hipEventDisableTiming));
     // Pages start as zeros: masked-out cache slots are multiplied by probability 0 in the value
     // product, which must not meet NaN/Inf bit patterns left in fresh memory.
-    KV_TRY(hipMemsetAsync(kv->kpages, 0, pool_elems * 2, stream));
-    KV_TRY(hipMemsetAsync(kv->klpages, 0, pool_elems, stream));
-    KV_TRY(hipMemsetAsync(kv->vpages, 0, pool_elems * 2, stream));
+    if (four_bit) KV_TRY(hipMemsetAsync(kv->pages4, 0, bytes4, stream));
+    else {
+        KV_TRY(hipMemsetAsync(kv->kpages, 0, pool_elems * 2, stream));
+        KV_TRY(hipMemsetAsync(kv->klpages, 0, pool_elems, stream));
+        KV_TRY(hipMemsetAsync(kv->vpages, 0, pool_elems * 2, stream));
+    }
     KV_TRY(hipMemsetAsync(kv->block_table, 0, bt * 4, stream));
     KV_TRY(hipMemsetAsync(kv->len, 0, (size_t)d.max_seqs * 4, stream));
     KV_TRY(hipStreamSynchronize(stream));
@@ -177,9 +189,13 @@ extern "C" int laser_kv_create(const laser_kv_desc* desc, void* stream_, laser_k
     return LASER_OK;
 }
 
+extern "C" int laser_kv_create(const laser_kv_desc* desc, void* stream, laser_kv** out) { return create_impl(desc, false, stream, out); }
+extern "C" int laser_kv_create_4bit(const laser_kv_desc* desc, void* stream, laser_kv** out) { return create_impl(desc, true, stream, out); }
+
 extern "C" int laser_kv_destroy(laser_kv* h) {
     if (!h) return LASER_OK;
     KV* kv = reinterpret_cast<KV*>(h);
+    (void)hipFree(kv->pages4); (void)hipFree(kv->part4);
     (void)hipFree(kv->kpages); (void)hipFree(kv->klpages); (void)hipFree(kv->vpages); (void)hipFree(kv->block_table);
     (void)hipFree(kv->len); (void)hipFree(kv->ids_dev);
     if (kv->ids_pinned) (void)hipHostFree(kv->ids_pinned);
@@ -251,6 +267,7 @@ extern "C" int laser_kv_import(laser_kv* h, int seq, int layer, const uint16_t* 
                   "%d tokens exceed the capacity reserved for slot %d", n_tokens, seq);
     if (n_tokens == 0) return LASER_OK;
     LASER_REQUIRE(k && v, LASER_E_INVALID_ARG, "NULL k/v");
+    if (kv->pages4) return kv4_import(kv, seq, layer, k, v, n_tokens, (hipStream_t)stream);
     const size_t total = ((size_t)n_tokens + 3) / 4 * kv->d.n_heads * (kv->d.head_dim / 8);
     hipLaunchKernelGGL(kv_import_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, (hipStream_t)stream,
                        kv->kpages, kv->klpages, kv->vpages, kv->block_table + (size_t)seq * kv->d.max_pages_per_seq, k, v,
@@ -299,7 +316,9 @@ static int commit_impl(laser_kv* h, const int32_t* seq_ids, const int32_t* accep
         kv->h_len_ub[seq_ids[b]] += kv->h_last_rows[seq_ids[b]];
         kv->h_last_rows[seq_ids[b]] = 0;
     }
-    if (accept_path && K > 0 && kv->d.n_layers > 0)
+    if (accept_path && K > 0 && kv->d.n_layers > 0 && kv->pages4) {
+        if ((rc = launch_kv4_compact(kv, ids_dev, accept_len, accept_path, B, K, (hipStream_t)stream))) return rc;
+    } else if (accept_path && K > 0 && kv->d.n_layers > 0)
         hipLaunchKernelGGL(kv_compact_kernel, dim3(kv->d.n_heads, kv->d.n_layers, B), dim3(kv->d.head_dim), 0, (hipStream_t)stream,
                            kv->kpages, kv->klpages, kv->vpages, kv->block_table, kv->len, ids_dev, accept_len, accept_path, K,
                            kv->d.n_heads, kv->d.head_dim, kv->d.max_pages_per_seq, kv->d.n_pages);

@@ -1,0 +1,479 @@
+// Keys and values of new rows into the 4-bit paged cache, with the rotary positions applied on the way (queries too), and back.
+//
+// Rotation (pairs i, i + D/2 of the first D channels): a' = a cos - b sin, b' = a sin + b cos. A group of 32 channels of a token
+// and head, x = its values: s = f16((max - min) / 15), m = f16(min), c = round((x - m) / s) within 0..15 (s = 0: 0).
+// Keys are rotated in 64 bits: products of 24-bit operands are exact there, so that a value half-way between two codes falls to the side that
+// the formula puts it on, whatever the order of the operations.
+// Bound: memory traffic, 2 bytes a channel in, 5 bits out (and 2 out for queries); see the launch function for what it measured.
+#include <algorithm>
+
+#include "four_bit.h"
+
+namespace laser {
+
+// Four lanes (g = 0..3) share a token and head; lane g takes channels 32 c + 8 g .. + 7 of the keys' groups c, whose rotary
+// partners (32 channels or a multiple of them away) are its own too, and channels 32 c + 4 g .. + 3 and 32 c + 16 + 4 g .. + 3 of
+// the values' groups, which are whole bytes of the page.
+template <class T>
+__device__ inline T quad_min(T x) { x = min(x, __shfl_xor(x, 1)); return min(x, __shfl_xor(x, 2)); }
+template <class T>
+__device__ inline T quad_max(T x) { x = max(x, __shfl_xor(x, 1)); return max(x, __shfl_xor(x, 2)); }
+
+struct Group { float s, m; uint32_t sm; };
+// lo, hi: the group's extremes. Values beyond fp16 saturate.
+__device__ inline Group make_group(double lo, double hi) {
+    const _Float16 s = f64_to_f16(fmin((hi - lo) / 15.0, 65504.0)), m = f64_to_f16(fmin(fmax(lo, -65504.0), 65504.0));
+    return Group{(float)s, (float)m, (uint32_t)__builtin_bit_cast(uint16_t, s) | ((uint32_t)__builtin_bit_cast(uint16_t, m) << 16)};
+}
+// round((x - m) / s): in 32 bits unless that comes near a border between two codes
+__device__ inline uint32_t code_of(double x, const Group& g, float inv) {
+    const double d = x - (double)g.m;
+    const float y = (float)d * inv;
+    float n = rintf(y);
+    if (fabsf(y - n) > 0.499f) n = (float)rint(d / (double)g.s);
+    return g.s > 0.f ? (uint32_t)fminf(fmaxf(n, 0.f), 15.f) : 0u;
+}
+
+template <int DT, int N>
+__device__ inline void load_sum(const Heads& h, size_t o, int n_part, int64_t part_stride, float (&x)[N]) {
+    load_elems<DT, N>(h.p, o, x);
+    if constexpr (DT == DT_F32)
+        for (int s = 1; s < n_part; ++s) {
+            float y[N];
+            load_elems<DT, N>(h.p, o + s * part_stride, y);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] += y[i];
+        }
+}
+
+template <int DH, int DT>
+__global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
+    constexpr int NG = DH / 32;
+    const int per_row = 4 * (a.H + a.Hq);
+    const long t = (long)blockIdx.x * 256 + threadIdx.x;
+    const int g = threadIdx.x & 3;
+    const long row = t / per_row;
+    const int item = (int)(t % per_row) >> 2;
+    if (row >= (long)a.B * a.R) return;                                  // (four lanes together, as every exit below)
+    const int b = (int)(row / a.R), r = (int)(row % a.R);
+    if (a.n_rows && r >= a.n_rows[b]) return;
+    const int slot_id = a.seqs.slot(b);
+    const int len = a.start >= 0 ? a.start : a.lens[slot_id];
+    const int slot = len + r;
+    const int hg = a.rope_dim / 64;                                      // groups in half of the rotated channels
+    int pos = 0;
+    if (hg) {
+        if (a.row_pos) pos = a.row_pos[row];
+        else if (!a.parent) pos = slot;
+        else {
+            const int32_t* parent = a.parent + (size_t)b * (a.R - 1);
+            int depth = 0;
+            for (int i = r; i > 0; i = up_row(parent, i)) ++depth;
+            pos = len + depth;
+        }
+        pos = min(max(pos, 0), a.max_pos - 1);
+    }
+    // (cos, sin) of channels 32 c + 8 g .. + 7, c < hg
+    const float2* turn = a.rope + (size_t)pos * (32 * hg) + 8 * g;
+
+    if (item >= a.H) {                                                   // ---- queries: rotated, in their own type
+        const int h = item - a.H;
+        const size_t qi = (size_t)b * a.q.seq + (size_t)r * a.q.row + (size_t)h * a.q.head + 8 * g;
+        const size_t qo = (size_t)b * a.q_out.seq + (size_t)r * a.q_out.row + (size_t)h * a.q_out.head + 8 * g;
+        float x[NG][8];
+#pragma unroll
+        for (int c = 0; c < NG; ++c) load_sum<DT, 8>(a.q, qi + 32 * c, a.n_part, a.part_stride, x[c]);
+        auto rotate = [&](float (&u)[8], float (&w)[8], int c) {
+            float cs[16];
+            load_elems<DT_F32, 8>(turn + 32 * c, 0, *reinterpret_cast<float(*)[8]>(cs));
+            load_elems<DT_F32, 8>(turn + 32 * c + 4, 0, *reinterpret_cast<float(*)[8]>(cs + 8));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float p = u[j], q = w[j], co = cs[2 * j], si = cs[2 * j + 1];
+                u[j] = p * co - q * si;
+                w[j] = p * si + q * co;
+            }
+        };
+        if (hg == NG / 2) {
+#pragma unroll
+            for (int c = 0; c < NG / 2; ++c) rotate(x[c], x[c + NG / 2], c);
+        } else if (NG == 4 && hg == 1) rotate(x[0], x[1], 0);
+#pragma unroll
+        for (int c = 0; c < NG; ++c) store_elems<DT, 8>(a.q_out.p, qo + 32 * c, x[c]);
+        return;
+    }
+
+    // ---- keys and values of one token and head
+    if (slot >= a.seqs.tokens(b) || slot < 0) return;
+    const int h = item, tp = slot % kPageSize;
+    const int pg = a.block_table[(size_t)slot_id * a.mpps + slot / kPageSize];
+    uint8_t* page = a.pages + ((size_t)pg * a.H + h) * page4_bytes(DH);
+    float kf[NG][8], vf[NG][8];
+    {
+        const size_t ki = (size_t)b * a.k.seq + (size_t)r * a.k.row + (size_t)h * a.k.head + 8 * g;
+        const size_t vi = (size_t)b * a.v.seq + (size_t)r * a.v.row + (size_t)h * a.v.head + 4 * g;
+#pragma unroll
+        for (int c = 0; c < NG; ++c) {
+            load_sum<DT, 8>(a.k, ki + 32 * c, a.n_part, a.part_stride, kf[c]);
+            load_sum<DT, 4>(a.v, vi + 32 * c, a.n_part, a.part_stride, *reinterpret_cast<float(*)[4]>(&vf[c][0]));
+            load_sum<DT, 4>(a.v, vi + 32 * c + 16, a.n_part, a.part_stride, *reinterpret_cast<float(*)[4]>(&vf[c][4]));
+        }
+    }
+    // A key or value that is not finite makes the token's key NaN: every row that sees the token gets NaN from this head, and no
+    // other row meets it. The codes and the values' scales stay finite, so that what a mask hides never enters a product.
+    bool bad = false;
+#pragma unroll
+    for (int c = 0; c < NG; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool fk = __builtin_isfinite(kf[c][j]), fv = __builtin_isfinite(vf[c][j]);
+            bad |= !fk || !fv;
+            kf[c][j] = fk ? kf[c][j] : 0.f;
+            vf[c][j] = fv ? vf[c][j] : 0.f;
+        }
+    bad |= (bool)__shfl_xor((int)bad, 1);
+    bad |= (bool)__shfl_xor((int)bad, 2);
+
+    double x[NG][8];
+#pragma unroll
+    for (int c = 0; c < NG; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[c][j] = kf[c][j];
+    auto rotate = [&](double (&u)[8], double (&w)[8], int c) {
+        float cs[16];
+        load_elems<DT_F32, 8>(turn + 32 * c, 0, *reinterpret_cast<float(*)[8]>(cs));
+        load_elems<DT_F32, 8>(turn + 32 * c + 4, 0, *reinterpret_cast<float(*)[8]>(cs + 8));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const double p = u[j], q = w[j], co = cs[2 * j], si = cs[2 * j + 1];
+            u[j] = p * co - q * si;
+            w[j] = p * si + q * co;
+        }
+    };
+    if (hg == NG / 2) {
+#pragma unroll
+        for (int c = 0; c < NG / 2; ++c) rotate(x[c], x[c + NG / 2], c);
+    } else if (NG == 4 && hg == 1) rotate(x[0], x[1], 0);
+
+    uint32_t kw[NG];                       // words 2 p, 2 p + 1 of groups 2 p, 2 p + 1
+    uint32_t ksm = 0, vsm = 0;             // of group g
+#pragma unroll
+    for (int c = 0; c < NG; ++c) kw[c] = 0;
+#pragma unroll
+    for (int c = 0; c < NG; ++c) {
+        double lo = x[c][0], hi = x[c][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) { lo = fmin(lo, x[c][j]); hi = fmax(hi, x[c][j]); }
+        const Group gr = make_group(quad_min(lo), quad_max(hi));
+        const float inv = 1.f / gr.s;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) kw[(c & ~1) + (j >> 2)] |= code_of(x[c][j], gr, inv) << (8 * code_byte(j & 3) + 4 * (c & 1));
+        if (c == g) ksm = bad ? (gr.sm & 0xFFFFu) | 0x7E000000u : gr.sm;
+    }
+    uint8_t* kp = page + (g * 16 + tp) * (DH / 8);
+    if constexpr (NG == 4) *reinterpret_cast<u32x4*>(kp) = u32x4{kw[0], kw[1], kw[2], kw[3]};
+    else *reinterpret_cast<u32x2*>(kp) = u32x2{kw[0], kw[1]};
+
+    uint8_t* vp = page + page4_v(DH) + ((tp >> 2) * 16 + 4 * g) * (DH / 8) + code_byte(tp & 3);
+#pragma unroll
+    for (int c = 0; c < NG; ++c) {
+        float lo = vf[c][0], hi = vf[c][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) { lo = fminf(lo, vf[c][j]); hi = fmaxf(hi, vf[c][j]); }
+        const Group gr = make_group((double)quad_min(lo), (double)quad_max(hi));
+        const float inv = 1.f / gr.s;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            vp[e * (DH / 8) + 4 * c] = (uint8_t)(code_of((double)vf[c][e], gr, inv) | (code_of((double)vf[c][4 + e], gr, inv) << 4));
+        if (c == g) vsm = gr.sm;
+    }
+    if (g < NG) {
+        reinterpret_cast<uint32_t*>(page + page4_ksm(DH))[tp * NG + g] = ksm;
+        reinterpret_cast<uint32_t*>(page + page4_vsm(DH))[tp * NG + g] = vsm;
+    }
+}
+
+int launch_kv4_append(const AppendArgs& a, int dh, int dtype, hipStream_t stream) {
+    const long threads = (long)a.B * a.R * 4 * (a.H + a.Hq);
+    const dim3 grid((unsigned)((threads + 255) / 256));
+    auto go = [&](auto dhc) {
+        constexpr int D = decltype(dhc)::value;
+        if (dtype == DT_F16) hipLaunchKernelGGL((kv4_append_kernel<D, DT_F16>), grid, dim3(256), 0, stream, a);
+        else if (dtype == DT_BF16) hipLaunchKernelGGL((kv4_append_kernel<D, DT_BF16>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((kv4_append_kernel<D, DT_F32>), grid, dim3(256), 0, stream, a);
+    };
+    if (dh == 128) go(std::integral_constant<int, 128>{});
+    else go(std::integral_constant<int, 64>{});
+    LASER_HIP_CHECK(hipGetLastError());
+    return LASER_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// The values that cached tokens stand for. Four lanes per token and head, channels as in the kernel above.
+struct ReadArgs {
+    SeqList seqs;
+    const int32_t* lens; const int32_t* block_table;
+    const uint8_t* pages;
+    Heads k, v;
+    int B, n, H, mpps, start;
+};
+
+template <int DH, int DT>
+__global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
+    constexpr int NG = DH / 32;
+    const long t = (long)blockIdx.x * 256 + threadIdx.x;
+    const int g = threadIdx.x & 3, h = (int)((t >> 2) % a.H);
+    const long row = (t >> 2) / a.H;
+    if (row >= (long)a.B * a.n) return;
+    const int b = (int)(row / a.n), r = (int)(row % a.n);
+    const int id = a.seqs.slot(b);
+    const int slot = (a.start >= 0 ? a.start : a.lens[id]) + r;
+    if (slot < 0 || slot >= a.seqs.tokens(b)) return;
+    const int tp = slot % kPageSize;
+    const int pg = a.block_table[(size_t)id * a.mpps + slot / kPageSize];
+    const uint8_t* page = a.pages + ((size_t)pg * a.H + h) * page4_bytes(DH);
+    const uint32_t* kw = reinterpret_cast<const uint32_t*>(page + (g * 16 + tp) * (DH / 8));
+    const uint32_t* ksm = reinterpret_cast<const uint32_t*>(page + page4_ksm(DH)) + tp * NG;
+    const uint32_t* vsm = reinterpret_cast<const uint32_t*>(page + page4_vsm(DH)) + tp * NG;
+    const uint8_t* vp = page + page4_v(DH) + ((tp >> 2) * 16 + 4 * g) * (DH / 8) + code_byte(tp & 3);
+    const size_t ko = (size_t)b * a.k.seq + (size_t)r * a.k.row + (size_t)h * a.k.head + 8 * g;
+    const size_t vo = (size_t)b * a.v.seq + (size_t)r * a.v.row + (size_t)h * a.v.head + 4 * g;
+#pragma unroll
+    for (int c = 0; c < NG; ++c) {
+        const float ks = sm_scale(ksm[c]), km = sm_offset(ksm[c]), vs = sm_scale(vsm[c]), vm = sm_offset(vsm[c]);
+        float x[8], u[4], w[4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fmaf(ks, (float)((kw[(c & ~1) + (j >> 2)] >> (8 * code_byte(j & 3) + 4 * (c & 1))) & 15u), km);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t byte = vp[e * (DH / 8) + 4 * c];
+            u[e] = fmaf(vs, (float)(byte & 15u), vm);
+            w[e] = fmaf(vs, (float)(byte >> 4), vm);
+        }
+        store_elems<DT, 8>(a.k.p, ko + 32 * c, x);
+        store_elems<DT, 4>(a.v.p, vo + 32 * c, u);
+        store_elems<DT, 4>(a.v.p, vo + 32 * c + 16, w);
+    }
+}
+
+// laser_kv_commit_tree's move of the accepted branch (see kv_compact_kernel): a lane owns one key byte and one value byte of a
+// token's dh / 2, four of them a word of sm, and moves them branch position by branch position.
+__global__ void kv4_compact_kernel(uint8_t* pages, const int32_t* block_table, const int32_t* len, const int32_t* seq_ids,
+                                   const int32_t* accept_len, const int32_t* accept_path, int K, int H, int dh, int mpps, int n_pages) {
+    const int h = blockIdx.x, l = blockIdx.y, b = blockIdx.z, c = threadIdx.x, ng = dh / 32;
+    const int id = seq_ids[b], len0 = len[id];
+    int acc = accept_len[b];
+    acc = acc < 0 ? 0 : (acc > K ? K : acc);
+    const int32_t* bt = block_table + (size_t)id * mpps;
+    const int kb = dh / 8;                                  // bytes a lane of the page holds
+    for (int j = 0; j < acc; ++j) {
+        const int i = accept_path[(size_t)b * K + j];
+        if (i < j || i >= K) break;
+        if (i == j) continue;
+        const int src = len0 + 1 + i, dst = len0 + 1 + j, st = src % kPageSize, dt = dst % kPageSize;
+        const uint8_t* sp = pages + (((size_t)l * n_pages + bt[src / kPageSize]) * H + h) * page4_bytes(dh);
+        uint8_t* dp = pages + (((size_t)l * n_pages + bt[dst / kPageSize]) * H + h) * page4_bytes(dh);
+        if (c < dh / 2) {
+            dp[(c / kb * 16 + dt) * kb + c % kb] = sp[(c / kb * 16 + st) * kb + c % kb];
+            const int r = c / ng, p = c % ng;
+            dp[page4_v(dh) + ((dt >> 2) * 16 + r) * kb + 4 * p + code_byte(dt & 3)] = sp[page4_v(dh) + ((st >> 2) * 16 + r) * kb + 4 * p + code_byte(st & 3)];
+        }
+        if (c < 2 * ng) {
+            const int o = (c < ng ? page4_ksm(dh) : page4_vsm(dh)) + 4 * (c % ng);
+            *reinterpret_cast<uint32_t*>(dp + o + 4 * ng * dt) = *reinterpret_cast<const uint32_t*>(sp + o + 4 * ng * st);
+        }
+    }
+}
+
+int launch_kv4_compact(const KV* kv, const int32_t* ids_dev, const int32_t* accept_len, const int32_t* accept_path, int B, int K, hipStream_t stream) {
+    hipLaunchKernelGGL(kv4_compact_kernel, dim3(kv->d.n_heads, kv->d.n_layers, B), dim3(64), 0, stream, kv->pages4, kv->block_table, kv->len,
+                       ids_dev, accept_len, accept_path, K, kv->d.n_heads, kv->d.head_dim, kv->d.max_pages_per_seq, kv->d.n_pages);
+    LASER_HIP_CHECK(hipGetLastError());
+    return LASER_OK;
+}
+
+__global__ void rope_table4_kernel(float2* tab, int max_pos, int half, double base) {
+    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= (size_t)max_pos * half) return;
+    const double ang = (double)(i / half) * pow(base, -(double)(i % half) / (double)half);
+    tab[i] = make_float2((float)cos(ang), (float)sin(ang));
+}
+
+// ---- checks that the three calls share -----------------------------------------------------------
+static int check_four_bit(const KV* kv, int layer, const int32_t* seq_ids, int B, int dtype) {
+    LASER_REQUIRE(kv != nullptr, LASER_E_INVALID_ARG, "kv is NULL");
+    LASER_REQUIRE(kv->pages4 != nullptr, LASER_E_SHAPE, "the cache was not made by laser_kv_create_4bit");
+    LASER_REQUIRE(layer >= 0 && layer < kv->d.n_layers, LASER_E_INVALID_ARG, "layer %d out of range", layer);
+    LASER_REQUIRE(dtype == LASER_F16 || dtype == LASER_BF16 || dtype == LASER_F32, LASER_E_INVALID_ARG, "unknown dtype %d", dtype);
+    LASER_REQUIRE(B >= 0 && B <= kv->d.max_seqs, LASER_E_INVALID_ARG, "B %d outside 0..max_seqs %d", B, kv->d.max_seqs);
+    LASER_REQUIRE(B == 0 || seq_ids, LASER_E_INVALID_ARG, "seq_ids is NULL");
+    std::vector<char> seen(kv->d.max_seqs, 0);
+    for (int b = 0; b < B; ++b) {
+        const int s = seq_ids[b];
+        LASER_REQUIRE(s >= 0 && s < kv->d.max_seqs, LASER_E_INVALID_ARG, "sequence slot %d out of range", s);
+        LASER_REQUIRE(!seen[s], LASER_E_INVALID_ARG, "sequence slot %d appears twice", s);
+        seen[s] = 1;
+    }
+    return LASER_OK;
+}
+
+static int check_heads(const laser_heads* t, const char* name, int dtype) {
+    LASER_REQUIRE(t && t->data, LASER_E_INVALID_ARG, "%s is NULL", name);
+    LASER_REQUIRE(t->seq >= 0 && t->row >= 0 && t->head >= 0, LASER_E_INVALID_ARG, "%s: negative stride", name);
+    LASER_REQUIRE((uintptr_t)t->data % dtype_bytes(dtype) == 0, LASER_E_INVALID_ARG, "%s is not aligned to its elements", name);
+    return LASER_OK;
+}
+
+static Heads heads_from(const laser_heads* t, int b0, int dtype) {
+    if (!t || !t->data) return Heads{nullptr, 0, 0, 0};
+    return Heads{(char*)t->data + (size_t)b0 * t->seq * dtype_bytes(dtype), t->seq, t->row, t->head};
+}
+
+static void fill_seqs(const KV* kv, const int32_t* ids, int B, SeqList& s) {
+    s.dev = nullptr;
+    s.cap_all = 0;
+    for (int b = 0; b < B; ++b) { s.id[b] = ids[b]; s.cap[b] = kv->h_npages[ids[b]] * kPageSize; }
+}
+
+static int check_rows(const KV* kv, const int32_t* seq_ids, int B, int R) {
+    LASER_REQUIRE(R >= 1 && R <= LASER_MAX_DRAFT + 1, LASER_E_INVALID_ARG, "R %d outside 1..%d", R, LASER_MAX_DRAFT + 1);
+    for (int b = 0; b < B; ++b) {
+        const int s = seq_ids[b];
+        LASER_REQUIRE(kv->h_len_ub[s] + R <= kv->h_npages[s] * kPageSize, LASER_E_OOM_PAGES, "slot %d: length bound %d + %d rows exceeds the %d tokens reserved",
+                      s, kv->h_len_ub[s], R, kv->h_npages[s] * kPageSize);
+    }
+    return LASER_OK;
+}
+
+static uint8_t* layer_pages(const KV* kv, int layer) {
+    return kv->pages4 + (size_t)layer * kv->d.n_pages * kv->d.n_heads * page4_bytes(kv->d.head_dim);
+}
+
+int kv4_import(KV* kv, int seq, int layer, const uint16_t* k, const uint16_t* v, int n_tokens, hipStream_t stream) {
+    const int64_t row = (int64_t)kv->d.n_heads * kv->d.head_dim;
+    AppendArgs a{};
+    fill_seqs(kv, &seq, 1, a.seqs);
+    a.block_table = kv->block_table;
+    a.pages = layer_pages(kv, layer);
+    a.k = Heads{(void*)k, 0, row, kv->d.head_dim};
+    a.v = Heads{(void*)v, 0, row, kv->d.head_dim};
+    a.B = 1; a.R = n_tokens; a.H = kv->d.n_heads; a.mpps = kv->d.max_pages_per_seq; a.n_part = 1;
+    return launch_kv4_append(a, kv->d.head_dim, DT_F16, stream);
+}
+
+}  // namespace laser
+
+using namespace laser;
+
+extern "C" int laser_rope_table(float* table, int max_pos, int rope_dim, double base, void* stream) {
+    LASER_REQUIRE(table != nullptr, LASER_E_INVALID_ARG, "table is NULL");
+    LASER_REQUIRE(max_pos > 0 && rope_dim > 0 && rope_dim % 2 == 0 && base > 0.0, LASER_E_INVALID_ARG, "bad size or base");
+    const size_t n = (size_t)max_pos * (rope_dim / 2);
+    LASER_REQUIRE((n + 255) / 256 < (1ull << 31), LASER_E_LIMIT, "table too large");
+    hipLaunchKernelGGL(rope_table4_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, (hipStream_t)stream, (float2*)table, max_pos, rope_dim / 2, base);
+    LASER_HIP_CHECK(hipGetLastError());
+    return LASER_OK;
+}
+
+extern "C" int laser_kv_append(laser_kv* h, int layer, const int32_t* seq_ids, const int32_t* n_rows, const int32_t* tree_parent,
+                               int B, int R, int dtype, const laser_heads* k, const laser_heads* v, const laser_heads* q,
+                               const laser_heads* q_out, int n_heads, const float* rope, int rope_dim, int max_pos, void* stream) {
+    KV* kv = reinterpret_cast<KV*>(h);
+    int rc = check_four_bit(kv, layer, seq_ids, B, dtype);
+    if (rc) return rc;
+    if ((rc = check_rows(kv, seq_ids, B, R))) return rc;
+    if (B == 0) return LASER_OK;
+    if ((rc = check_heads(k, "k", dtype)) || (rc = check_heads(v, "v", dtype))) return rc;
+    LASER_REQUIRE(n_heads >= 0 && n_heads <= (1 << 20), LASER_E_INVALID_ARG, "n_heads %d out of range", n_heads);
+    if (n_heads > 0 && ((rc = check_heads(q, "q", dtype)) || (rc = check_heads(q_out, "q_out", dtype)))) return rc;
+    const int dh = kv->d.head_dim;
+    LASER_REQUIRE(rope_dim == 0 || rope_dim == dh || (rope_dim == 64 && dh == 128), LASER_E_SHAPE, "rope_dim %d: 0, 64 or head_dim", rope_dim);
+    if (rope_dim) {
+        LASER_REQUIRE(rope != nullptr && (uintptr_t)rope % 8 == 0, LASER_E_INVALID_ARG, "rope is NULL or not aligned to 8 bytes");
+        LASER_REQUIRE(max_pos > 0, LASER_E_INVALID_ARG, "max_pos must be positive");
+        for (int b = 0; b < B; ++b)
+            LASER_REQUIRE(kv->h_len_ub[seq_ids[b]] + R <= max_pos, LASER_E_LIMIT, "slot %d: position would exceed max_pos %d", seq_ids[b], max_pos);
+    }
+    for (int b0 = 0; b0 < B; b0 += kSeqChunk) {
+        AppendArgs a{};
+        a.B = std::min(kSeqChunk, B - b0);
+        fill_seqs(kv, seq_ids + b0, a.B, a.seqs);
+        a.lens = kv->len; a.block_table = kv->block_table;
+        a.pages = layer_pages(kv, layer);
+        a.n_rows = n_rows ? n_rows + b0 : nullptr;
+        a.parent = tree_parent && R > 1 ? tree_parent + (size_t)b0 * (R - 1) : nullptr;
+        a.rope = (const float2*)rope;
+        a.k = heads_from(k, b0, dtype); a.v = heads_from(v, b0, dtype);
+        if (n_heads > 0) { a.q = heads_from(q, b0, dtype); a.q_out = heads_from(q_out, b0, dtype); }
+        a.R = R; a.H = kv->d.n_heads; a.Hq = n_heads; a.mpps = kv->d.max_pages_per_seq; a.start = -1;
+        a.rope_dim = rope_dim; a.max_pos = max_pos; a.n_part = 1;
+        if ((rc = launch_kv4_append(a, dh, dtype, (hipStream_t)stream))) return rc;
+    }
+    for (int b = 0; b < B; ++b) kv->h_last_rows[seq_ids[b]] = R;         // what a commit may add
+    return LASER_OK;
+}
+
+extern "C" int laser_kv_attend(laser_kv* h, int layer, const int32_t* seq_ids, const int32_t* n_rows, const int32_t* tree_parent,
+                               int B, int R, int n_heads, int dtype, const laser_heads* q, float scale, const laser_heads* out, void* stream) {
+    KV* kv = reinterpret_cast<KV*>(h);
+    int rc = check_four_bit(kv, layer, seq_ids, B, dtype);
+    if (rc) return rc;
+    if ((rc = check_rows(kv, seq_ids, B, R))) return rc;
+    if (B == 0) return LASER_OK;
+    if ((rc = check_heads(q, "q", dtype)) || (rc = check_heads(out, "out", dtype))) return rc;
+    LASER_REQUIRE(n_heads > 0 && n_heads % kv->d.n_heads == 0, LASER_E_SHAPE, "n_heads %d is not a multiple of the cache's %d", n_heads, kv->d.n_heads);
+    LASER_REQUIRE(n_heads / kv->d.n_heads <= 256, LASER_E_LIMIT, "more than 256 query heads per key/value head");
+    LASER_REQUIRE(std::isfinite(scale), LASER_E_INVALID_ARG, "scale is not finite");
+    for (int b0 = 0; b0 < B; b0 += kSeqChunk) {
+        AttendArgs a{};
+        a.B = std::min(kSeqChunk, B - b0);
+        fill_seqs(kv, seq_ids + b0, a.B, a.seqs);
+        int most = 0;
+        for (int b = b0; b < b0 + a.B; ++b) most = std::max(most, kv->h_len_ub[seq_ids[b]] + R);
+        a.lens = kv->len; a.block_table = kv->block_table;
+        a.pages = layer_pages(kv, layer);
+        a.n_rows = n_rows ? n_rows + b0 : nullptr;
+        a.parent = tree_parent && R > 1 ? tree_parent + (size_t)b0 * (R - 1) : nullptr;
+        a.q = heads_from(q, b0, dtype); a.out = heads_from(out, b0, dtype);
+        a.part = kv->part4;
+        a.R = R; a.H = kv->d.n_heads; a.G = n_heads / kv->d.n_heads; a.mpps = kv->d.max_pages_per_seq;
+        a.scale_log2 = scale * 1.44269504f;
+        if ((rc = launch_kv4_attend(a, kv->d.head_dim, dtype, most, (hipStream_t)stream))) return rc;
+    }
+    return LASER_OK;
+}
+
+extern "C" int laser_kv_read(laser_kv* h, int layer, const int32_t* seq_ids, int B, int start, int n, int dtype, const laser_heads* k,
+                             const laser_heads* v, void* stream) {
+    KV* kv = reinterpret_cast<KV*>(h);
+    int rc = check_four_bit(kv, layer, seq_ids, B, dtype);
+    if (rc) return rc;
+    LASER_REQUIRE(start >= -1 && n >= 0, LASER_E_INVALID_ARG, "start %d, n %d", start, n);
+    for (int b = 0; b < B; ++b) {
+        const int s = seq_ids[b], first = start >= 0 ? start : kv->h_len_ub[s];
+        LASER_REQUIRE((long)first + n <= (long)kv->h_npages[s] * kPageSize, LASER_E_OOM_PAGES, "slot %d: tokens %d .. %ld exceed the %d reserved", s, first,
+                      (long)first + n, kv->h_npages[s] * kPageSize);
+    }
+    if (B == 0 || n == 0) return LASER_OK;
+    if ((rc = check_heads(k, "k", dtype)) || (rc = check_heads(v, "v", dtype))) return rc;
+    for (int b0 = 0; b0 < B; b0 += kSeqChunk) {
+        ReadArgs a{};
+        a.B = std::min(kSeqChunk, B - b0);
+        fill_seqs(kv, seq_ids + b0, a.B, a.seqs);
+        a.lens = kv->len; a.block_table = kv->block_table;
+        a.pages = layer_pages(kv, layer);
+        a.k = heads_from(k, b0, dtype); a.v = heads_from(v, b0, dtype);
+        a.n = n; a.H = kv->d.n_heads; a.mpps = kv->d.max_pages_per_seq; a.start = start;
+        const dim3 grid((unsigned)(((long)a.B * n * a.H * 4 + 255) / 256));
+        auto go = [&](auto dhc) {
+            constexpr int D = decltype(dhc)::value;
+            if (dtype == DT_F16) hipLaunchKernelGGL((kv4_read_kernel<D, DT_F16>), grid, dim3(256), 0, (hipStream_t)stream, a);
+            else if (dtype == DT_BF16) hipLaunchKernelGGL((kv4_read_kernel<D, DT_BF16>), grid, dim3(256), 0, (hipStream_t)stream, a);
+            else hipLaunchKernelGGL((kv4_read_kernel<D, DT_F32>), grid, dim3(256), 0, (hipStream_t)stream, a);
+        };
+        if (kv->d.head_dim == 128) go(std::integral_constant<int, 128>{});
+        else go(std::integral_constant<int, 64>{});
+        LASER_HIP_CHECK(hipGetLastError());
+    }
+    return LASER_OK;
+}

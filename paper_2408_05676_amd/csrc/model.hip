@@ -5,6 +5,7 @@
 #include <string>
 #include <vector>
 
+#include "four_bit.h"
 #include "gemm_tile_plan.h"
 #include "gemm_skinny.h"
 #include "gemm_mid.h"
@@ -777,6 +778,40 @@ static void copies_for_few_rows(Model* m, hipStream_t stream) {
     if (m->no_few_copies) (void)hipGetLastError();
 }
 
+// A layer's rotary positions, cache write and attention on a 4-bit cache. The qkv rows (the sums of n_part arrays, see RopeArgs) go in as
+// fp32; rotated queries replace the first array's and are read back by the attention, whose result is split into two planes.
+static int four_bit_attention(Model* m, KV* kv, const int32_t* ids_dev, const RopeArgs& ra, int layer, int B, int R, int max_tokens, hipStream_t stream) {
+    const int dm = m->d.d_model, H = m->d.n_heads, dh = m->dh;
+    const int64_t row = 3 * (int64_t)dm;
+    float* qkv = const_cast<float*>(ra.qkv);
+    AppendArgs ap{};
+    ap.seqs.dev = ids_dev;
+    ap.seqs.cap_all = kv->d.max_pages_per_seq * kPageSize;
+    ap.lens = kv->len; ap.block_table = kv->block_table;
+    ap.pages = kv->pages4 + (size_t)layer * kv->d.n_pages * H * page4_bytes(dh);
+    ap.row_pos = m->row_pos;
+    ap.rope = m->rope;
+    ap.q = Heads{qkv, R * row, row, dh};
+    ap.k = Heads{qkv + dm, R * row, row, dh};
+    ap.v = Heads{qkv + 2 * dm, R * row, row, dh};
+    ap.q_out = ap.q;
+    ap.B = B; ap.R = R; ap.H = H; ap.Hq = H; ap.mpps = kv->d.max_pages_per_seq; ap.start = -1; ap.rope_dim = dh; ap.max_pos = m->d.max_pos;
+    ap.n_part = ra.n_part; ap.part_stride = (int64_t)ra.part_stride;
+    if (const int rc = launch_kv4_append(ap, dh, DT_F32, stream)) return rc;
+    AttendArgs at{};
+    at.seqs = ap.seqs;
+    at.lens = kv->len; at.block_table = kv->block_table;
+    at.pages = ap.pages;
+    at.row_anc = m->row_anc;
+    at.q = ap.q_out;
+    at.out = Heads{m->attn, (int64_t)R * dm, dm, dh};
+    at.out_lo = m->attn_lo;
+    at.part = kv->part4;
+    at.B = B; at.R = R; at.H = H; at.G = 1; at.mpps = kv->d.max_pages_per_seq;
+    at.scale_log2 = 1.44269504f / sqrtf((float)dh);
+    return launch_kv4_attend(at, dh, DT_F32, max_tokens, stream);
+}
+
 // parent: NULL for a chain of drafts, else the token tree's parent array (see tree_parent_of)
 static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pending, const int32_t* drafts,
                    const int32_t* parent, const int32_t* draft_len, int B, int K, int max_len_ub, hipStream_t stream) {
@@ -826,6 +861,9 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
         RopeArgs ra{g.n_part ? m->kpart : m->qkv, m->row_pos, m->row_slot, ids_dev, kv->block_table, m->rope, m->q, m->q_lo, kv->kpages, kv->klpages, kv->vpages,
                     R, dm, d.n_heads, m->dh, kv->d.max_pages_per_seq, l, kv->d.n_pages,
                     M, std::max(1, std::min(4, dm / 2048)), B, std::max(1, g.n_part), (size_t)M * 3 * dm};
+        if (kv->pages4) {                            // a 4-bit cache: the kernels of laser_kv_append and laser_kv_attend
+            if ((rc = four_bit_attention(m, kv, ids_dev, ra, l, B, R, max_len_ub + R, stream))) return rc;
+        } else {
         const int v_blocks = (B * d.n_heads + 256 / m->dh - 1) / (256 / m->dh) * ((R + 2 * kPageSize - 2) / kPageSize);
         const dim3 rg((unsigned)(M * ra.ny + v_blocks));
         switch (ra.n_part) {
@@ -852,6 +890,7 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
             dim3 cg(d.n_heads, B * nqt);
             if (m->dh == 128) hipLaunchKernelGGL(attn_combine_kernel<128>, cg, dim3(256), 0, stream, aa);
             else hipLaunchKernelGGL(attn_combine_kernel<64>, cg, dim3(256), 0, stream, aa);
+        }
         }
         GemmArgs go{d.wo + (size_t)l * dm * dm, many ? m->w16[1] + (size_t)l * dm * dm : nullptr, m->attn, m->attn_lo, M, dm, dm, 1, m->x, nullptr};
         go.part = m->kpart; go.part_floats = m->kpart_floats; go.want_split = m->ksplit_opt[1]; go.mid_waves = m->mid_waves; go.want_tile = m->tile;
@@ -1006,7 +1045,7 @@ static int verify_impl(laser_model* mh, laser_kv* kh, const int32_t* seq_ids, co
     }
     const int32_t* ids_dev = nullptr;
     if ((rc = kv->stage_ids(seq_ids, B, stream, &ids_dev))) return rc;
-    const bool fused = m->use_fused && fused_supported(m, B, K, max_ub);
+    const bool fused = m->use_fused && !kv->pages4 && fused_supported(m, B, K, max_ub);
     if (fused || (B * R > 16 && B * R <= kSkinnyMaxRows)) copies_for_few_rows(m, stream);
     if (fused) {
         if (parent)          // token tree: positions (depth) and ancestor masks of the rows

@@ -30,6 +30,8 @@ struct KV {
     uint16_t* kpages = nullptr;
     uint8_t* klpages = nullptr;       // 8-bit low plane of the split keys: k = kpages + klpages / 4096
     uint16_t* vpages = nullptr;
+    uint8_t* pages4 = nullptr;        // a 4-bit cache has these instead (four_bit.h), and
+    float* part4 = nullptr;           // the attention's results of context parts, of a fixed size
     int32_t* block_table = nullptr;   // [dev] [max_seqs][max_pages_per_seq]
     int32_t* len = nullptr;           // [dev] [max_seqs] committed tokens
     // host bookkeeping

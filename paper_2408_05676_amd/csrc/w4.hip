@@ -1,0 +1,291 @@
+// Products of rows with 4-bit weights: out[M][N] = x[M][Kd] W^T, W[n][i] = m + s c of its group (laser.h).
+//
+// A handle keeps, for every tile of 16 outputs, blocks of 128 inputs one after the other: 1 KB of codes as the 64 lanes of a wave
+// hold a matrix operand (lane (r = lane % 16, g = lane / 16): output r, inputs 32 c + 8 g .. + 7 in word c) and the 16 x (128 / group)
+// scales and offsets. A wave streams the blocks of its tiles over its share of the inputs; per group
+//   D = sum c x (matrix instructions on the bare codes), X = sum x (one more, with ones), acc += s D + m X in fp32.
+// Codes enter as 16-bit floats: for fp16 rows a code masked out of its word is the subnormal c 2^-24, for bf16 rows it is put under the
+// exponent of 128 and stands for 128 + c, which the offset m - 128 s takes back.
+// Bound: the weights' way from memory.
+#include <algorithm>
+#include <vector>
+
+#include "four_bit.h"
+
+namespace laser {
+
+struct W4 { int N, Kd, group, nkb; uint8_t* blocks; };
+
+constexpr int block_bytes(int ng) { return 1024 + 64 * ng; }      // ng = groups of a block
+
+// ------------------------------------------------------------------------------------------------
+// A thread per word of codes, and the first 16 ng of a block for its scales and offsets. Outputs and inputs beyond the matrix are zeros.
+__global__ __launch_bounds__(256) void w4_layout_kernel(const uint8_t* codes, const uint16_t* scales, const uint16_t* offsets, int N, int Kd, int group,
+                                                        int nkb, uint8_t* blocks) {
+    const size_t blk = blockIdx.x;
+    const int tile = (int)(blk / nkb), kb = (int)(blk % nkb), ng = 128 / group, t = threadIdx.x;
+    uint8_t* out = blocks + blk * block_bytes(ng);
+    {
+        const int lane = t >> 2, c = t & 3, n = tile * 16 + (lane & 15), i = kb * 128 + 32 * c + 8 * (lane >> 4);
+        uint32_t w = 0;
+        if (n < N && i < Kd)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {                         // element j: bits 4 (j / 2) of half j % 2
+                const uint32_t byte = codes[((size_t)n * Kd + i + j) >> 1];
+                w |= ((j & 1 ? byte >> 4 : byte) & 15u) << (4 * (j >> 1) + 16 * (j & 1));
+            }
+        reinterpret_cast<uint32_t*>(out)[t] = w;
+    }
+    if (t < 16 * ng) {
+        const int n = tile * 16 + t / ng, gi = kb * ng + t % ng, per = Kd / group;
+        uint32_t sm = 0;
+        if (n < N && gi < per) sm = (uint32_t)scales[(size_t)n * per + gi] | ((uint32_t)offsets[(size_t)n * per + gi] << 16);
+        reinterpret_cast<uint32_t*>(out + 1024)[t] = sm;
+    }
+}
+
+// Eight threads per group of a bf16 matrix.
+__global__ __launch_bounds__(256) void w4_quantize_kernel(const uint16_t* w, size_t groups, int group, uint8_t* codes, uint16_t* scales, uint16_t* offsets) {
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int lane = threadIdx.x & 7, per = group / 8;            // elements a thread takes: 4, 8 or 16
+    if (i >= groups) return;                                      // (eight lanes together)
+    const uint16_t* p = w + i * group + lane * per;
+    float lo = INFINITY, hi = -INFINITY;
+    for (int j = 0; j < per; ++j) { const float x = bf16_to_f32(p[j]); lo = fminf(lo, x); hi = fmaxf(hi, x); }
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) { lo = fminf(lo, __shfl_xor(lo, o)); hi = fmaxf(hi, __shfl_xor(hi, o)); }
+    const _Float16 s = f64_to_f16(fmin(((double)hi - (double)lo) / 15.0, 65504.0)), m = (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f);
+    auto code = [&](uint16_t h) {
+        const double n = rint(((double)bf16_to_f32(h) - (double)(float)m) / (double)(float)s);
+        return (float)s > 0.f ? (uint32_t)fmin(fmax(n, 0.0), 15.0) : 0u;
+    };
+    uint8_t* q = codes + (i * group + lane * per) / 2;
+    for (int j = 0; j < per; j += 2) q[j / 2] = (uint8_t)(code(p[j]) | (code(p[j + 1]) << 4));
+    if (lane == 0) { scales[i] = __builtin_bit_cast(uint16_t, s); offsets[i] = __builtin_bit_cast(uint16_t, m); }
+}
+
+// ------------------------------------------------------------------------------------------------
+struct W4Args {
+    const uint8_t* blocks;
+    const uint16_t* x; uint16_t* out;
+    int64_t x_stride, out_stride;
+    int M, N, Kd, nkb, tiles;
+};
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+template <bool BF>
+__device__ inline float4_t mfma_x(const Frag8& a, const Frag8& b, float4_t c) {
+    if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a.v4), __builtin_bit_cast(bf16x8_t, b.v4), c, 0, 0, 0);
+    else return mfma_16x16x32(a, b, c);
+}
+
+// BF: bf16 rows (else fp16). NG: groups of a block. MT: 16-row tiles. NT: 16-output tiles of a wave. WK: waves that share the inputs.
+template <bool BF, int NG, int MT, int NT, int WK>
+__global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
+    constexpr int kDepth = MT * 4 + NT <= 6 ? 3 : 2;               // blocks in flight per wave
+    constexpr int CPG = 4 / NG;                                    // 32-input pieces of a group
+    extern __shared__ float lds[];                                 // [WK][NT][MT][16 rows][16 outputs]
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int tile0 = blockIdx.x * NT, row0 = blockIdx.y * (MT * 16);
+    const int k0 = (int)((long)a.nkb * wave / WK), k1 = (int)((long)a.nkb * (wave + 1) / WK);
+    const uint8_t* wp[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) wp[n] = a.blocks + (size_t)min(tile0 + n, a.tiles - 1) * a.nkb * block_bytes(NG);
+    const uint16_t* xp[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) xp[m] = a.x + (size_t)min(row0 + m * 16 + r, a.M - 1) * a.x_stride + 8 * g;
+    // lane r of a row of sixteen keeps the scale of output 4 g + r / NG, group r % NG
+    const int sm_at = 1024 + 4 * (4 * g * NG + (lane & (4 * NG - 1)));
+
+    u32x4 wq[kDepth][NT];
+    uint32_t smq[kDepth][NT];
+    Frag8 xq[kDepth][MT][4];
+    auto load = [&](auto slot, int kb) {
+        constexpr int s = decltype(slot)::value;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint8_t* p = wp[n] + (size_t)kb * block_bytes(NG);
+            wq[s][n] = *reinterpret_cast<const u32x4*>(p + lane * 16);
+            smq[s][n] = *reinterpret_cast<const uint32_t*>(p + sm_at);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = kb * 128 + 32 * c;                   // past the last input (a padded block): zeros
+                u32x4 v = {0, 0, 0, 0};
+                if (i < a.Kd) v = *reinterpret_cast<const u32x4_a2*>(xp[m] + i);
+                xq[s][m][c].v4 = v;
+            }
+    };
+    Frag8 ones;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ones.w[i] = BF ? 0x3F803F80u : 0x3C003C00u;
+    constexpr uint32_t kBias = BF ? 0x43004300u : 0u;
+
+    float4_t acc[NT][MT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = float4_t{0.f, 0.f, 0.f, 0.f};
+
+    auto multiply = [&](auto slot) {
+        constexpr int s = decltype(slot)::value;
+        float ss[NT], mm[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float sc = sm_scale(smq[s][n]);
+            ss[n] = BF ? sc : sc * kCodeUnit;
+            mm[n] = BF ? fmaf(-128.f, sc, sm_offset(smq[s][n])) : sm_offset(smq[s][n]);
+        }
+        static_for<0, NG>([&](auto gg) {
+            constexpr int gi = decltype(gg)::value;
+            float4_t X[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                X[m] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < CPG; ++c) X[m] = mfma_x<BF>(ones, xq[s][m][gi * CPG + c], X[m]);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                Frag8 wf[CPG];
+#pragma unroll
+                for (int c = 0; c < CPG; ++c)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) wf[c].w[j] = ((wq[s][n][gi * CPG + c] >> (4 * j)) & kCodeLo) | kBias;
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    float4_t D = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < CPG; ++c) D = mfma_x<BF>(wf[c], xq[s][m][gi * CPG + c], D);
+                    static_for<0, 4>([&](auto ii) {
+                        constexpr int i = decltype(ii)::value;
+                        acc[n][m][i] = fmaf(row_lane<i * NG + gi>(ss[n]), D[i], acc[n][m][i]);
+                        acc[n][m][i] = fmaf(row_lane<i * NG + gi>(mm[n]), X[m][i], acc[n][m][i]);
+                    });
+                }
+            }
+        });
+    };
+    static_for<0, kDepth>([&](auto s) { if (k0 + decltype(s)::value < k1) load(s, k0 + decltype(s)::value); });
+    for (int kb = k0; kb < k1; kb += kDepth)
+        static_for<0, kDepth>([&](auto s) {
+            constexpr int j = decltype(s)::value;
+            if (kb + j < k1) {
+                multiply(s);
+                if (kb + j + kDepth < k1) load(s, kb + j + kDepth);
+            }
+        });
+
+    // ---- the waves' sums, in their order
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+            *reinterpret_cast<float4_t*>(lds + (((size_t)wave * NT + n) * MT + m) * 256 + r * 16 + 4 * g) = acc[n][m];   // [row r][output 4 g + i]
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < NT * MT * 256; idx += WK * 64) {
+        const int o = idx & 15, n = idx >> 4 & (NT - 1), row = idx / (16 * NT);        // outputs of a row side by side
+        const int at = (n * MT + (row >> 4)) * 256 + (row & 15) * 16 + o;
+        float v = lds[at];
+#pragma unroll
+        for (int w = 1; w < WK; ++w) v += lds[w * NT * MT * 256 + at];
+        const int gr = row0 + row, gn = (tile0 + n) * 16 + o;
+        if (gr < a.M && gn < a.N) a.out[(size_t)gr * a.out_stride + gn] = BF ? f32_to_bf16(v) : f32_to_f16(v);
+    }
+}
+
+template <bool BF, int NG, int MT>
+static void launch_w4(const W4Args& a, hipStream_t stream) {
+    auto go = [&](auto nt, auto wk) {
+        constexpr int NT = decltype(nt)::value, WK = decltype(wk)::value;
+        const dim3 grid((unsigned)((a.tiles + NT - 1) / NT), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
+        hipLaunchKernelGGL((w4_matmul_kernel<BF, NG, MT, NT, WK>), grid, dim3(WK * 64), WK * NT * MT * 1024, stream, a);
+    };
+    if (a.tiles >= 1024) go(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+    else go(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+}
+
+template <bool BF, int NG>
+static void launch_rows(const W4Args& a, hipStream_t stream) {
+    const int mt = std::min(5, (a.M + 15) / 16);
+    switch (mt) {
+        case 1: launch_w4<BF, NG, 1>(a, stream); break;
+        case 2: launch_w4<BF, NG, 2>(a, stream); break;
+        case 3: launch_w4<BF, NG, 3>(a, stream); break;
+        case 4: launch_w4<BF, NG, 4>(a, stream); break;
+        default: launch_w4<BF, NG, 5>(a, stream); break;
+    }
+}
+
+}  // namespace laser
+
+using namespace laser;
+
+static int check_w4(int N, int Kd, int group) {
+    LASER_REQUIRE(group == 32 || group == 64 || group == 128, LASER_E_SHAPE, "group %d: 32, 64 or 128", group);
+    LASER_REQUIRE(N > 0 && Kd > 0, LASER_E_INVALID_ARG, "N and Kd must be positive");
+    LASER_REQUIRE(Kd % group == 0, LASER_E_SHAPE, "Kd %d is not a multiple of the group, %d", Kd, group);
+    LASER_REQUIRE(((long)N + 15) / 16 * ((Kd + 127) / 128) < (1l << 31), LASER_E_LIMIT, "matrix too large");
+    return LASER_OK;
+}
+
+extern "C" int laser_w4_create(const uint8_t* codes, const uint16_t* scales, const uint16_t* offsets, int N, int Kd, int group, void* stream, laser_w4** out) {
+    LASER_REQUIRE(codes && scales && offsets && out, LASER_E_INVALID_ARG, "NULL argument");
+    if (const int rc = check_w4(N, Kd, group)) return rc;
+    LASER_REQUIRE((uintptr_t)scales % 2 == 0 && (uintptr_t)offsets % 2 == 0, LASER_E_INVALID_ARG, "scales or offsets are not aligned to their elements");
+    W4* w = new W4{N, Kd, group, (Kd + 127) / 128, nullptr};
+    const size_t n_blocks = (size_t)((N + 15) / 16) * w->nkb;
+    auto fail = [&](hipError_t e, const char* what) {
+        set_error("%s: %s", what, hipGetErrorString(e));
+        laser_w4_destroy(reinterpret_cast<laser_w4*>(w));
+        return LASER_E_HIP;
+    };
+    hipError_t e = hipMalloc((void**)&w->blocks, n_blocks * block_bytes(128 / group));
+    if (e != hipSuccess) return fail(e, "hipMalloc");
+    hipLaunchKernelGGL(w4_layout_kernel, dim3((unsigned)n_blocks), dim3(256), 0, (hipStream_t)stream, codes, scales, offsets, N, Kd, group, w->nkb, w->blocks);
+    if ((e = hipGetLastError()) != hipSuccess) return fail(e, "w4_layout_kernel");
+    if ((e = hipStreamSynchronize((hipStream_t)stream)) != hipSuccess) return fail(e, "hipStreamSynchronize");
+    *out = reinterpret_cast<laser_w4*>(w);
+    return LASER_OK;
+}
+
+extern "C" int laser_w4_destroy(laser_w4* h) {
+    W4* w = reinterpret_cast<W4*>(h);
+    if (!w) return LASER_OK;
+    if (w->blocks) (void)hipFree(w->blocks);
+    delete w;
+    return LASER_OK;
+}
+
+extern "C" int laser_w4_quantize(const uint16_t* w, int N, int Kd, int group, uint8_t* codes, uint16_t* scales, uint16_t* offsets, void* stream) {
+    LASER_REQUIRE(w && codes && scales && offsets, LASER_E_INVALID_ARG, "NULL argument");
+    if (const int rc = check_w4(N, Kd, group)) return rc;
+    const size_t groups = (size_t)N * (Kd / group);
+    hipLaunchKernelGGL(w4_quantize_kernel, dim3((unsigned)((groups * 8 + 255) / 256)), dim3(256), 0, (hipStream_t)stream, w, groups, group, codes, scales, offsets);
+    LASER_HIP_CHECK(hipGetLastError());
+    return LASER_OK;
+}
+
+extern "C" int laser_w4_matmul(const laser_w4* h, const void* x, int64_t x_stride, int M, int dtype, void* out, int64_t out_stride, void* stream) {
+    const W4* w = reinterpret_cast<const W4*>(h);
+    LASER_REQUIRE(w != nullptr, LASER_E_INVALID_ARG, "w is NULL");
+    LASER_REQUIRE(dtype == LASER_F16 || dtype == LASER_BF16, LASER_E_INVALID_ARG, "dtype %d: LASER_F16 or LASER_BF16", dtype);
+    LASER_REQUIRE(M >= 0 && M <= 65535 * 80, LASER_E_INVALID_ARG, "M %d out of range", M);
+    LASER_REQUIRE(x_stride >= w->Kd && out_stride >= w->N, LASER_E_INVALID_ARG, "rows overlap: strides %lld, %lld", (long long)x_stride, (long long)out_stride);
+    if (M == 0) return LASER_OK;
+    LASER_REQUIRE(x && out, LASER_E_INVALID_ARG, "NULL argument");
+    LASER_REQUIRE((uintptr_t)x % 2 == 0 && (uintptr_t)out % 2 == 0, LASER_E_INVALID_ARG, "x or out is not aligned to its elements");
+    const W4Args a{w->blocks, (const uint16_t*)x, (uint16_t*)out, x_stride, out_stride, M, w->N, w->Kd, w->nkb, (w->N + 15) / 16};
+    auto go = [&](auto bf) {
+        constexpr bool BF = decltype(bf)::value;
+        if (w->group == 128) launch_rows<BF, 1>(a, (hipStream_t)stream);
+        else if (w->group == 64) launch_rows<BF, 2>(a, (hipStream_t)stream);
+        else launch_rows<BF, 4>(a, (hipStream_t)stream);
+    };
+    if (dtype == LASER_BF16) go(std::true_type{});
+    else go(std::false_type{});
+    LASER_HIP_CHECK(hipGetLastError());
+    return LASER_OK;
+}
