@@ -22,17 +22,19 @@ constexpr float kCodeUnit = 16777216.f;              // 2^24: what a code masked
 // 2 (j / 2) and 2 (j / 2) + 1 in its two halves.
 __host__ __device__ constexpr int code_byte(int j) { return (j >> 1) + 2 * (j & 1); }
 
-// One page of one head in the 4-bit cache: 16 tokens' key codes (8 dh bytes), their sm (2 dh), value codes (8 dh), their sm:
+// One page of one head in the 4-bit cache: 16 tokens' key codes (8 dh bytes), value codes (8 dh), the keys' sm (2 dh), the values' sm:
 // 20 dh bytes at ((l * n_pages + page) * H + h) * 20 dh. Codes lie as the 64 lanes of a wave hold a matrix operand, dh / 8
 // bytes a lane; lane (r = lane % 16, g = lane / 16) holds
 //   keys    token r, channels 8 g .. 8 g + 7 of each group: groups 2 p (low) and 2 p + 1 (high) in words 2 p (channels 0..3 of
 //           the eight) and 2 p + 1 (4..7)
 //   values  tokens 4 g .. 4 g + 3 of channels 32 p + r (low) and 32 p + 16 + r (high) in word p
-// and a page's sm are [token][group], so that lane (r, g) finds those of tokens 4 g .. 4 g + 3 in its own row of 16 lanes.
+// and a page's sm are [token / 4][group][token % 4]: those of a lane's four tokens and one group are 16 bytes, those of all groups a row of lanes.
 __host__ __device__ constexpr int page4_bytes(int dh) { return 20 * dh; }
-__host__ __device__ constexpr int page4_ksm(int dh) { return 8 * dh; }
-__host__ __device__ constexpr int page4_v(int dh) { return 10 * dh; }
+__host__ __device__ constexpr int page4_v(int dh) { return 8 * dh; }
+__host__ __device__ constexpr int page4_ksm(int dh) { return 16 * dh; }
 __host__ __device__ constexpr int page4_vsm(int dh) { return 18 * dh; }
+// place of token t, group c among a page's sm
+__host__ __device__ constexpr int sm_index(int dh, int t, int c) { return (t >> 2) * (dh / 8) + c * 4 + (t & 3); }
 
 // [host] ids of up to kSeqChunk sequences ride in the kernel arguments: nothing is staged, and a captured launch keeps its own.
 // cap: tokens the sequence's pages hold; slots beyond are neither read nor written, whatever the length on the device says.
@@ -164,7 +166,7 @@ struct AttendArgs {
     Heads q, out;
     void* out_lo;                                    // not NULL: the result is two fp16 planes (see split_f16), this is the low one
     float* part;
-    int B, R, H, G, mpps, nsplit, nt;                // G = query heads per key/value head; nt = 16-row tiles per key/value head
+    int B, R, H, G, mpps, nsplit, nt, J;             // G = query heads per key/value head; nt = tiles of J packed rows per key/value head
     float scale_log2;
 };
 int launch_kv4_append(const AppendArgs& a, int dh, int dtype, hipStream_t stream);

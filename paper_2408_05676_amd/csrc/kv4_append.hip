@@ -188,8 +188,8 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
         if (c == g) vsm = gr.sm;
     }
     if (g < NG) {
-        reinterpret_cast<uint32_t*>(page + page4_ksm(DH))[tp * NG + g] = ksm;
-        reinterpret_cast<uint32_t*>(page + page4_vsm(DH))[tp * NG + g] = vsm;
+        reinterpret_cast<uint32_t*>(page + page4_ksm(DH))[sm_index(DH, tp, g)] = ksm;
+        reinterpret_cast<uint32_t*>(page + page4_vsm(DH))[sm_index(DH, tp, g)] = vsm;
     }
 }
 
@@ -233,14 +233,14 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
     const int pg = a.block_table[(size_t)id * a.mpps + slot / kPageSize];
     const uint8_t* page = a.pages + ((size_t)pg * a.H + h) * page4_bytes(DH);
     const uint32_t* kw = reinterpret_cast<const uint32_t*>(page + (g * 16 + tp) * (DH / 8));
-    const uint32_t* ksm = reinterpret_cast<const uint32_t*>(page + page4_ksm(DH)) + tp * NG;
-    const uint32_t* vsm = reinterpret_cast<const uint32_t*>(page + page4_vsm(DH)) + tp * NG;
+    const uint32_t* ksm = reinterpret_cast<const uint32_t*>(page + page4_ksm(DH)) + sm_index(DH, tp, 0);
+    const uint32_t* vsm = reinterpret_cast<const uint32_t*>(page + page4_vsm(DH)) + sm_index(DH, tp, 0);
     const uint8_t* vp = page + page4_v(DH) + ((tp >> 2) * 16 + 4 * g) * (DH / 8) + code_byte(tp & 3);
     const size_t ko = (size_t)b * a.k.seq + (size_t)r * a.k.row + (size_t)h * a.k.head + 8 * g;
     const size_t vo = (size_t)b * a.v.seq + (size_t)r * a.v.row + (size_t)h * a.v.head + 4 * g;
 #pragma unroll
     for (int c = 0; c < NG; ++c) {
-        const float ks = sm_scale(ksm[c]), km = sm_offset(ksm[c]), vs = sm_scale(vsm[c]), vm = sm_offset(vsm[c]);
+        const float ks = sm_scale(ksm[4 * c]), km = sm_offset(ksm[4 * c]), vs = sm_scale(vsm[4 * c]), vm = sm_offset(vsm[4 * c]);
         float x[8], u[4], w[4];
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = fmaf(ks, (float)((kw[(c & ~1) + (j >> 2)] >> (8 * code_byte(j & 3) + 4 * (c & 1))) & 15u), km);
@@ -279,8 +279,8 @@ __global__ void kv4_compact_kernel(uint8_t* pages, const int32_t* block_table, c
             dp[page4_v(dh) + ((dt >> 2) * 16 + r) * kb + 4 * p + code_byte(dt & 3)] = sp[page4_v(dh) + ((st >> 2) * 16 + r) * kb + 4 * p + code_byte(st & 3)];
         }
         if (c < 2 * ng) {
-            const int o = (c < ng ? page4_ksm(dh) : page4_vsm(dh)) + 4 * (c % ng);
-            *reinterpret_cast<uint32_t*>(dp + o + 4 * ng * dt) = *reinterpret_cast<const uint32_t*>(sp + o + 4 * ng * st);
+            const int o = c < ng ? page4_ksm(dh) : page4_vsm(dh);
+            *reinterpret_cast<uint32_t*>(dp + o + 4 * sm_index(dh, dt, c % ng)) = *reinterpret_cast<const uint32_t*>(sp + o + 4 * sm_index(dh, st, c % ng));
         }
     }
 }

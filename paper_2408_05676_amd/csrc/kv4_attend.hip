@@ -17,7 +17,7 @@
 
 namespace laser {
 
-constexpr int kAttendWaves = 4;
+constexpr int kWaves = 4;                            // of a workgroup; one and two were slower (16 users' single tokens, 1024 behind them: 23.7, 22.1, 18.2 us)
 constexpr float kSumUnit = 1.f / 256.f;              // sums of 32 queries below 2^15, in fp16: scores are in this unit until they are scaled
 constexpr int kPartSlots = 2048;                     // (tile, split) results a launch may leave for the joining kernel
 constexpr int part_floats(int dh) { return 32 + 16 * dh; }
@@ -41,27 +41,6 @@ __device__ inline float sum_over_rows(float x) {
     return x + __shfl_xor(x, 32);
 }
 
-template <int DH>
-struct Page {                                        // one page's registers of a lane
-    uint32_t k[DH / 32], v[DH / 32], ksm, km, vsm;   // ksm, vsm: of token 4 g + r / NG, group r % NG; km: of token r, group g
-    __device__ inline void load(const uint8_t* p, int lane) {
-        constexpr int NG = DH / 32;
-        const int sm = 4 * ((lane >> 4) * 4 * NG + (lane & (4 * NG - 1)));
-        if constexpr (NG == 4) {
-            const u32x4 a = *reinterpret_cast<const u32x4*>(p + lane * 16), b = *reinterpret_cast<const u32x4*>(p + page4_v(DH) + lane * 16);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { k[i] = a[i]; v[i] = b[i]; }
-        } else {
-            const u32x2 a = *reinterpret_cast<const u32x2*>(p + lane * 8), b = *reinterpret_cast<const u32x2*>(p + page4_v(DH) + lane * 8);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) { k[i] = a[i]; v[i] = b[i]; }
-        }
-        ksm = *reinterpret_cast<const uint32_t*>(p + page4_ksm(DH) + sm);
-        km = *reinterpret_cast<const uint32_t*>(p + page4_ksm(DH) + 4 * ((lane & 15) * NG + (lane >> 4 & (NG - 1))));
-        vsm = *reinterpret_cast<const uint32_t*>(p + page4_vsm(DH) + sm);
-    }
-};
-
 template <int DT>
 __device__ inline void store_out(const AttendArgs& a, size_t o, const float (&x)[4]) {
     if constexpr (DT == DT_SPLIT) {
@@ -75,29 +54,84 @@ __device__ inline void store_out(const AttendArgs& a, size_t o, const float (&x)
     }
 }
 
-// IN: type of q; OUT: of the result; RT: 16-row tiles a workgroup takes.
-template <int DH, int IN, int OUT, int RT>
-__global__ __launch_bounds__(kAttendWaves * 64, RT >= 4 ? 1 : RT == 2 ? 2 : 3) void kv4_attend_kernel(AttendArgs a) {
+// ---- a wave's ring of two pairs of pages in LDS, written by the loads themselves
+// A pair: the codes of both pages one after the other, then both pages' scales and offsets; requests of 1 KB, 16 bytes a lane.
+template <int DH>
+struct Ring {
+    static constexpr int kCodes = 16 * DH, kSm = 4 * DH;             // bytes of a page
+    static constexpr int kFull = 2 * kCodes / 1024;                  // requests for the codes
+    static constexpr int kLoads = kFull + 1;                         // and one for both pages' scales (half of it twice where they are 512 bytes)
+    static constexpr int kSlot = kLoads * 1024;
+
+    // m0: where a request's first lane writes, one wait state before its use
+    __device__ static inline void request(uint32_t lds, const uint8_t* uniform, uint32_t off) {
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" ::"v"(off), "s"(lds), "s"(uniform) : "memory", "m0");
+    }
+    __device__ static inline void request(uint32_t lds, const uint8_t* per_lane) {
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(per_lane), "s"(lds) : "memory", "m0");
+    }
+    __device__ static inline void load(uint32_t lds, const uint8_t* a, const uint8_t* b, int lane) {
+#pragma unroll
+        for (int i = 0; i < kFull; ++i) request(lds + i * 1024, i < kFull / 2 ? a : b, (i % (kFull / 2)) * 1024 + lane * 16);
+        const uint8_t* p = lane & (kSm / 16) ? b : a;
+        request(lds + kFull * 1024, p + kCodes + (lane & (kSm / 16 - 1)) * 16);
+    }
+    template <int NEWER>
+    __device__ static inline void wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(NEWER * kLoads) : "memory"); }
+    __device__ static inline void have_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+};
+
+template <int CG>
+__device__ inline float sum_over_groups(float x) {                   // over the CG lanes of a query row
+    if constexpr (CG >= 2) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
+    if constexpr (CG >= 4) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
+    return x;
+}
+
+// IN: type of q; OUT: of the result. A workgroup takes a tile; its waves share the context.
+// CG = 1: a tile is 16 rows, a column of the scores each. CG = all groups (4, or 2 at 64 channels): a tile is 16 / CG rows, and a column one
+// group of a row: the operand holds that group's queries and zeros for the others, one chain of matrix instructions gives the scores'
+// parts by group, each lane scales its own (four multiply-adds instead of thirty-two) and the lanes of a row add up; likewise p s is
+// formed for one group a lane, and of the result the sixteen rows give each channel only that of its group.
+template <int DH, int IN, int OUT, int CG>
+__global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a) {
     constexpr int NG = DH / 32, NT = DH / 16;        // groups, 16-channel tiles
+    constexpr int J = 16 / CG;                       // rows of a tile
     constexpr bool kTwoQ = IN == DT_F32, kTwoP = OUT != DT_BF16;
     constexpr int kStride = DH + 4;                  // of a row in LDS: four rows apart are sixteen banks apart
-    __shared__ float sm_m[kAttendWaves][16], sm_l[kAttendWaves][16];
-    __shared__ float sm_o[kAttendWaves][16 * kStride];
-    const int ntb = (a.nt + RT - 1) / RT;
-    const int h = blockIdx.x / ntb, tile0 = blockIdx.x % ntb * RT, b = blockIdx.y, split = blockIdx.z;
+    constexpr int kWaveLds = 2 * Ring<DH>::kSlot > J * kStride * 4 ? 2 * Ring<DH>::kSlot : J * kStride * 4;
+    __shared__ float sm_m[kWaves][J], sm_l[kWaves][J];
+    __shared__ __attribute__((aligned(1024))) char lds[kWaves * kWaveLds];      // a wave's ring, later its results [J][kStride]
+    const int h = blockIdx.x / a.nt, tile = blockIdx.x % a.nt, b = blockIdx.y, split = blockIdx.z;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int r = lane & 15, g = lane >> 4;
+    const int r = lane & 15, g = lane >> 4, j = r / CG, cc = r % CG;
     // (what the whole wave shares is kept in scalar registers: addresses, loop bounds and branches)
     const int slot = __builtin_amdgcn_readfirstlane(a.seqs.slot(b)), len = __builtin_amdgcn_readfirstlane(a.lens[slot]), cap = a.seqs.tokens(b);
     int nr = a.n_rows ? min(max(a.n_rows[b], 0), a.R) : a.R;
     nr = __builtin_amdgcn_readfirstlane(max(0, min(nr, cap - len)));      // (a length beyond the pages: rows that have no slot are left out)
     const int P = nr * a.G;                          // packed rows
-    if (tile0 * 16 >= P || len < 0) return;
+    if (tile * J >= P || len < 0) return;
+
+    // ---- this workgroup's pages [p0, p1), this wave's pairs of them; the first two are on their way while the queries are made ready
+    const int npages = (len + nr + kPageSize - 1) / kPageSize;
+    const int per = ((npages + a.nsplit - 1) / a.nsplit + 1) & ~1;
+    const int p0 = split * per, p1 = min(npages, p0 + per);
+    const uint8_t* base = a.pages + (size_t)h * page4_bytes(DH);
+    const size_t page_step = (size_t)a.H * page4_bytes(DH);
+    typedef const __attribute__((address_space(4))) int32_t* scalar_ints;       // (not written while the kernel runs)
+    const scalar_ints bt = (scalar_ints)(a.block_table + (size_t)slot * a.mpps);
+    auto page_at = [&](int p) { return base + (size_t)(unsigned)__builtin_amdgcn_readfirstlane(bt[min(p, p1 - 1)]) * page_step; };
+    constexpr int kStep = 2 * kWaves;
+    char* const mine = lds + wave * kWaveLds;
+    const uint32_t ring = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine);
+    int p = p0 + 2 * wave;
+    if (p < p1) Ring<DH>::load(ring, page_at(p), page_at(p + 1), lane);
+    if (p + kStep < p1) Ring<DH>::load(ring + Ring<DH>::kSlot, page_at(p + kStep), page_at(p + kStep + 1), lane);
 
     // ---- which rows of the step each row sees: lane l works out row l's, by pointer doubling along the tree
     unsigned long long anc_l;
     if (a.row_anc) anc_l = a.row_anc[(size_t)b * a.R + min(lane, a.R - 1)];
-    else if (!a.parent) anc_l = lane >= 63 ? ~0ull : (2ull << lane) - 1;
+    else if (!a.parent) anc_l = (2ull << lane) - 1;
     else {
         anc_l = 1ull << lane;
         int up = lane > 0 && lane < a.R ? up_row(a.parent + (size_t)b * (a.R - 1), lane) : 0;
@@ -109,127 +143,157 @@ __global__ __launch_bounds__(kAttendWaves * 64, RT >= 4 ? 1 : RT == 2 ? 2 : 3) v
         }
     }
 
-    Frag8 q[RT][NG], ql[kTwoQ ? RT : 1][NG];
-    Frag8 qsum[RT];                                  // operand of the offsets: first input 8 g is group g, in two parts
-    float cs[RT];
-    unsigned long long anc[RT];
+    // ---- queries: multiplied by a power of two of their row, to below 2^15 (and by 1/16 in odd groups, whose codes come out 16 times
+    // larger); cs > 0 takes scores back to the exponents of 2 (the sign of the scale has gone into the queries)
+    Frag8 q[NG], ql[NG];
+    Frag8 qsum;                                  // CG = 1, operand of the offsets: first input 8 g is the sum of group g, in two parts
+    constexpr float kUnit = CG == 1 ? kCodeUnit * kSumUnit : 1.f;         // of the keys' scales: scores come in units of kSumUnit, else 2^-24
+    const int pi = min(tile * J + j, P - 1), row = pi / a.G, hq = h * a.G + pi % a.G;
+    const unsigned anc_lo = __shfl((unsigned)anc_l, row), anc_hi = __shfl((unsigned)(anc_l >> 32), row);
+    const unsigned long long anc = ((unsigned long long)anc_hi << 32) | anc_lo;
+    const size_t qo = (size_t)b * a.q.seq + (size_t)row * a.q.row + (size_t)hq * a.q.head + 8 * g;
+    float x[NG][8], mx = 0.f;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const int pi = min((tile0 + t) * 16 + r, P - 1), row = pi / a.G, hq = h * a.G + pi % a.G;
-        {
-            const unsigned lo = __shfl((unsigned)anc_l, row), hi = __shfl((unsigned)(anc_l >> 32), row);
-            anc[t] = ((unsigned long long)hi << 32) | lo;
-        }
-        const size_t qo = (size_t)b * a.q.seq + (size_t)row * a.q.row + (size_t)hq * a.q.head + 8 * g;
-        float x[NG][8], mx = 0.f;
+    for (int c = 0; c < NG; ++c) {
+        load_elems<IN, 8>(a.q.p, qo + 32 * c, x[c]);
 #pragma unroll
-        for (int c = 0; c < NG; ++c) {
-            load_elems<IN, 8>(a.q.p, qo + 32 * c, x[c]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) mx = fmaxf(mx, fabsf(x[c][j]));
-        }
-        mx = max_over_rows(mx);
-        int e = 0;
-        if (mx > 0.f && mx < INFINITY) { (void)frexpf(mx, &e); e = min(max(15 - e, -80), 100); }
-        float own = 0.f;                             // the sum of group g, by lane (r, g)
-#pragma unroll
-        for (int c = 0; c < NG; ++c) {
-            float s = 0.f, y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[c][j] = ldexpf(x[c][j], e);
-            q[t][c] = pack8(x[c]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = (float)q[t][c].v[j];
-            if constexpr (kTwoQ) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[c][j] -= y[j];
-                ql[t][c] = pack8(x[c]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s += (float)ql[t][c].v[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s += y[j];
-            s = sum_over_rows(s) * kSumUnit;
-            if (c == g) own = s;
-        }
-        {
-            const _Float16 hi = (_Float16)own;
-            const half2_t two = {hi, (_Float16)(own - (float)hi)};
-            qsum[t].v4 = u32x4{__builtin_bit_cast(uint32_t, two), 0u, 0u, 0u};
-        }
-        cs[t] = ldexpf(a.scale_log2 / kSumUnit, -e);
+        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[c][i]));
     }
-
-    float4_t acc[RT][NT], accm[RT];
-    float m_ref[RT], l_run[RT], pf = 16.f;           // pf: factor of p s; smaller once a scale beyond 511 was met, so that fp16 holds 8 s pf
+    mx = max_over_rows(mx);
+    int e = 0;
+    if (mx > 0.f && mx < INFINITY) { (void)frexpf(mx, &e); e = min(max(15 - e, -80), 100); }
+    const float up = ldexpf(a.scale_log2 < 0.f ? -1.f : a.scale_log2 > 0.f ? 1.f : 0.f, e);
+    float own = 0.f;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        m_ref[t] = -INFINITY;
-        l_run[t] = 0.f;
-        accm[t] = float4_t{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < NG; ++c) {
+        float s = 0.f, y[8];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[t][n] = float4_t{0.f, 0.f, 0.f, 0.f};
-    }
-
-    // ---- this workgroup's pages [p0, p1), this wave's pairs of them
-    const int npages = (len + nr + kPageSize - 1) / kPageSize;
-    const int per = ((npages + a.nsplit - 1) / a.nsplit + 1) & ~1;
-    const int p0 = split * per, p1 = min(npages, p0 + per);
-    const uint8_t* base = a.pages + (size_t)h * page4_bytes(DH);
-    const size_t page_step = (size_t)a.H * page4_bytes(DH);
-    typedef const __attribute__((address_space(4))) int32_t* scalar_ints;       // (not written while the kernel runs)
-    const scalar_ints bt = (scalar_ints)(a.block_table + (size_t)slot * a.mpps);
-    auto page_at = [&](int p) { return base + (size_t)(unsigned)__builtin_amdgcn_readfirstlane(bt[min(p, p1 - 1)]) * page_step; };
-    constexpr int kStep = 2 * kAttendWaves;
-
-    // Two pages p and p + 1 of this wave. Every lane has the scores of its tokens 4 g .. 4 g + 3 of each page and its query row r.
-    const float ks_unit = kCodeUnit * kSumUnit * (lane & 1 ? 1.f / 16.f : 1.f);      // odd groups: codes from bits 4..7
-    auto pair_of_pages = [&](const Page<DH> (&pg)[2], int p) {
-        // Scales of values: fp16 holds p s pf as long as s <= 511
-        if (pf == 16.f && __any(sm_scale(pg[0].vsm) > 511.f || sm_scale(pg[1].vsm) > 511.f)) {
-            pf = 1.f / 16.f;
+        for (int i = 0; i < 8; ++i) x[c][i] *= c & 1 ? up * (1.f / 16.f) : up;
+        q[c] = pack8(x[c]);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
+        for (int i = 0; i < 8; ++i) y[i] = (float)q[c].v[i];
+        if constexpr (kTwoQ) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < 8; ++i) x[c][i] -= y[i];
+            ql[c] = pack8(x[c]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t][n][i] *= 1.f / 256.f;
+            for (int i = 0; i < 8; ++i) s += (float)ql[c].v[i];
         }
-        float x[RT][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += y[i];
+        s = sum_over_rows(s) * ((c & 1 ? 16.f : 1.f) * (CG == 1 ? kSumUnit : 1.f / kCodeUnit));
+        if (c == (CG == 1 ? g : cc)) own = s;
+        if (CG > 1 && c != cc) {
+            q[c].v4 = u32x4{0, 0, 0, 0};
+            if constexpr (kTwoQ) ql[c].v4 = u32x4{0, 0, 0, 0};
+        }
+    }
+    const float qs = own;                            // (CG > 1: the sum of the lane's own group)
+    if constexpr (CG == 1) {
+        const _Float16 hi = (_Float16)own;
+        const half2_t two = {hi, (_Float16)(own - (float)hi)};
+        qsum.v4 = u32x4{__builtin_bit_cast(uint32_t, two), 0u, 0u, 0u};
+    }
+    const float cs = a.scale_log2 == 0.f ? 1.f : fmaxf(ldexpf(fabsf(a.scale_log2) * (CG == 1 ? 1.f / kSumUnit : kCodeUnit), -e), 1e-37f);
+
+    // ---- the walk. Weights are p = 2^(score - ref); ref moves, and what was summed with it, when a score passes it by more than `over`,
+    // and is then set to `back` below the row's largest score. p s is thus at most 2^over s: within fp16 while s <= 511, and beyond, once a larger scale
+    // has been met, with over = -1.
+    float4_t acc[NT], accm = {0.f, 0.f, 0.f, 0.f};
+    float ref = -INFINITY, limit = -INFINITY, l_run = 0.f, over = 7.f, back = 4.f;       // limit: (ref + over) in units of the scores before cs
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
+    auto rescale = [&](float ref_new) {
+        const float alpha = ref == ref_new ? 1.f : __builtin_amdgcn_exp2f(ref - ref_new);
+        l_run *= alpha;
+        ref = ref_new;
+        limit = (ref_new + over) / cs;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float al = __shfl(alpha, 4 * g + i);                   // accumulator rows are the score columns 4 g + i
+            accm[i] *= al;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[n][i] *= al;
+        }
+    };
+
+    uint32_t at = 0;                                 // of the pair in the ring
+    for (; p < p1; p += kStep, at ^= Ring<DH>::kSlot) {
+        // the pair behind the next one: its page numbers now, the request once this pair has been read
+        const bool more = p + 2 * kStep < p1;
+        const uint8_t *n0 = page_at(p + 2 * kStep), *n1 = page_at(p + 2 * kStep + 1);
+        if (p + kStep < p1) Ring<DH>::template wait<1>();
+        else Ring<DH>::template wait<0>();
+        const char* from = mine + at;
+        uint32_t kw[2][NG], vw[2][NG];
+        uint32_t ksm[2][CG == 1 ? 1 : 4], vsm[2][CG == 1 ? 1 : 4], km[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const float ks = sm_scale(pg[u].ksm) * ks_unit;
-            Frag8 km;
-            km.v4 = u32x4{__builtin_amdgcn_perm(pg[u].km, pg[u].km, 0x07060706u), 0u, 0u, 0u};
+            const char *pk = from + u * Ring<DH>::kCodes + lane * 4 * NG, *pv = pk + page4_v(DH), *ps = from + 2 * Ring<DH>::kCodes + u * Ring<DH>::kSm;
+            if constexpr (NG == 4) {
+                const u32x4 k = *reinterpret_cast<const u32x4*>(pk), v = *reinterpret_cast<const u32x4*>(pv);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { kw[u][i] = k[i]; vw[u][i] = v[i]; }
+            } else {
+                const u32x2 k = *reinterpret_cast<const u32x2*>(pk), v = *reinterpret_cast<const u32x2*>(pv);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) { kw[u][i] = k[i]; vw[u][i] = v[i]; }
+            }
+            if constexpr (CG == 1) {                 // lane r: of token 4 g + r % 4, group r / 4; km: of token r, group g
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(ps);
+                ksm[u][0] = w[g * 4 * NG + (lane & (4 * NG - 1))];
+                vsm[u][0] = w[16 * NG + g * 4 * NG + (lane & (4 * NG - 1))];
+                km[u] = w[sm_index(DH, r, g & (NG - 1))];
+            } else {                                 // of tokens 4 g .. 4 g + 3, the lane's own group
+                const u32x4 k = *reinterpret_cast<const u32x4*>(ps + (g * NG + cc) * 16), v = *reinterpret_cast<const u32x4*>(ps + 64 * NG + (g * NG + cc) * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { ksm[u][i] = k[i]; vsm[u][i] = v[i]; }
+            }
+        }
+        Ring<DH>::have_read();
+        if (more) Ring<DH>::load(ring + at, n0, n1, lane);
+
+        // ---- scores: every lane has those of its tokens 4 g .. 4 g + 3 of each page and its row
+        float s[8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
             Frag8 kf[NG];
 #pragma unroll
             for (int c = 0; c < NG; c += 2)
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    const uint32_t a0 = pg[u].k[c + w], a1 = a0 >> 8;
+                    const uint32_t a0 = kw[u][c + w], a1 = a0 >> 8;
                     kf[c].w[2 * w] = a0 & kCodeLo;
                     kf[c].w[2 * w + 1] = a1 & kCodeLo;
                     kf[c + 1].w[2 * w] = a0 & kCodeHi;
                     kf[c + 1].w[2 * w + 1] = a1 & kCodeHi;
                 }
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                float4_t d[NG], s = mfma_16x16x32(km, qsum[t], float4_t{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                for (int c = 0; c < NG; ++c) {
-                    d[c] = float4_t{0.f, 0.f, 0.f, 0.f};
-                    if constexpr (kTwoQ) d[c] = mfma_16x16x32(kf[c], ql[t][c], d[c]);
-                    d[c] = mfma_16x16x32(kf[c], q[t][c], d[c]);
-                }
-                static_for<0, NG>([&](auto cc) {
-                    constexpr int c = decltype(cc)::value;
+            if constexpr (CG == 1) {
+                const float ks = sm_scale(ksm[u][0]) * kUnit;
+                Frag8 kmf;
+                kmf.v4 = u32x4{__builtin_amdgcn_perm(km[u], km[u], 0x07060706u), 0u, 0u, 0u};
+                float4_t sum = mfma_16x16x32(kmf, qsum, float4_t{0.f, 0.f, 0.f, 0.f});
+                static_for<0, NG>([&](auto ci) {
+                    constexpr int c = decltype(ci)::value;
+                    float4_t d = {0.f, 0.f, 0.f, 0.f};
+                    if constexpr (kTwoQ) d = mfma_16x16x32(kf[c], ql[c], d);
+                    d = mfma_16x16x32(kf[c], q[c], d);
                     static_for<0, 4>([&](auto ii) {
                         constexpr int i = decltype(ii)::value;
-                        s[i] = fmaf(row_lane<i * NG + c>(ks), d[c][i], s[i]);
+                        sum[i] = fmaf(row_lane<c * 4 + i>(ks), d[i], sum[i]);
                     });
                 });
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[t][4 * u + i] = s[i] * cs[t];
+                for (int i = 0; i < 4; ++i) s[4 * u + i] = sum[i];
+            } else {
+                float4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < NG; ++c) {
+                    if constexpr (kTwoQ) d = mfma_16x16x32(kf[c], ql[c], d);
+                    d = mfma_16x16x32(kf[c], q[c], d);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * u + i] = sum_over_groups<CG>(fmaf(sm_scale(ksm[u][i]), d[i], sm_offset(ksm[u][i]) * qs));
             }
         }
         if ((p + 2) * kPageSize > len) {             // slots behind the committed ones: along the row's own branch only
@@ -238,221 +302,233 @@ __global__ __launch_bounds__(kAttendWaves * 64, RT >= 4 ? 1 : RT == 2 ? 2 : 3) v
                 // the lane's four slots start rel behind the committed length: bits rel .. rel + 3 of the row's mask, ones below 0
                 const int rel = p + u < p1 ? (p + u) * kPageSize + 4 * g - len : 64;
                 const int up = min(max(rel, 0), 63), under = min(max(-rel, 0), 4);
+                const unsigned ahead = rel < 64 ? (unsigned)(anc >> up) : 0u, behind = ((unsigned)anc << under) | ((1u << under) - 1u);
+                const unsigned seen = rel >= 0 ? ahead : behind;
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const unsigned ahead = rel < 64 ? (unsigned)(anc[t] >> up) : 0u, behind = ((unsigned)anc[t] << under) | ((1u << under) - 1u);
-                    const unsigned seen = rel >= 0 ? ahead : behind;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[t][4 * u + i] = (seen >> i) & 1u ? x[t][4 * u + i] : -INFINITY;
-                }
+                for (int i = 0; i < 4; ++i) s[4 * u + i] = (seen >> i) & 1u ? s[4 * u + i] : -INFINITY;
             }
         } else if (p + 1 >= p1) {                    // an odd number of pages
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[t][4 + i] = -INFINITY;
+            for (int i = 0; i < 4; ++i) s[4 + i] = -INFINITY;
         }
 
-        // ---- weights p = 2^(x - m_ref), in place of x; their sums with the offsets
-        Frag8 vm;                                    // offsets as an operand: column r < NG is group r (the others are not used)
+        // ---- weights in place of scores, and their sums with the offsets
+        Frag8 vm;                                    // offsets as an operand: column 4 c is group c (CG > 1: column r is group r % CG)
+        bool large = false;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint32_t e0 = pg[u].vsm, e1 = row_ahead<NG>(e0), e2 = row_ahead<2 * NG>(e0), e3 = row_ahead<3 * NG>(e0);
-            vm.w[2 * u] = __builtin_amdgcn_perm(e1, e0, 0x07060302u);
-            vm.w[2 * u + 1] = __builtin_amdgcn_perm(e3, e2, 0x07060302u);
+            if constexpr (CG == 1) {
+                const uint32_t e0 = vsm[u][0], e1 = row_ahead<1>(e0), e2 = row_ahead<2>(e0), e3 = row_ahead<3>(e0);
+                vm.w[2 * u] = __builtin_amdgcn_perm(e1, e0, 0x07060302u);
+                vm.w[2 * u + 1] = __builtin_amdgcn_perm(e3, e2, 0x07060302u);
+                large |= sm_scale(e0) > 511.f;
+            } else {
+                vm.w[2 * u] = __builtin_amdgcn_perm(vsm[u][1], vsm[u][0], 0x07060302u);
+                vm.w[2 * u + 1] = __builtin_amdgcn_perm(vsm[u][3], vsm[u][2], 0x07060302u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) large |= sm_scale(vsm[u][i]) > 511.f;
+            }
         }
+        if (over > 0.f && __any(large)) {
+            over = -1.f;
+            back = -4.f;
+            rescale(ref + 8.f);
+        }
+        const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+        if (__any(mx > limit)) rescale(fmaxf(ref, max_over_rows(mx) * cs - back));
+        const float mu = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const float mx = fmaxf(fmaxf(fmaxf(x[t][0], x[t][1]), fmaxf(x[t][2], x[t][3])), fmaxf(fmaxf(x[t][4], x[t][5]), fmaxf(x[t][6], x[t][7])));
-            if (__any(mx > m_ref[t] + 3.f)) {
-                const float m_new = fmaxf(m_ref[t], max_over_rows(mx));
-                const float alpha = m_ref[t] == m_new ? 1.f : __builtin_amdgcn_exp2f(m_ref[t] - m_new);
-                l_run[t] *= alpha;
-                m_ref[t] = m_new;
+        for (int i = 0; i < 8; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, -mu));
+            l_run += s[i];
+        }
+        const Frag8 ph = pack8(s);
+        accm = mfma_16x16x32(ph, vm, accm);
+        if constexpr (kTwoP) {
+            float lo[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float al = __shfl(alpha, 4 * g + i);       // accumulator rows are 4 g + i
-                    accm[t][i] *= al;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[t][n][i] *= al;
-                }
-            }
-            const float mu = m_ref[t] == -INFINITY ? 0.f : m_ref[t];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[t][i] = __builtin_amdgcn_exp2f(x[t][i] - mu);
-                l_run[t] += x[t][i];
-            }
-            const Frag8 ph = pack8(x[t]);
-            accm[t] = mfma_16x16x32(ph, vm, accm[t]);
+            for (int i = 0; i < 8; ++i) lo[i] = s[i] - (float)ph.v[i];
+            accm = mfma_16x16x32(pack8(lo), vm, accm);
+        }
+
+        // ---- values: operand fragments of tokens 4 g .. 4 g + 3 of both pages, p s of the group (CG > 1: of the lane's own) against them
+        Frag8 pv, pl;
+        auto weigh = [&](auto ci) {
+            constexpr int c = decltype(ci)::value;
+            float ps[8];
+            static_for<0, 8>([&](auto ii) {
+                constexpr int i = decltype(ii)::value;
+                if constexpr (CG == 1) ps[i] = row_lane<c * 4 + i % 4>(sm_scale(vsm[i / 4][0])) * s[i];
+                else ps[i] = sm_scale(vsm[i / 4][i % 4]) * s[i];
+            });
+            pv = pack8(ps);
             if constexpr (kTwoP) {
                 float lo[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) lo[i] = x[t][i] - (float)ph.v[i];
-                accm[t] = mfma_16x16x32(pack8(lo), vm, accm[t]);
+                for (int i = 0; i < 8; ++i) lo[i] = ps[i] - (float)pv.v[i];
+                pl = pack8(lo);
             }
-        }
-        // ---- values: operand fragments of tokens 4 g .. 4 g + 3 of both pages
-        const float vs0 = sm_scale(pg[0].vsm) * pf, vs1 = sm_scale(pg[1].vsm) * pf;
-        static_for<0, NG>([&](auto cc) {
-            constexpr int c = decltype(cc)::value;
+        };
+        static_for<0, NG>([&](auto ci) {
+            constexpr int c = decltype(ci)::value;
+            if constexpr (CG == 1 || c == 0) weigh(ci);
             Frag8 va, vb;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint32_t a0 = pg[u].v[c], a1 = a0 >> 8;
+                const uint32_t a0 = vw[u][c], a1 = a0 >> 8;
                 va.w[2 * u] = a0 & kCodeLo;
                 va.w[2 * u + 1] = a1 & kCodeLo;
                 vb.w[2 * u] = a0 & kCodeHi;
                 vb.w[2 * u + 1] = a1 & kCodeHi;
             }
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                float ps[8];
-                static_for<0, 4>([&](auto ii) {
-                    constexpr int i = decltype(ii)::value;
-                    ps[i] = row_lane<i * NG + c>(vs0) * x[t][i];
-                    ps[4 + i] = row_lane<i * NG + c>(vs1) * x[t][4 + i];
-                });
-                const Frag8 pv = pack8(ps);
-                acc[t][2 * c] = mfma_16x16x32(pv, va, acc[t][2 * c]);
-                acc[t][2 * c + 1] = mfma_16x16x32(pv, vb, acc[t][2 * c + 1]);
-                if constexpr (kTwoP) {
-                    float lo[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) lo[i] = ps[i] - (float)pv.v[i];
-                    const Frag8 pl = pack8(lo);
-                    acc[t][2 * c] = mfma_16x16x32(pl, va, acc[t][2 * c]);
-                    acc[t][2 * c + 1] = mfma_16x16x32(pl, vb, acc[t][2 * c + 1]);
-                }
+            acc[2 * c] = mfma_16x16x32(pv, va, acc[2 * c]);
+            acc[2 * c + 1] = mfma_16x16x32(pv, vb, acc[2 * c + 1]);
+            if constexpr (kTwoP) {
+                acc[2 * c] = mfma_16x16x32(pl, va, acc[2 * c]);
+                acc[2 * c + 1] = mfma_16x16x32(pl, vb, acc[2 * c + 1]);
             }
         });
-    };
-
-    // Each turn first requests the next pair (past the end: the last page again) and the page numbers of the pair behind it.
-    Page<DH> pa[2], pb[2];
-    int p = p0 + 2 * wave;
-    if (p < p1) {
-        pa[0].load(page_at(p), lane);
-        pa[1].load(page_at(p + 1), lane);
-        const uint8_t *n0 = page_at(p + kStep), *n1 = page_at(p + kStep + 1);
-        auto turn = [&](Page<DH> (&now)[2], Page<DH> (&next)[2]) {
-            next[0].load(n0, lane);
-            next[1].load(n1, lane);
-            n0 = page_at(p + 2 * kStep);
-            n1 = page_at(p + 2 * kStep + 1);
-            pair_of_pages(now, p);
-            p += kStep;
-        };
-        while (true) {
-            turn(pa, pb);
-            if (p >= p1) break;
-            turn(pb, pa);
-            if (p >= p1) break;
-        }
     }
 
-    // ---- join the waves, one tile at a time
-    const float unit = kCodeUnit / pf;
+    // ---- join the waves (a wave's results lie where its ring was: every request of it has been waited for)
+    float* const res = reinterpret_cast<float*>(mine);
+    const float l = sum_over_rows(l_run);
+    if (g == 0 && cc == 0) { sm_m[wave][j] = ref; sm_l[wave][j] = l; }
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        if ((tile0 + t) * 16 >= P) break;            // (the same for the whole workgroup)
-        const float l = sum_over_rows(l_run[t]);
-        if (t > 0) __syncthreads();                  // the tile before has been read
-        if (g == 0) { sm_m[wave][r] = m_ref[t]; sm_l[wave][r] = l; }
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                sm_o[wave][(4 * g + i) * kStride + 16 * n + r] = fmaf(acc[t][n][i], n & 1 ? unit / 16.f : unit, __shfl(accm[t][i], 16 * g + n / 2));
-        __syncthreads();
-        for (int idx = threadIdx.x; idx < 4 * DH; idx += kAttendWaves * 64) {
-            const int row = idx / (DH / 4), c = idx % (DH / 4) * 4;
-            float M = sm_m[0][row], L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 1; w < kAttendWaves; ++w) M = fmaxf(M, sm_m[w][row]);
-#pragma unroll
-            for (int w = 0; w < kAttendWaves; ++w) {
-                const float mw = sm_m[w][row], f = mw == M ? 1.f : __builtin_amdgcn_exp2f(mw - M);
-                L += sm_l[w][row] * f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] += sm_o[w][row * kStride + c + j] * f;
+        for (int i = 0; i < 4; ++i)
+            if (CG == 1 || i % CG == n / 2) {    // (row 4 g + i is group i % CG of query row (4 g + i) / CG)
+                const float om = __shfl(accm[i], 16 * g + (CG == 1 ? 4 : 1) * (n / 2));
+                res[(4 * g + i) / CG * kStride + 16 * n + r] = fmaf(acc[n][i], n & 1 ? kCodeUnit / 16.f : kCodeUnit, om);
             }
-            if (a.nsplit == 1) {
-                const int pi = (tile0 + t) * 16 + row;
-                if (pi < P) {
-                    const float inv = L == 0.f ? 0.f : 1.f / L;          // (nothing seen: 0; NaN stays)
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < J * DH / 4; idx += kWaves * 64) {
+        const int row = idx / (DH / 4), c = idx % (DH / 4) * 4;
+        float M = sm_m[0][row], L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] *= inv;
-                    store_out<OUT>(a, (size_t)b * a.out.seq + (size_t)(pi / a.G) * a.out.row + (size_t)(h * a.G + pi % a.G) * a.out.head + c, o);
-                }
-            } else {
-                float* part = a.part + ((((size_t)b * a.H + h) * a.nt + tile0 + t) * a.nsplit + split) * part_floats(DH);
-                if (c == 0) { part[row] = M; part[16 + row] = L; }
-                *reinterpret_cast<float4_t*>(part + 32 + row * DH + c) = float4_t{o[0], o[1], o[2], o[3]};
+        for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm_m[w][row]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float mw = sm_m[w][row], f = mw == M ? 1.f : __builtin_amdgcn_exp2f(mw - M);
+            const float4_t v = *reinterpret_cast<const float4_t*>(lds + w * kWaveLds + (row * kStride + c) * 4);
+            L += sm_l[w][row] * f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += v[i] * f;
+        }
+        if (a.nsplit == 1) {
+            const int pi = tile * J + row;
+            if (pi < P) {
+                const float inv = L == 0.f ? 0.f : 1.f / L;          // (nothing seen: 0; NaN stays)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] *= inv;
+                store_out<OUT>(a, (size_t)b * a.out.seq + (size_t)(pi / a.G) * a.out.row + (size_t)(h * a.G + pi % a.G) * a.out.head + c, o);
             }
+        } else {
+            float* part = a.part + ((((size_t)b * a.H + h) * a.nt + tile) * a.nsplit + split) * part_floats(DH);
+            if (c == 0) { part[row] = M; part[16 + row] = L; }
+            *reinterpret_cast<float4_t*>(part + 32 + row * DH + c) = float4_t{o[0], o[1], o[2], o[3]};
         }
     }
 }
 
-// Joins the parts of a split context: a workgroup per tile.
+// Joins the parts of a split context: a workgroup per row, four channels a thread, the parts dealt round to 1024 / DH groups of threads.
 template <int DH, int OUT>
 __global__ __launch_bounds__(256) void kv4_join_kernel(AttendArgs a) {
-    const int h = blockIdx.x / a.nt, tile = blockIdx.x % a.nt, b = blockIdx.y;
+    constexpr int C = DH / 4, S = 256 / C;
+    __shared__ float sm_m[S], sm_l[S];
+    __shared__ float4_t sm_o[S][C];
+    const int row = blockIdx.x % a.J, tile = blockIdx.x / a.J % a.nt, h = blockIdx.x / a.J / a.nt, b = blockIdx.y, pi = tile * a.J + row;
     const int slot = a.seqs.slot(b), len = a.lens[slot];
     int nr = a.n_rows ? min(max(a.n_rows[b], 0), a.R) : a.R;
     nr = max(0, min(nr, a.seqs.tokens(b) - len));
-    const int P = nr * a.G;
-    if (len < 0) return;
+    if (pi >= nr * a.G || len < 0) return;
     const float* part = a.part + (((size_t)b * a.H + h) * a.nt + tile) * a.nsplit * part_floats(DH);
-    for (int idx = threadIdx.x; idx < 4 * DH; idx += 256) {
-        const int row = idx / (DH / 4), c = idx % (DH / 4) * 4, pi = tile * 16 + row;
-        if (pi >= P) continue;
-        float M = -INFINITY, L = 0.f;
-        float4_t o = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < a.nsplit; ++s) M = fmaxf(M, part[(size_t)s * part_floats(DH) + row]);
-        for (int s = 0; s < a.nsplit; ++s) {
-            const float* ps = part + (size_t)s * part_floats(DH);
-            const float ms = ps[row], f = ms == M ? 1.f : __builtin_amdgcn_exp2f(ms - M);
-            const float4_t v = *reinterpret_cast<const float4_t*>(ps + 32 + row * DH + c);
-            L += ps[16 + row] * f;
+    const int c = threadIdx.x % C, s0 = threadIdx.x / C;
+    float M = -INFINITY, L = 0.f;
+    float4_t o = {0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 4;                             // parts requested together
+    for (int s = s0; s < a.nsplit; s += U * S) {
+        float m[U], l[U];
+        float4_t v[U];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] += v[j] * f;
+        for (int u = 0; u < U; ++u) {
+            const float* ps = part + (size_t)min(s + u * S, a.nsplit - 1) * part_floats(DH);
+            m[u] = ps[row];
+            l[u] = ps[16 + row];
+            v[u] = *reinterpret_cast<const float4_t*>(ps + 32 + row * DH + 4 * c);
         }
-        const float inv = L == 0.f ? 0.f : 1.f / L;
-        const float x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-        store_out<OUT>(a, (size_t)b * a.out.seq + (size_t)(pi / a.G) * a.out.row + (size_t)(h * a.G + pi % a.G) * a.out.head + c, x);
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            m[u] = s + u * S < a.nsplit ? m[u] : -INFINITY;
+            top = fmaxf(top, m[u]);
+        }
+        const float keep = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
+        L *= keep;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] *= keep;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float f = s + u * S >= a.nsplit ? 0.f : m[u] == top ? 1.f : __builtin_amdgcn_exp2f(m[u] - top);
+            L += l[u] * f;                           // (0 times NaN stays NaN: a part that has met one)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] += v[u][j] * f;
+        }
+        M = top;
     }
+    if (c == 0) { sm_m[s0] = M; sm_l[s0] = L; }
+    sm_o[s0][c] = o;
+    __syncthreads();
+    if (s0 != 0) return;
+    float top = sm_m[0], sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 1; s < S; ++s) top = fmaxf(top, sm_m[s]);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const float f = sm_m[s] == top ? 1.f : __builtin_amdgcn_exp2f(sm_m[s] - top);
+        const float4_t v = sm_o[s][c];
+        sum += sm_l[s] * f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] += v[j] * f;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= inv;
+    store_out<OUT>(a, (size_t)b * a.out.seq + (size_t)(pi / a.G) * a.out.row + (size_t)(h * a.G + pi % a.G) * a.out.head + 4 * c, x);
 }
 
 template <int DH, int IN, int OUT>
-static void launch(const AttendArgs& a, int rt, hipStream_t stream) {
-    const dim3 grid((unsigned)(a.H * ((a.nt + rt - 1) / rt)), (unsigned)a.B, (unsigned)a.nsplit);
-    if (rt == 1) hipLaunchKernelGGL((kv4_attend_kernel<DH, IN, OUT, 1>), grid, dim3(kAttendWaves * 64), 0, stream, a);
-    else if (rt == 2) hipLaunchKernelGGL((kv4_attend_kernel<DH, IN, OUT, 2>), grid, dim3(kAttendWaves * 64), 0, stream, a);
-    else hipLaunchKernelGGL((kv4_attend_kernel<DH, IN, OUT, 4>), grid, dim3(kAttendWaves * 64), 0, stream, a);
-    if (a.nsplit > 1) hipLaunchKernelGGL((kv4_join_kernel<DH, OUT>), dim3((unsigned)(a.H * a.nt), (unsigned)a.B), dim3(256), 0, stream, a);
+static void launch(const AttendArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.H * a.nt), (unsigned)a.B, (unsigned)a.nsplit);
+    if (a.J == 16) hipLaunchKernelGGL((kv4_attend_kernel<DH, IN, OUT, 1>), grid, dim3(kWaves * 64), 0, stream, a);
+    else hipLaunchKernelGGL((kv4_attend_kernel<DH, IN, OUT, DH / 32>), grid, dim3(kWaves * 64), 0, stream, a);
+    if (a.nsplit > 1) hipLaunchKernelGGL((kv4_join_kernel<DH, OUT>), dim3((unsigned)(a.H * a.nt * a.J), (unsigned)a.B), dim3(256), 0, stream, a);
 }
 
 // max_tokens: the most slots any of the sequences may have by the host's bounds
 int launch_kv4_attend(AttendArgs a, int dh, int dtype, int max_tokens, hipStream_t stream) {
     int ncu = 0;
     LASER_HIP_CHECK(hipDeviceGetAttribute(&ncu, hipDeviceAttributeMultiprocessorCount, 0));
-    a.nt = (a.R * a.G + 15) / 16;
-    const int rt = a.nt >= 4 ? 4 : a.nt >= 2 ? 2 : 1;
-    const long groups = (long)a.B * a.H * ((a.nt + rt - 1) / rt), tiles = (long)a.B * a.H * a.nt;
-    // Split the context until every compute unit has a few workgroups, as long as each has a pair of pages for every wave.
+    // Up to 4 rows of a key/value head (8 at 64 channels) the columns of a tile are groups: 4 rows behind 65000 tokens 22.7 us (25.0 with rows
+    // as columns), 1 row of 16 sequences behind 1024 18.1 (19.5); two such tiles for up to 8 rows 21.6 and one of 16 18.8 (8 rows, 4000 tokens).
+    const int P = a.R * a.G, few = 16 * 32 / dh;
+    a.J = P <= few ? few : 16;
+    a.nt = (P + a.J - 1) / a.J;
+    // Split the context for two workgroups on every compute unit, as long as each wave has a pair of pages.
+    const long tiles = (long)a.B * a.H * a.nt;
     const int pages = (max_tokens + kPageSize - 1) / kPageSize;
-    long want = std::max(1l, 3l * ncu / groups);
-    want = std::min(want, (long)(pages + 2 * kAttendWaves - 1) / (2 * kAttendWaves));
+    long want = std::max(1l, 2l * ncu / tiles);
+    want = std::min(want, (long)(pages + 2 * kWaves - 1) / (2 * kWaves));
     want = std::min(want, (long)kPartSlots / tiles);
     a.nsplit = (int)std::max(1l, want);
     const bool split_out = a.out_lo != nullptr;
     auto go = [&](auto dhc) {
         constexpr int D = decltype(dhc)::value;
-        if (dtype == DT_F16) launch<D, DT_F16, DT_F16>(a, rt, stream);
-        else if (dtype == DT_BF16) launch<D, DT_BF16, DT_BF16>(a, rt, stream);
-        else if (!split_out) launch<D, DT_F32, DT_F32>(a, rt, stream);
-        else launch<D, DT_F32, DT_SPLIT>(a, rt, stream);
+        if (dtype == DT_F16) launch<D, DT_F16, DT_F16>(a, stream);
+        else if (dtype == DT_BF16) launch<D, DT_BF16, DT_BF16>(a, stream);
+        else if (!split_out) launch<D, DT_F32, DT_F32>(a, stream);
+        else launch<D, DT_F32, DT_SPLIT>(a, stream);
     };
     if (dh == 128) go(std::integral_constant<int, 128>{});
     else go(std::integral_constant<int, 64>{});
