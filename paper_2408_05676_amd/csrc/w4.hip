@@ -79,12 +79,14 @@ __device__ inline float4_t mfma_x(const Frag8& a, const Frag8& b, float4_t c) {
     else return mfma_16x16x32(a, b, c);
 }
 
-// BF: bf16 rows (else fp16). NG: groups of a block. MT: 16-row tiles. NT: 16-output tiles of a wave. WK: waves that share the inputs.
-template <bool BF, int NG, int MT, int NT, int WK>
+// BF: bf16 rows (else fp16). NG: groups of a block. SWAP: more than four rows. MT: 16-row tiles. NT: 16-output tiles of a wave. WK: waves that share the inputs.
+// Weights are requested two blocks ahead, rows XD pieces of 32 inputs ahead, two pieces (whole lines of memory) together.
+template <bool BF, int NG, bool SWAP, int MT, int NT, int WK>
 __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
-    constexpr int kDepth = MT * 4 + NT <= 6 ? 3 : 2;               // blocks in flight per wave
-    constexpr int CPG = 4 / NG;                                    // 32-input pieces of a group
-    extern __shared__ float lds[];                                 // [WK][NT][MT][16 rows][16 outputs]
+    constexpr int WD = 2;
+    constexpr int XD = MT == 1 ? 8 : 4;
+    constexpr int CPG = 4 / NG;                                    // pieces of a group
+    extern __shared__ float lds[];                                 // [WK / 2][NT][MT][16 rows][16 outputs]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int tile0 = blockIdx.x * NT, row0 = blockIdx.y * (MT * 16);
     const int k0 = (int)((long)a.nkb * wave / WK), k1 = (int)((long)a.nkb * (wave + 1) / WK);
@@ -93,30 +95,36 @@ __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
     for (int n = 0; n < NT; ++n) wp[n] = a.blocks + (size_t)min(tile0 + n, a.tiles - 1) * a.nkb * block_bytes(NG);
     const uint16_t* xp[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) xp[m] = a.x + (size_t)min(row0 + m * 16 + r, a.M - 1) * a.x_stride + 8 * g;
+    for (int m = 0; m < MT; ++m) xp[m] = a.x + (size_t)min(row0 + m * 16 + (SWAP ? lane >> 2 : r), a.M - 1) * a.x_stride + 8 * (SWAP ? lane & 3 : g);
     // lane r of a row of sixteen keeps the scale of output 4 g + r / NG, group r % NG
     const int sm_at = 1024 + 4 * (4 * g * NG + (lane & (4 * NG - 1)));
 
-    u32x4 wq[kDepth][NT];
-    uint32_t smq[kDepth][NT];
-    Frag8 xq[kDepth][MT][4];
-    auto load = [&](auto slot, int kb) {
+    // More than four rows are requested four lanes to a row, so that lanes side by side share lines of memory, and change places on their way to
+    // the operand: lane (r, g) takes what lane 4 r + g loaded. Requested as operands, sixteen rows side by side, they took 68 clocks a request:
+    // 72 rows x 11008 x 4096 49 us, so 28; 9 rows x 4096 x 22016 14.0 and 13.0. Up to four rows lanes share lines anyway, and changing places costs
+    // more than it gains (one row x 11008 x 4096 8.0 us, so 9.3).
+    const int from = 4 * (4 * r + g);
+    u32x4 wq[WD][NT];
+    uint32_t smq[WD][NT];
+    Frag8 xq[XD][MT];
+    auto load_w = [&](auto slot, int kb) {
         constexpr int s = decltype(slot)::value;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const uint8_t* p = wp[n] + (size_t)kb * block_bytes(NG);
+            const uint8_t* p = wp[n] + (size_t)min(kb, k1 - 1) * block_bytes(NG);
             wq[s][n] = *reinterpret_cast<const u32x4*>(p + lane * 16);
             smq[s][n] = *reinterpret_cast<const uint32_t*>(p + sm_at);
         }
+    };
+    const int last = min(k1 * 4, a.Kd / 32) - 1;                                // (past the last input, in a padded block: codes, scales and offsets are zero)
+    auto load_x = [&](auto slot, int piece) {                      // pieces `piece`, `piece` + 1
+        constexpr int s = decltype(slot)::value;
+        const int i = min(piece, last) * 32, j = min(piece + 1, last) * 32;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int i = kb * 128 + 32 * c;                   // past the last input (a padded block): zeros
-                u32x4 v = {0, 0, 0, 0};
-                if (i < a.Kd) v = *reinterpret_cast<const u32x4_a2*>(xp[m] + i);
-                xq[s][m][c].v4 = v;
-            }
+        for (int m = 0; m < MT; ++m) {
+            xq[s][m].v4 = *reinterpret_cast<const u32x4_a2*>(xp[m] + i);
+            xq[s + 1][m].v4 = *reinterpret_cast<const u32x4_a2*>(xp[m] + j);
+        }
     };
     Frag8 ones;
 #pragma unroll
@@ -129,94 +137,109 @@ __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[n][m] = float4_t{0.f, 0.f, 0.f, 0.f};
 
-    auto multiply = [&](auto slot) {
-        constexpr int s = decltype(slot)::value;
-        float ss[NT], mm[NT];
+    if (k0 < k1) {
+        static_for<0, XD / 2>([&](auto s) { load_x(std::integral_constant<int, 2 * decltype(s)::value>{}, 4 * k0 + 2 * decltype(s)::value); });
+        static_for<0, WD>([&](auto s) { load_w(s, k0 + decltype(s)::value); });
+        for (int kb0 = k0; kb0 < k1; kb0 += WD)
+            static_for<0, WD>([&](auto ws) {
+                constexpr int s = decltype(ws)::value;
+                const int kb = kb0 + s;
+                if (kb < k1) {
+                    float ss[NT], mm[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float sc = sm_scale(smq[s][n]);
-            ss[n] = BF ? sc : sc * kCodeUnit;
-            mm[n] = BF ? fmaf(-128.f, sc, sm_offset(smq[s][n])) : sm_offset(smq[s][n]);
-        }
-        static_for<0, NG>([&](auto gg) {
-            constexpr int gi = decltype(gg)::value;
-            float4_t X[MT];
+                    for (int n = 0; n < NT; ++n) {
+                        const float sc = sm_scale(smq[s][n]);
+                        ss[n] = BF ? sc : sc * kCodeUnit;
+                        mm[n] = BF ? fmaf(-128.f, sc, sm_offset(smq[s][n])) : sm_offset(smq[s][n]);
+                    }
+                    static_for<0, NG>([&](auto gg) {
+                        constexpr int gi = decltype(gg)::value;
+                        float4_t X[MT], D[NT][MT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                X[m] = float4_t{0.f, 0.f, 0.f, 0.f};
+                        for (int m = 0; m < MT; ++m) {
+                            X[m] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < CPG; ++c) X[m] = mfma_x<BF>(ones, xq[s][m][gi * CPG + c], X[m]);
-            }
+                            for (int n = 0; n < NT; ++n) D[n][m] = float4_t{0.f, 0.f, 0.f, 0.f};
+                        }
+                        static_for<0, CPG>([&](auto pc) {
+                            constexpr int c = gi * CPG + decltype(pc)::value, xs = (s * 4 + c) % XD;
+                            Frag8 xf[MT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                Frag8 wf[CPG];
+                            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int c = 0; c < CPG; ++c)
+                                for (int j = 0; j < 4; ++j) xf[m].w[j] = SWAP ? __builtin_amdgcn_ds_bpermute(from, xq[xs][m].w[j]) : xq[xs][m].w[j];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) wf[c].w[j] = ((wq[s][n][gi * CPG + c] >> (4 * j)) & kCodeLo) | kBias;
+                            for (int m = 0; m < MT; ++m) X[m] = mfma_x<BF>(ones, xf[m], X[m]);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    float4_t D = float4_t{0.f, 0.f, 0.f, 0.f};
+                            for (int n = 0; n < NT; ++n) {
+                                Frag8 wf;
 #pragma unroll
-                    for (int c = 0; c < CPG; ++c) D = mfma_x<BF>(wf[c], xq[s][m][gi * CPG + c], D);
-                    static_for<0, 4>([&](auto ii) {
-                        constexpr int i = decltype(ii)::value;
-                        acc[n][m][i] = fmaf(row_lane<i * NG + gi>(ss[n]), D[i], acc[n][m][i]);
-                        acc[n][m][i] = fmaf(row_lane<i * NG + gi>(mm[n]), X[m][i], acc[n][m][i]);
+                                for (int j = 0; j < 4; ++j) wf.w[j] = ((wq[s][n][c] >> (4 * j)) & kCodeLo) | kBias;
+#pragma unroll
+                                for (int m = 0; m < MT; ++m) D[n][m] = mfma_x<BF>(wf, xf[m], D[n][m]);
+                            }
+                            if constexpr (c % 2 == 1) load_x(std::integral_constant<int, xs - 1>{}, 4 * kb + c - 1 + XD);
+                        });
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            static_for<0, 4>([&](auto ii) {
+                                constexpr int i = decltype(ii)::value;
+                                const float sc = row_lane<i * NG + gi>(ss[n]), of = row_lane<i * NG + gi>(mm[n]);
+#pragma unroll
+                                for (int m = 0; m < MT; ++m) acc[n][m][i] = fmaf(of, X[m][i], fmaf(sc, D[n][m][i], acc[n][m][i]));
+                            });
                     });
+                    load_w(ws, kb + WD);
                 }
-            }
-        });
-    };
-    static_for<0, kDepth>([&](auto s) { if (k0 + decltype(s)::value < k1) load(s, k0 + decltype(s)::value); });
-    for (int kb = k0; kb < k1; kb += kDepth)
-        static_for<0, kDepth>([&](auto s) {
-            constexpr int j = decltype(s)::value;
-            if (kb + j < k1) {
-                multiply(s);
-                if (kb + j + kDepth < k1) load(s, kb + j + kDepth);
-            }
-        });
+            });
+    }
 
-    // ---- the waves' sums, in their order
+    // ---- the waves' sums: those of the upper half go to the lower half, whose are then added up in their order
+    auto place = [&](int w, int n, int m) {                        // [row r][output 4 g + i]
+        return reinterpret_cast<float4_t*>(lds + ((w * NT + n) * MT + m) * 256 + r * 16 + 4 * g);
+    };
+    if (wave >= WK / 2)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-            *reinterpret_cast<float4_t*>(lds + (((size_t)wave * NT + n) * MT + m) * 256 + r * 16 + 4 * g) = acc[n][m];   // [row r][output 4 g + i]
+            for (int m = 0; m < MT; ++m) *place(wave - WK / 2, n, m) = acc[n][m];
+    __syncthreads();
+    if (wave < WK / 2)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) *place(wave, n, m) = acc[n][m] + *place(wave, n, m);
     __syncthreads();
     for (int idx = threadIdx.x; idx < NT * MT * 256; idx += WK * 64) {
         const int o = idx & 15, n = idx >> 4 & (NT - 1), row = idx / (16 * NT);        // outputs of a row side by side
         const int at = (n * MT + (row >> 4)) * 256 + (row & 15) * 16 + o;
         float v = lds[at];
 #pragma unroll
-        for (int w = 1; w < WK; ++w) v += lds[w * NT * MT * 256 + at];
+        for (int w = 1; w < WK / 2; ++w) v += lds[w * NT * MT * 256 + at];
         const int gr = row0 + row, gn = (tile0 + n) * 16 + o;
         if (gr < a.M && gn < a.N) a.out[(size_t)gr * a.out_stride + gn] = BF ? f32_to_bf16(v) : f32_to_f16(v);
     }
 }
 
-template <bool BF, int NG, int MT>
+template <bool BF, int NG, bool SWAP, int MT, int NT, int WK>
 static void launch_w4(const W4Args& a, hipStream_t stream) {
-    auto go = [&](auto nt, auto wk) {
-        constexpr int NT = decltype(nt)::value, WK = decltype(wk)::value;
-        const dim3 grid((unsigned)((a.tiles + NT - 1) / NT), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
-        hipLaunchKernelGGL((w4_matmul_kernel<BF, NG, MT, NT, WK>), grid, dim3(WK * 64), WK * NT * MT * 1024, stream, a);
-    };
-    if (a.tiles >= 1024) go(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
-    else go(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+    const dim3 grid((unsigned)((a.tiles + NT - 1) / NT), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
+    hipLaunchKernelGGL((w4_matmul_kernel<BF, NG, SWAP, MT, NT, WK>), grid, dim3(WK * 64), WK / 2 * NT * MT * 1024, stream, a);
 }
 
+// Output tiles per wave (NT) and waves to a workgroup (WK): several tiles share a wave's rows where there are tiles enough for every
+// compute unit all the same. bf16, group 128, us with one tile and eight waves / as taken here:
+//   1 row 4096 -> 22016 14.4 / 11.9, 9 rows 15.8 / 13.0;   24 rows 4096 -> 12288 14.8 / 11.4, 40 rows 20.7 / 14.4;   72 rows 4096 -> 22016 66.8 / 39.7,
+//   2048 -> 6144 15.9 / 10.2. And where one tile is taken, with two: 1 row 4096 -> 4096 4.3 / 5.2, 72 rows 11008 -> 4096 28.1 / 29.9.
 template <bool BF, int NG>
 static void launch_rows(const W4Args& a, hipStream_t stream) {
     const int mt = std::min(5, (a.M + 15) / 16);
-    switch (mt) {
-        case 1: launch_w4<BF, NG, 1>(a, stream); break;
-        case 2: launch_w4<BF, NG, 2>(a, stream); break;
-        case 3: launch_w4<BF, NG, 3>(a, stream); break;
-        case 4: launch_w4<BF, NG, 4>(a, stream); break;
-        default: launch_w4<BF, NG, 5>(a, stream); break;
-    }
+    if (a.M <= 4) a.tiles >= 1024 ? launch_w4<BF, NG, false, 1, 2, 4>(a, stream) : launch_w4<BF, NG, false, 1, 1, 8>(a, stream);
+    else if (mt == 1) a.tiles >= 1024 ? launch_w4<BF, NG, true, 1, 2, 4>(a, stream) : launch_w4<BF, NG, true, 1, 1, 8>(a, stream);
+    else if (mt == 2) a.tiles >= 512 ? launch_w4<BF, NG, true, 2, 4, 8>(a, stream) : launch_w4<BF, NG, true, 2, 1, 8>(a, stream);
+    else if (mt == 3) a.tiles >= 512 ? launch_w4<BF, NG, true, 3, 4, 8>(a, stream) : launch_w4<BF, NG, true, 3, 1, 8>(a, stream);
+    else if (mt == 4) a.tiles >= 320 ? launch_w4<BF, NG, true, 4, 2, 8>(a, stream) : launch_w4<BF, NG, true, 4, 1, 8>(a, stream);
+    else a.tiles >= 320 ? launch_w4<BF, NG, true, 5, 2, 8>(a, stream) : launch_w4<BF, NG, true, 5, 1, 8>(a, stream);
 }
 
 }  // namespace laser
