@@ -5,6 +5,7 @@ There is no fallback of any kind: if liblaser.so is missing or a call fails, Las
 from __future__ import annotations
 
 import ctypes as C
+from array import array
 import sys
 import os
 
@@ -344,17 +345,38 @@ class KVCache4(KVCache):
         _check(lib().laser_kv_create_4bit(C.byref(d), _stream(stream), C.byref(self._h)), "laser_kv_create_4bit")
 
 
-def _heads(t: torch.Tensor, name: str, B: int, R: int, H: int, dh: int, dtype) -> _Heads:
+def _heads(t: torch.Tensor, name: str, shape, dtype, dev: int) -> _Heads:
     """A [B][R][H][dh] tensor, in any order of its first three dimensions, as laser_heads."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and tuple(t.shape) == (B, R, H, dh) and (t.stride(3) == 1 or t.numel() == 0)):
-        raise LaserError(f"{name} must be a CUDA tensor [{B}][{R}][{H}][{dh}] of {dtype} with contiguous channels")
-    _here(t, name)
-    return _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.shape != shape:
+        raise LaserError(f"{name} must be a CUDA tensor {list(shape)} of {dtype} with contiguous channels")
+    s = t.stride()
+    if s[3] != 1 and t.numel():
+        raise LaserError(f"{name} must have contiguous channels")
+    _here(t, name, dev)
+    return _Heads(t.data_ptr(), s[0], s[1], s[2])
 
 
-def _here(t: torch.Tensor, name: str) -> None:
-    if t.device.index != torch.cuda.current_device():
+def _here(t: torch.Tensor, name: str, dev: int) -> None:
+    if t.get_device() != dev:
         raise LaserError(f"{name} is on {t.device}, not on the current device")
+
+
+def _device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _on(stream, dev: int) -> int:
+    """_stream() at a tenth of its host time where the current stream is meant (a small call takes less than that on the device)."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
+def _ids(seq_ids):
+    """Sequence slots as a host int32 array."""
+    return _host_i32(seq_ids, "seq_ids") if isinstance(seq_ids, (np.ndarray, torch.Tensor)) else array("i", seq_ids)
+
+
+def _ids_ptr(ids) -> int:
+    return ids.ctypes.data if isinstance(ids, np.ndarray) else ids.buffer_info()[0]
 
 
 def _out(shape, dtype, device, stream) -> torch.Tensor:
@@ -366,23 +388,29 @@ def _out(shape, dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _step_args(kv, ids, n_rows, tree_parent, B, R):
+def _cache_device(kv) -> int:
     if not isinstance(kv, KVCache4):
         raise LaserError("kv must be a KVCache4")
-    if kv.device != torch.cuda.current_device():
+    dev = _device()
+    if kv.device != dev:
         raise LaserError(f"the cache is on device {kv.device}, not on the current one")
-    if ids.size != B:
+    return dev
+
+
+def _step_args(n_ids, n_rows, tree_parent, B, R, dev):
+    if n_ids != B:
         raise LaserError(f"seq_ids must name {B} sequences")
     if n_rows is not None:
-        if tuple(n_rows.shape) != (B,):
+        if n_rows.shape != (B,):
             raise LaserError("n_rows must be [B]")
-        _here(n_rows, "n_rows")
+        _here(n_rows, "n_rows", dev)
+        n_rows = _dev(n_rows, torch.int32, "n_rows")
     if tree_parent is not None:
-        if tuple(tree_parent.shape) != (B, R - 1):
+        if tree_parent.shape != (B, R - 1):
             raise LaserError("tree_parent must be [B][R - 1]")
-        _here(tree_parent, "tree_parent")
-    return (None if n_rows is None else _dev(n_rows, torch.int32, "n_rows"),
-            None if tree_parent is None else _dev(tree_parent, torch.int32, "tree_parent"))
+        _here(tree_parent, "tree_parent", dev)
+        tree_parent = _dev(tree_parent, torch.int32, "tree_parent")
+    return n_rows, tree_parent
 
 
 def rope_table(max_pos: int, dim: int, base: float = 10000.0, stream=None) -> torch.Tensor:
@@ -396,67 +424,69 @@ def kv_append(kv: KVCache4, layer: int, seq_ids, k: torch.Tensor, v: torch.Tenso
               q_out=None, stream=None):
     """laser_kv_append: keys and values [B][R][heads][head_dim] of a step's rows into the cache, rotated by `rope`
     (rope_table; None: not rotated). Returns the rotated queries (q [B][R][query heads][head_dim], may be q_out itself) or None."""
-    ids = _host_i32(seq_ids, "seq_ids")
-    if k.dim() != 4:
+    dev, ids = _cache_device(kv), _ids(seq_ids)
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
         raise LaserError("k must be [B][R][heads][head_dim]")
-    B, R = k.shape[0], k.shape[1]
-    nr, tp = _step_args(kv, ids, n_rows, tree_parent, B, R)
+    B, R = k.shape[:2]
+    nr, tp = _step_args(len(ids), n_rows, tree_parent, B, R, dev)
     dt = k.dtype
     if dt not in _DTYPES:
         raise LaserError(f"k: {dt} is not float16, bfloat16 or float32")
-    hk = _heads(k, "k", B, R, kv.n_heads, kv.head_dim, dt)
-    hv = _heads(v, "v", B, R, kv.n_heads, kv.head_dim, dt)
+    shape = (B, R, kv.n_heads, kv.head_dim)
+    hk, hv = _heads(k, "k", shape, dt, dev), _heads(v, "v", shape, dt, dev)
     hq = ho = None
     n_heads = 0
     if q is not None:
-        if q.dim() != 4:
+        if not isinstance(q, torch.Tensor) or q.dim() != 4:
             raise LaserError("q must be [B][R][heads][head_dim]")
         n_heads = q.shape[2]
         if q_out is None:
             q_out = _out(q.shape, dt, q.device, stream)
-        hq, ho = _heads(q, "q", B, R, n_heads, kv.head_dim, dt), _heads(q_out, "q_out", B, R, n_heads, kv.head_dim, dt)
+        shape = (B, R, n_heads, kv.head_dim)
+        hq, ho = _heads(q, "q", shape, dt, dev), _heads(q_out, "q_out", shape, dt, dev)
     rope_p, rope_dim, max_pos = None, 0, 0
     if rope is not None:
         if rope.dim() != 3 or rope.shape[2] != 2:
             raise LaserError("rope must be [max_pos][rope_dim / 2][2]")
-        _here(rope, "rope")
+        _here(rope, "rope", dev)
         rope_p, max_pos, rope_dim = _dev(rope, torch.float32, "rope"), rope.shape[0], 2 * rope.shape[1]
-    _check(lib().laser_kv_append(kv._h, layer, ids.ctypes.data, nr, tp, B, R, _DTYPES[dt], hk, hv, hq, ho, n_heads, rope_p, rope_dim, max_pos,
-                                 _stream(stream)), "laser_kv_append")
+    _check(lib().laser_kv_append(kv._h, layer, _ids_ptr(ids), nr, tp, B, R, _DTYPES[dt], hk, hv, hq, ho, n_heads, rope_p, rope_dim, max_pos,
+                                 _on(stream, dev)), "laser_kv_append")
     return q_out
 
 
 def kv_attend(kv: KVCache4, layer: int, seq_ids, q: torch.Tensor, tree_parent=None, n_rows=None, scale=None, out=None, stream=None) -> torch.Tensor:
     """laser_kv_attend: q [B][R][query heads][head_dim] -> the same shape. scale: 1 / sqrt(head_dim) unless given."""
-    ids = _host_i32(seq_ids, "seq_ids")
+    dev, ids = _cache_device(kv), _ids(seq_ids)
     if not isinstance(q, torch.Tensor) or q.dim() != 4:
         raise LaserError("q must be [B][R][heads][head_dim]")
     B, R, H, dh = q.shape
-    nr, tp = _step_args(kv, ids, n_rows, tree_parent, B, R)
+    nr, tp = _step_args(len(ids), n_rows, tree_parent, B, R, dev)
     if q.dtype not in _DTYPES:
         raise LaserError(f"q: {q.dtype} is not float16, bfloat16 or float32")
-    hq = _heads(q, "q", B, R, H, kv.head_dim, q.dtype)
+    shape = (B, R, H, kv.head_dim)
+    hq = _heads(q, "q", shape, q.dtype, dev)
     if out is None:
         out = _out(q.shape, q.dtype, q.device, stream)
-    ho = _heads(out, "out", B, R, H, kv.head_dim, q.dtype)
-    _check(lib().laser_kv_attend(kv._h, layer, ids.ctypes.data, nr, tp, B, R, H, _DTYPES[q.dtype], hq, dh ** -0.5 if scale is None else scale, ho,
-                                 _stream(stream)), "laser_kv_attend")
+    ho = _heads(out, "out", shape, q.dtype, dev)
+    _check(lib().laser_kv_attend(kv._h, layer, _ids_ptr(ids), nr, tp, B, R, H, _DTYPES[q.dtype], hq, dh ** -0.5 if scale is None else scale, ho,
+                                 _on(stream, dev)), "laser_kv_attend")
     return out
 
 
 def kv_read(kv: KVCache4, layer: int, seq_ids, n: int, start: int = -1, dtype=torch.float16, out=None, stream=None):
     """laser_kv_read: the keys and values [B][n][heads][head_dim] that tokens start .. start + n - 1 (-1: those behind the committed
     length) stand for."""
-    ids = _host_i32(seq_ids, "seq_ids")
-    _step_args(kv, ids, None, None, ids.size, 1)
-    shape = (ids.size, n, kv.n_heads, kv.head_dim)
+    dev, ids = _cache_device(kv), _ids(seq_ids)
+    B = len(ids)
+    shape = (B, n, kv.n_heads, kv.head_dim)
     if out is None:
         out = _out(shape, dtype, "cuda", stream), _out(shape, dtype, "cuda", stream)
     k, v = out
     if k.dtype not in _DTYPES:
         raise LaserError(f"{k.dtype} is not float16, bfloat16 or float32")
-    _check(lib().laser_kv_read(kv._h, layer, ids.ctypes.data, ids.size, start, n, _DTYPES[k.dtype], _heads(k, "k", *shape, k.dtype),
-                               _heads(v, "v", *shape, k.dtype), _stream(stream)), "laser_kv_read")
+    _check(lib().laser_kv_read(kv._h, layer, _ids_ptr(ids), B, start, n, _DTYPES[k.dtype], _heads(k, "k", shape, k.dtype, dev),
+                               _heads(v, "v", shape, k.dtype, dev), _on(stream, dev)), "laser_kv_read")
     return k, v
 
 
@@ -465,7 +495,7 @@ def w4_quantize(w: torch.Tensor, group: int = 128, stream=None):
     p = _dev(w, torch.bfloat16, "w")
     if w.dim() != 2:
         raise LaserError("w must be [N][Kd]")
-    _here(w, "w")
+    _here(w, "w", _device())
     N, Kd = w.shape
     if group not in (32, 64, 128) or Kd % group:
         raise LaserError(f"group {group}: 32, 64 or 128, and Kd {Kd} a multiple of it")
@@ -483,12 +513,12 @@ class W4:
             raise LaserError("codes must be [N][Kd / 2], scales and offsets [N][Kd / group]")
         for t, n in ((codes, "codes"), (scales, "scales"), (offsets, "offsets")):
             if isinstance(t, torch.Tensor) and t.is_cuda:
-                _here(t, n)
+                _here(t, n, _device())
         self.N, self.Kd = codes.shape[0], 2 * codes.shape[1]
         self.group = self.Kd // scales.shape[1]
         if self.group * scales.shape[1] != self.Kd:
             raise LaserError("Kd is not a multiple of the number of groups")
-        self.device = codes.device
+        self.device = codes.get_device()
         _check(lib().laser_w4_create(_dev(codes, torch.uint8, "codes"), _dev(scales, torch.float16, "scales"), _dev(offsets, torch.float16, "offsets"),
                                      self.N, self.Kd, self.group, _stream(stream), C.byref(self._h)), "laser_w4_create")
 
@@ -505,18 +535,17 @@ class W4:
 
 def w4_matmul(w: W4, x: torch.Tensor, out=None, stream=None) -> torch.Tensor:
     """laser_w4_matmul: x [M][Kd] (float16 or bfloat16, contiguous within a row) -> [M][N] of the same type."""
-    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype in (torch.float16, torch.bfloat16) and x.dim() == 2 and x.shape[1] == w.Kd and x.stride(1) == 1):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in (torch.float16, torch.bfloat16) or x.dim() != 2 or x.shape[1] != w.Kd or x.stride(1) != 1:
         raise LaserError(f"x must be a CUDA tensor [M][{w.Kd}] of float16 or bfloat16 with contiguous rows")
-    M = x.shape[0]
+    M, dev = x.shape[0], _device()
     if out is None:
         out = _out((M, w.N), x.dtype, x.device, stream)
-    if not (out.is_cuda and out.dtype == x.dtype and tuple(out.shape) == (M, w.N) and (out.stride(1) == 1 or w.N == 1)):
+    elif not isinstance(out, torch.Tensor) or not out.is_cuda or out.dtype != x.dtype or out.shape != (M, w.N) or (out.stride(1) != 1 and w.N > 1):
         raise LaserError(f"out must be a CUDA tensor [{M}][{w.N}] of {x.dtype} with contiguous rows")
-    _here(x, "x")
-    if out.device != x.device or w.device != x.device:
-        raise LaserError(f"x, out and the weights are on {x.device}, {out.device} and {w.device}")
+    if x.get_device() != dev or out.get_device() != dev or w.device != dev:
+        raise LaserError(f"x, out and the weights must be on the current device, not on {x.device}, {out.device} and {w.device}")
     _check(lib().laser_w4_matmul(w._h, x.data_ptr(), x.stride(0) if M > 1 else w.Kd, M, _DTYPES[x.dtype], out.data_ptr(),
-                                 out.stride(0) if M > 1 else w.N, _stream(stream)), "laser_w4_matmul")
+                                 out.stride(0) if M > 1 else w.N, _on(stream, dev)), "laser_w4_matmul")
     return out
 
 

@@ -11,9 +11,9 @@
 
 namespace laser {
 
-// Four lanes (g = 0..3) share a token and head; lane g takes channels 32 c + 8 g .. + 7 of the keys' groups c, whose rotary
-// partners (32 channels or a multiple of them away) are its own too, and channels 32 c + 4 g .. + 3 and 32 c + 16 + 4 g .. + 3 of
-// the values' groups, which are whole bytes of the page.
+// A thread takes two groups' worth of a quarter g of a token and head, keys, values or queries: channels 8 g .. 8 g + 7 of groups `half` and half + 2
+// (0 and 1 at 64 channels) of keys and queries, whose rotary partners are then its own or its neighbour's; of values channels 4 g .. + 3 and
+// 16 + 4 g .. + 3 of its groups, which are whole bytes of the page. Keys, values and queries are in different waves.
 template <class T>
 __device__ inline T quad_min(T x) { x = min(x, __shfl_xor(x, 1)); return min(x, __shfl_xor(x, 2)); }
 template <class T>
@@ -46,156 +46,162 @@ __device__ inline void load_sum(const Heads& h, size_t o, int n_part, int64_t pa
         }
 }
 
+template <class T>
+__device__ inline T quad_or(T x) { x |= __shfl_xor(x, 1); return x | __shfl_xor(x, 2); }
+
 template <int DH, int DT>
 __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
-    constexpr int NG = DH / 32;
-    const int per_row = 4 * (a.H + a.Hq);
+    constexpr int NG = DH / 32, SP = NG / 2, STEP = NG / 2;              // threads of a quarter; a thread's groups are half and half + STEP
+    const int what = blockIdx.y;                                         // 0: keys, 1: values, 2: queries
+    const int heads = what == 2 ? a.Hq : a.H;
     const long t = (long)blockIdx.x * 256 + threadIdx.x;
-    const int g = threadIdx.x & 3;
-    const long row = t / per_row;
-    const int item = (int)(t % per_row) >> 2;
-    if (row >= (long)a.B * a.R) return;                                  // (four lanes together, as every exit below)
+    const int g = threadIdx.x & 3, half = threadIdx.x >> 2 & (SP - 1);
+    const long item = t / (4 * SP), row = item / heads;
+    const int h = (int)(item % heads);
+    if (row >= (long)a.B * a.R) return;                                  // (the threads of a head together, as every exit below)
     const int b = (int)(row / a.R), r = (int)(row % a.R);
     if (a.n_rows && r >= a.n_rows[b]) return;
     const int slot_id = a.seqs.slot(b);
     const int len = a.start >= 0 ? a.start : a.lens[slot_id];
     const int slot = len + r;
-    const int hg = a.rope_dim / 64;                                      // groups in half of the rotated channels
-    int pos = 0;
-    if (hg) {
-        if (a.row_pos) pos = a.row_pos[row];
-        else if (!a.parent) pos = slot;
-        else {
-            const int32_t* parent = a.parent + (size_t)b * (a.R - 1);
-            int depth = 0;
-            for (int i = r; i > 0; i = up_row(parent, i)) ++depth;
-            pos = len + depth;
-        }
-        pos = min(max(pos, 0), a.max_pos - 1);
-    }
-    // (cos, sin) of channels 32 c + 8 g .. + 7, c < hg
-    const float2* turn = a.rope + (size_t)pos * (32 * hg) + 8 * g;
+    if (what < 2 && (slot >= a.seqs.tokens(b) || slot < 0)) return;
 
-    if (item >= a.H) {                                                   // ---- queries: rotated, in their own type
-        const int h = item - a.H;
-        const size_t qi = (size_t)b * a.q.seq + (size_t)r * a.q.row + (size_t)h * a.q.head + 8 * g;
-        const size_t qo = (size_t)b * a.q_out.seq + (size_t)r * a.q_out.row + (size_t)h * a.q_out.head + 8 * g;
-        float x[NG][8];
-#pragma unroll
-        for (int c = 0; c < NG; ++c) load_sum<DT, 8>(a.q, qi + 32 * c, a.n_part, a.part_stride, x[c]);
-        auto rotate = [&](float (&u)[8], float (&w)[8], int c) {
-            float cs[16];
-            load_elems<DT_F32, 8>(turn + 32 * c, 0, *reinterpret_cast<float(*)[8]>(cs));
-            load_elems<DT_F32, 8>(turn + 32 * c + 4, 0, *reinterpret_cast<float(*)[8]>(cs + 8));
+    // ---- positions; (cos, sin) of the eight channels of a rotated group c: turn + 32 c (c counts within the first half of the rotated ones)
+    const int hg = a.rope_dim / 64;                                      // groups in half of the rotated channels
+    const float2* turn = nullptr;
+    if (hg && what != 1) {
+        int pos = slot;
+        if (a.row_pos) pos = a.row_pos[row];
+        else if (a.parent) {
+            const int32_t* parent = a.parent + (size_t)b * (a.R - 1);
+            pos = len;
+            for (int i = r; i > 0; i = up_row(parent, i)) ++pos;
+        }
+        turn = a.rope + (size_t)min(max(pos, 0), a.max_pos - 1) * (32 * hg) + 8 * g;
+    }
+    // Rotates x[0], x[1] in T. hg == STEP: they are each other's partners. 64 of 128 channels: groups 0 and 1 are, which two threads hold.
+    auto rotate = [&](auto& x) {
+        typedef typename std::remove_reference<decltype(x[0][0])>::type T;
+        if (!hg) return;
+        float cs[16];
+        const float2* tp = turn + (hg == STEP ? 32 * half : 0);
+        load_elems<DT_F32, 8>(tp, 0, *reinterpret_cast<float(*)[8]>(cs));
+        load_elems<DT_F32, 8>(tp + 4, 0, *reinterpret_cast<float(*)[8]>(cs + 8));
+        if (hg == STEP) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float p = u[j], q = w[j], co = cs[2 * j], si = cs[2 * j + 1];
-                u[j] = p * co - q * si;
-                w[j] = p * si + q * co;
+                const T p = x[0][j], q = x[1][j], co = cs[2 * j], si = cs[2 * j + 1];
+                x[0][j] = p * co - q * si;
+                x[1][j] = p * si + q * co;
             }
-        };
-        if (hg == NG / 2) {
+        } else {
 #pragma unroll
-            for (int c = 0; c < NG / 2; ++c) rotate(x[c], x[c + NG / 2], c);
-        } else if (NG == 4 && hg == 1) rotate(x[0], x[1], 0);
+            for (int j = 0; j < 8; ++j) {
+                const T mine = x[0][j], other = __shfl_xor((float)mine, 4), co = cs[2 * j], si = cs[2 * j + 1];      // (inputs: fp32 holds them)
+                x[0][j] = half ? other * si + mine * co : mine * co - other * si;
+            }
+        }
+    };
+    const Heads& in = what == 0 ? a.k : what == 1 ? a.v : a.q;
+    const size_t at = (size_t)b * in.seq + (size_t)r * in.row + (size_t)h * in.head;
+
+    if (what == 2) {                                                     // ---- queries: in their own type
+        const size_t to = (size_t)b * a.q_out.seq + (size_t)r * a.q_out.row + (size_t)h * a.q_out.head;
+        float x[2][8];
 #pragma unroll
-        for (int c = 0; c < NG; ++c) store_elems<DT, 8>(a.q_out.p, qo + 32 * c, x[c]);
+        for (int c = 0; c < 2; ++c) load_sum<DT, 8>(in, at + 32 * (half + c * STEP) + 8 * g, a.n_part, a.part_stride, x[c]);
+        rotate(x);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) store_elems<DT, 8>(a.q_out.p, to + 32 * (half + c * STEP) + 8 * g, x[c]);
         return;
     }
 
-    // ---- keys and values of one token and head
-    if (slot >= a.seqs.tokens(b) || slot < 0) return;
-    const int h = item, tp = slot % kPageSize;
+    const int tp = slot % kPageSize;
     const int pg = a.block_table[(size_t)slot_id * a.mpps + slot / kPageSize];
     uint8_t* page = a.pages + ((size_t)pg * a.H + h) * page4_bytes(DH);
-    float kf[NG][8], vf[NG][8];
-    {
-        const size_t ki = (size_t)b * a.k.seq + (size_t)r * a.k.row + (size_t)h * a.k.head + 8 * g;
-        const size_t vi = (size_t)b * a.v.seq + (size_t)r * a.v.row + (size_t)h * a.v.head + 4 * g;
-#pragma unroll
-        for (int c = 0; c < NG; ++c) {
-            load_sum<DT, 8>(a.k, ki + 32 * c, a.n_part, a.part_stride, kf[c]);
-            load_sum<DT, 4>(a.v, vi + 32 * c, a.n_part, a.part_stride, *reinterpret_cast<float(*)[4]>(&vf[c][0]));
-            load_sum<DT, 4>(a.v, vi + 32 * c + 16, a.n_part, a.part_stride, *reinterpret_cast<float(*)[4]>(&vf[c][4]));
-        }
-    }
     // A key or value that is not finite makes the token's key NaN: every row that sees the token gets NaN from this head, and no
     // other row meets it. The codes and the values' scales stay finite, so that what a mask hides never enters a product.
-    bool bad = false;
-#pragma unroll
-    for (int c = 0; c < NG; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool fk = __builtin_isfinite(kf[c][j]), fv = __builtin_isfinite(vf[c][j]);
-            bad |= !fk || !fv;
-            kf[c][j] = fk ? kf[c][j] : 0.f;
-            vf[c][j] = fv ? vf[c][j] : 0.f;
-        }
-    bad |= (bool)__shfl_xor((int)bad, 1);
-    bad |= (bool)__shfl_xor((int)bad, 2);
-
-    double x[NG][8];
-#pragma unroll
-    for (int c = 0; c < NG; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[c][j] = kf[c][j];
-    auto rotate = [&](double (&u)[8], double (&w)[8], int c) {
-        float cs[16];
-        load_elems<DT_F32, 8>(turn + 32 * c, 0, *reinterpret_cast<float(*)[8]>(cs));
-        load_elems<DT_F32, 8>(turn + 32 * c + 4, 0, *reinterpret_cast<float(*)[8]>(cs + 8));
+    auto finite = [&](float (&x)[8]) {
+        bool all = true;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const double p = u[j], q = w[j], co = cs[2 * j], si = cs[2 * j + 1];
-            u[j] = p * co - q * si;
-            w[j] = p * si + q * co;
+            const bool f = __builtin_isfinite(x[j]);
+            all &= f;
+            x[j] = f ? x[j] : 0.f;
         }
+        return all;
     };
-    if (hg == NG / 2) {
+    float x[2][8];
+    if (what == 0) {                                                     // ---- keys
+        bool bad = false;
 #pragma unroll
-        for (int c = 0; c < NG / 2; ++c) rotate(x[c], x[c + NG / 2], c);
-    } else if (NG == 4 && hg == 1) rotate(x[0], x[1], 0);
-
-    uint32_t kw[NG];                       // words 2 p, 2 p + 1 of groups 2 p, 2 p + 1
-    uint32_t ksm = 0, vsm = 0;             // of group g
+        for (int c = 0; c < 2; ++c) load_sum<DT, 8>(in, at + 32 * (half + c * STEP) + 8 * g, a.n_part, a.part_stride, x[c]);
+        {
+            const size_t va = (size_t)b * a.v.seq + (size_t)r * a.v.row + (size_t)h * a.v.head;
+            float v[2][8];
 #pragma unroll
-    for (int c = 0; c < NG; ++c) kw[c] = 0;
+            for (int c = 0; c < 2; ++c) load_sum<DT, 8>(a.v, va + 32 * (half + c * STEP) + 8 * g, a.n_part, a.part_stride, v[c]);
 #pragma unroll
-    for (int c = 0; c < NG; ++c) {
-        double lo = x[c][0], hi = x[c][0];
+            for (int c = 0; c < 2; ++c) bad |= !finite(v[c]) | !finite(x[c]);
+        }
+        bad = quad_or((int)bad);
+        if (SP == 2) bad |= (bool)__shfl_xor((int)bad, 4);
+        double y[2][8];
 #pragma unroll
-        for (int j = 1; j < 8; ++j) { lo = fmin(lo, x[c][j]); hi = fmax(hi, x[c][j]); }
-        const Group gr = make_group(quad_min(lo), quad_max(hi));
-        const float inv = 1.f / gr.s;
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) kw[(c & ~1) + (j >> 2)] |= code_of(x[c][j], gr, inv) << (8 * code_byte(j & 3) + 4 * (c & 1));
-        if (c == g) ksm = bad ? (gr.sm & 0xFFFFu) | 0x7E000000u : gr.sm;
+            for (int j = 0; j < 8; ++j) y[c][j] = x[c][j];
+        rotate(y);
+        uint32_t code[2][2] = {{0, 0}, {0, 0}};                          // of groups half, half + STEP: bits 0..3 of the bytes of two words
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            double lo = y[c][0], hi = y[c][0];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) { lo = fmin(lo, y[c][j]); hi = fmax(hi, y[c][j]); }
+            const Group gr = make_group(quad_min(lo), quad_max(hi));
+            const float inv = 1.f / gr.s;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) code[c][j >> 2] |= code_of(y[c][j], gr, inv) << (8 * code_byte(j & 3));
+            if (g == 0) reinterpret_cast<uint32_t*>(page + page4_ksm(DH))[sm_index(DH, tp, half + c * STEP)] = bad ? (gr.sm & 0xFFFFu) | 0x7E000000u : gr.sm;
+        }
+        uint8_t* kp = page + (g * 16 + tp) * (DH / 8);
+        if constexpr (SP == 1) {
+            *reinterpret_cast<u32x2*>(kp) = u32x2{code[0][0] | (code[1][0] << 4), code[0][1] | (code[1][1] << 4)};
+        } else {
+            // words 0, 1 are groups 0 (low) and 1 (high), words 2, 3 groups 2 and 3: a thread keeps its own half and gets the other's codes
+            const uint32_t o0 = __shfl_xor(half ? code[0][0] : code[1][0], 4), o1 = __shfl_xor(half ? code[0][1] : code[1][1], 4);
+            const u32x2 w = half ? u32x2{o0 | (code[1][0] << 4), o1 | (code[1][1] << 4)} : u32x2{code[0][0] | (o0 << 4), code[0][1] | (o1 << 4)};
+            *reinterpret_cast<u32x2*>(kp + 8 * half) = w;
+        }
+        return;
     }
-    uint8_t* kp = page + (g * 16 + tp) * (DH / 8);
-    if constexpr (NG == 4) *reinterpret_cast<u32x4*>(kp) = u32x4{kw[0], kw[1], kw[2], kw[3]};
-    else *reinterpret_cast<u32x2*>(kp) = u32x2{kw[0], kw[1]};
-
+    // ---- values
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const size_t vi = at + 32 * (half + c * STEP) + 4 * g;
+        load_sum<DT, 4>(in, vi, a.n_part, a.part_stride, *reinterpret_cast<float(*)[4]>(&x[c][0]));
+        load_sum<DT, 4>(in, vi + 16, a.n_part, a.part_stride, *reinterpret_cast<float(*)[4]>(&x[c][4]));
+    }
     uint8_t* vp = page + page4_v(DH) + ((tp >> 2) * 16 + 4 * g) * (DH / 8) + code_byte(tp & 3);
 #pragma unroll
-    for (int c = 0; c < NG; ++c) {
-        float lo = vf[c][0], hi = vf[c][0];
+    for (int c = 0; c < 2; ++c) {
+        (void)finite(x[c]);
+        const int grp = half + c * STEP;
+        float lo = x[c][0], hi = x[c][0];
 #pragma unroll
-        for (int j = 1; j < 8; ++j) { lo = fminf(lo, vf[c][j]); hi = fmaxf(hi, vf[c][j]); }
+        for (int j = 1; j < 8; ++j) { lo = fminf(lo, x[c][j]); hi = fmaxf(hi, x[c][j]); }
         const Group gr = make_group((double)quad_min(lo), (double)quad_max(hi));
         const float inv = 1.f / gr.s;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            vp[e * (DH / 8) + 4 * c] = (uint8_t)(code_of((double)vf[c][e], gr, inv) | (code_of((double)vf[c][4 + e], gr, inv) << 4));
-        if (c == g) vsm = gr.sm;
-    }
-    if (g < NG) {
-        reinterpret_cast<uint32_t*>(page + page4_ksm(DH))[sm_index(DH, tp, g)] = ksm;
-        reinterpret_cast<uint32_t*>(page + page4_vsm(DH))[sm_index(DH, tp, g)] = vsm;
+            vp[e * (DH / 8) + 4 * grp] = (uint8_t)(code_of((double)x[c][e], gr, inv) | (code_of((double)x[c][4 + e], gr, inv) << 4));
+        if (g == 0) reinterpret_cast<uint32_t*>(page + page4_vsm(DH))[sm_index(DH, tp, grp)] = gr.sm;
     }
 }
 
 int launch_kv4_append(const AppendArgs& a, int dh, int dtype, hipStream_t stream) {
-    const long threads = (long)a.B * a.R * 4 * (a.H + a.Hq);
-    const dim3 grid((unsigned)((threads + 255) / 256));
+    const long threads = (long)a.B * a.R * 4 * (dh / 64) * std::max(a.H, a.Hq);
+    const dim3 grid((unsigned)((threads + 255) / 256), a.Hq > 0 ? 3 : 2);
     auto go = [&](auto dhc) {
         constexpr int D = decltype(dhc)::value;
         if (dtype == DT_F16) hipLaunchKernelGGL((kv4_append_kernel<D, DT_F16>), grid, dim3(256), 0, stream, a);
@@ -209,7 +215,7 @@ int launch_kv4_append(const AppendArgs& a, int dh, int dtype, hipStream_t stream
 }
 
 // ------------------------------------------------------------------------------------------------
-// The values that cached tokens stand for. Four lanes per token and head, channels as in the kernel above.
+// The values that cached tokens stand for: threads as in the kernel above.
 struct ReadArgs {
     SeqList seqs;
     const int32_t* lens; const int32_t* block_table;
@@ -220,10 +226,11 @@ struct ReadArgs {
 
 template <int DH, int DT>
 __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
-    constexpr int NG = DH / 32;
+    constexpr int NG = DH / 32, SP = NG / 2;
     const long t = (long)blockIdx.x * 256 + threadIdx.x;
-    const int g = threadIdx.x & 3, h = (int)((t >> 2) % a.H);
-    const long row = (t >> 2) / a.H;
+    const int g = threadIdx.x & 3, half = threadIdx.x >> 2 & (SP - 1);
+    const long item = t / (4 * SP), row = item / a.H;
+    const int h = (int)(item % a.H);
     if (row >= (long)a.B * a.n) return;
     const int b = (int)(row / a.n), r = (int)(row % a.n);
     const int id = a.seqs.slot(b);
@@ -232,25 +239,31 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
     const int tp = slot % kPageSize;
     const int pg = a.block_table[(size_t)id * a.mpps + slot / kPageSize];
     const uint8_t* page = a.pages + ((size_t)pg * a.H + h) * page4_bytes(DH);
-    const uint32_t* kw = reinterpret_cast<const uint32_t*>(page + (g * 16 + tp) * (DH / 8));
-    const uint32_t* ksm = reinterpret_cast<const uint32_t*>(page + page4_ksm(DH)) + sm_index(DH, tp, 0);
-    const uint32_t* vsm = reinterpret_cast<const uint32_t*>(page + page4_vsm(DH)) + sm_index(DH, tp, 0);
+    if (blockIdx.y == 0) {                           // keys of groups 2 half (low) and 2 half + 1 (high)
+        const u32x2 w = *reinterpret_cast<const u32x2*>(page + (g * 16 + tp) * (DH / 8) + 8 * half);
+        const size_t ko = (size_t)b * a.k.seq + (size_t)r * a.k.row + (size_t)h * a.k.head + 64 * half + 8 * g;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const uint32_t sm = reinterpret_cast<const uint32_t*>(page + page4_ksm(DH))[sm_index(DH, tp, 2 * half + c)];
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = fmaf(sm_scale(sm), (float)((w[j >> 2] >> (8 * code_byte(j & 3) + 4 * c)) & 15u), sm_offset(sm));
+            store_elems<DT, 8>(a.k.p, ko + 32 * c, x);
+        }
+        return;
+    }
     const uint8_t* vp = page + page4_v(DH) + ((tp >> 2) * 16 + 4 * g) * (DH / 8) + code_byte(tp & 3);
-    const size_t ko = (size_t)b * a.k.seq + (size_t)r * a.k.row + (size_t)h * a.k.head + 8 * g;
-    const size_t vo = (size_t)b * a.v.seq + (size_t)r * a.v.row + (size_t)h * a.v.head + 4 * g;
+    const size_t vo = (size_t)b * a.v.seq + (size_t)r * a.v.row + (size_t)h * a.v.head + 64 * half + 4 * g;
 #pragma unroll
-    for (int c = 0; c < NG; ++c) {
-        const float ks = sm_scale(ksm[4 * c]), km = sm_offset(ksm[4 * c]), vs = sm_scale(vsm[4 * c]), vm = sm_offset(vsm[4 * c]);
-        float x[8], u[4], w[4];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = fmaf(ks, (float)((kw[(c & ~1) + (j >> 2)] >> (8 * code_byte(j & 3) + 4 * (c & 1))) & 15u), km);
+    for (int c = 0; c < 2; ++c) {
+        const uint32_t sm = reinterpret_cast<const uint32_t*>(page + page4_vsm(DH))[sm_index(DH, tp, 2 * half + c)];
+        float u[4], w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t byte = vp[e * (DH / 8) + 4 * c];
-            u[e] = fmaf(vs, (float)(byte & 15u), vm);
-            w[e] = fmaf(vs, (float)(byte >> 4), vm);
+            const uint32_t byte = vp[e * (DH / 8) + 4 * (2 * half + c)];
+            u[e] = fmaf(sm_scale(sm), (float)(byte & 15u), sm_offset(sm));
+            w[e] = fmaf(sm_scale(sm), (float)(byte >> 4), sm_offset(sm));
         }
-        store_elems<DT, 8>(a.k.p, ko + 32 * c, x);
         store_elems<DT, 4>(a.v.p, vo + 32 * c, u);
         store_elems<DT, 4>(a.v.p, vo + 32 * c + 16, w);
     }
@@ -464,7 +477,7 @@ extern "C" int laser_kv_read(laser_kv* h, int layer, const int32_t* seq_ids, int
         a.pages = layer_pages(kv, layer);
         a.k = heads_from(k, b0, dtype); a.v = heads_from(v, b0, dtype);
         a.n = n; a.H = kv->d.n_heads; a.mpps = kv->d.max_pages_per_seq; a.start = start;
-        const dim3 grid((unsigned)(((long)a.B * n * a.H * 4 + 255) / 256));
+        const dim3 grid((unsigned)(((long)a.B * n * a.H * 4 * (kv->d.head_dim / 64) + 255) / 256), 2);
         auto go = [&](auto dhc) {
             constexpr int D = decltype(dhc)::value;
             if (dtype == DT_F16) hipLaunchKernelGGL((kv4_read_kernel<D, DT_F16>), grid, dim3(256), 0, (hipStream_t)stream, a);
