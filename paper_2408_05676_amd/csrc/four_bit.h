@@ -167,7 +167,7 @@ struct AttendArgs {
     void* out_lo;                                    // not NULL: the result is two fp16 planes (see split_f16), this is the low one
     float* part;
     int B, R, H, G, mpps, nsplit, nt, J;             // G = query heads per key/value head; nt = tiles of J packed rows per key/value head
-    float scale_log2;
+    float scale_log2, inv_g;
 };
 int launch_kv4_append(const AppendArgs& a, int dh, int dtype, hipStream_t stream);
 int launch_kv4_attend(AttendArgs a, int dh, int dtype, int max_tokens, hipStream_t stream);

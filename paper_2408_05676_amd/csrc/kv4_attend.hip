@@ -54,6 +54,13 @@ __device__ inline void store_out(const AttendArgs& a, size_t o, const float (&x)
     }
 }
 
+// pi / G: packed rows are below 64 G, so the quotient is off by less than 2^-17, and never within 1 / (2 G) >= 2^-9 of a border
+__device__ inline int row_of(const AttendArgs& a, int pi) { return (int)(((float)pi + 0.5f) * a.inv_g); }
+__device__ inline size_t out_at(const AttendArgs& a, int b, int h, int pi) {
+    const int row = row_of(a, pi);
+    return (size_t)b * a.out.seq + (size_t)row * a.out.row + (size_t)(h * a.G + pi - row * a.G) * a.out.head;
+}
+
 // ---- a wave's ring of two pairs of pages in LDS, written by the loads themselves
 // A pair: the codes of both pages one after the other, then both pages' scales and offsets; requests of 1 KB, 16 bytes a lane.
 template <int DH>
@@ -81,6 +88,8 @@ struct Ring {
     __device__ static inline void have_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 };
 
+typedef const __attribute__((address_space(4))) int32_t* scalar_ints;       // (of arrays that no one writes while the kernel runs)
+
 template <int CG>
 __device__ inline float sum_over_groups(float x) {                   // over the CG lanes of a query row
     if constexpr (CG >= 2) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
@@ -106,7 +115,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4, j = r / CG, cc = r % CG;
     // (what the whole wave shares is kept in scalar registers: addresses, loop bounds and branches)
-    const int slot = __builtin_amdgcn_readfirstlane(a.seqs.slot(b)), len = __builtin_amdgcn_readfirstlane(a.lens[slot]), cap = a.seqs.tokens(b);
+    const int slot = __builtin_amdgcn_readfirstlane(a.seqs.slot(b)), len = ((scalar_ints)a.lens)[slot], cap = a.seqs.tokens(b);
     int nr = a.n_rows ? min(max(a.n_rows[b], 0), a.R) : a.R;
     nr = __builtin_amdgcn_readfirstlane(max(0, min(nr, cap - len)));      // (a length beyond the pages: rows that have no slot are left out)
     const int P = nr * a.G;                          // packed rows
@@ -118,7 +127,6 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     const int p0 = split * per, p1 = min(npages, p0 + per);
     const uint8_t* base = a.pages + (size_t)h * page4_bytes(DH);
     const size_t page_step = (size_t)a.H * page4_bytes(DH);
-    typedef const __attribute__((address_space(4))) int32_t* scalar_ints;       // (not written while the kernel runs)
     const scalar_ints bt = (scalar_ints)(a.block_table + (size_t)slot * a.mpps);
     auto page_at = [&](int p) { return base + (size_t)(unsigned)__builtin_amdgcn_readfirstlane(bt[min(p, p1 - 1)]) * page_step; };
     constexpr int kStep = 2 * kWaves;
@@ -148,7 +156,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     Frag8 q[NG], ql[NG];
     Frag8 qsum;                                  // CG = 1, operand of the offsets: first input 8 g is the sum of group g, in two parts
     constexpr float kUnit = CG == 1 ? kCodeUnit * kSumUnit : 1.f;         // of the keys' scales: scores come in units of kSumUnit, else 2^-24
-    const int pi = min(tile * J + j, P - 1), row = pi / a.G, hq = h * a.G + pi % a.G;
+    const int pi = min(tile * J + j, P - 1), row = row_of(a, pi), hq = h * a.G + pi - row * a.G;
     const unsigned anc_lo = __shfl((unsigned)anc_l, row), anc_hi = __shfl((unsigned)(anc_l >> 32), row);
     const unsigned long long anc = ((unsigned long long)anc_hi << 32) | anc_lo;
     const size_t qo = (size_t)b * a.q.seq + (size_t)row * a.q.row + (size_t)hq * a.q.head + 8 * g;
@@ -163,26 +171,23 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     int e = 0;
     if (mx > 0.f && mx < INFINITY) { (void)frexpf(mx, &e); e = min(max(15 - e, -80), 100); }
     const float up = ldexpf(a.scale_log2 < 0.f ? -1.f : a.scale_log2 > 0.f ? 1.f : 0.f, e);
+    Frag8 ones;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ones.w[i] = 0x3C003C00u;
     float own = 0.f;
 #pragma unroll
     for (int c = 0; c < NG; ++c) {
-        float s = 0.f, y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[c][i] *= c & 1 ? up * (1.f / 16.f) : up;
         q[c] = pack8(x[c]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = (float)q[c].v[i];
+        float4_t sum = mfma_16x16x32(ones, q[c], float4_t{0.f, 0.f, 0.f, 0.f});          // of the lane's query row
         if constexpr (kTwoQ) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[c][i] -= y[i];
+            for (int i = 0; i < 8; ++i) x[c][i] -= (float)q[c].v[i];
             ql[c] = pack8(x[c]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += (float)ql[c].v[i];
+            sum = mfma_16x16x32(ones, ql[c], sum);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += y[i];
-        s = sum_over_rows(s) * ((c & 1 ? 16.f : 1.f) * (CG == 1 ? kSumUnit : 1.f / kCodeUnit));
-        if (c == (CG == 1 ? g : cc)) own = s;
+        if (c == (CG == 1 ? g : cc)) own = sum[0] * ((c & 1 ? 16.f : 1.f) * (CG == 1 ? kSumUnit : 1.f / kCodeUnit));
         if (CG > 1 && c != cc) {
             q[c].v4 = u32x4{0, 0, 0, 0};
             if constexpr (kTwoQ) ql[c].v4 = u32x4{0, 0, 0, 0};
@@ -422,7 +427,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
                 const float inv = L == 0.f ? 0.f : 1.f / L;          // (nothing seen: 0; NaN stays)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[i] *= inv;
-                store_out<OUT>(a, (size_t)b * a.out.seq + (size_t)(pi / a.G) * a.out.row + (size_t)(h * a.G + pi % a.G) * a.out.head + c, o);
+                store_out<OUT>(a, out_at(a, b, h, pi) + c, o);
             }
         } else {
             float* part = a.part + ((((size_t)b * a.H + h) * a.nt + tile) * a.nsplit + split) * part_floats(DH);
@@ -495,7 +500,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttendArgs a) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] *= inv;
-    store_out<OUT>(a, (size_t)b * a.out.seq + (size_t)(pi / a.G) * a.out.row + (size_t)(h * a.G + pi % a.G) * a.out.head + 4 * c, x);
+    store_out<OUT>(a, out_at(a, b, h, pi) + 4 * c, x);
 }
 
 template <int DH, int IN, int OUT>
@@ -513,6 +518,7 @@ int launch_kv4_attend(AttendArgs a, int dh, int dtype, int max_tokens, hipStream
     // Up to 4 rows of a key/value head (8 at 64 channels) the columns of a tile are groups: 4 rows behind 65000 tokens 22.7 us (25.0 with rows
     // as columns), 1 row of 16 sequences behind 1024 18.1 (19.5); two such tiles for up to 8 rows 21.6 and one of 16 18.8 (8 rows, 4000 tokens).
     const int P = a.R * a.G, few = 16 * 32 / dh;
+    a.inv_g = 1.f / (float)a.G;
     a.J = P <= few ? few : 16;
     a.nt = (P + a.J - 1) / a.J;
     // Split the context for two workgroups on every compute unit, as long as each wave has a pair of pages.
