@@ -311,6 +311,16 @@ int laser_w4_quantize(const uint16_t* w, int N, int Kd, int group, uint8_t* code
  * streams may share a handle. Made for few rows (every weight is read once up to 80 rows, again for every 80 further ones). */
 int laser_w4_matmul(const laser_w4* w, const void* x, int64_t x_stride, int M, int dtype, void* out, int64_t out_stride, void* stream);
 
+/* laser_model_set_w4: from the next call on, steps of the model multiply with `w` instead of the bf16 matrix `which` of the layer (NULL: with the
+ * bf16 matrix again); shapes as in laser_model_desc. The handle is borrowed and must live while the model (or a graph captured from its
+ * steps) may use it. Steps of a model with any such matrix take the general path, rows enter these products as single fp16 values, and
+ * a model whose projections are all set makes no fp16 copies of them. */
+#define LASER_W_QKV  0
+#define LASER_W_O    1
+#define LASER_W_GU   2
+#define LASER_W_DOWN 3
+int laser_model_set_w4(laser_model* model, int layer, int which, const laser_w4* w);
+
 /* laser_verify_step (Eq. 3 / Eq. 6 forward, Eq. 4 / 7 / 8 acceptance, correction rule of Sec. 2.1).
  * For sequence b, rows r = 0..K hold the tokens [pending[b], drafts[b][0..K-1]] at positions
  * len+r; their keys/values go to cache slots len..len+K; row r attends to slots 0..len+r. The

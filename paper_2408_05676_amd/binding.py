@@ -80,6 +80,7 @@ def lib():
         "laser_kv_read": [vp, i32, vp, i32, i32, i32, i32, C.POINTER(_Heads), C.POINTER(_Heads), vp],
         "laser_w4_create": [vp, vp, vp, i32, i32, i32, vp, C.POINTER(vp)],
         "laser_w4_destroy": [vp],
+        "laser_model_set_w4": [vp, i32, i32, vp],
         "laser_w4_quantize": [vp, i32, i32, i32, vp, vp, vp, vp],
         "laser_w4_matmul": [vp, vp, i64, i32, i32, vp, i64, vp],
         "laser_kv_destroy": [vp],
@@ -260,6 +261,12 @@ class Model:
 
     def set_option(self, name: str, value: int):
         _check(lib().laser_model_set_option(self._h, name.encode(), value), "laser_model_set_option")
+
+    def set_w4(self, layer: int, name: str, w4) -> None:
+        """laser_model_set_w4: name is wqkv, wo, wgu or wdown, w4 a W4 (kept alive by this object) or None."""
+        which = ("wqkv", "wo", "wgu", "wdown").index(name)
+        _check(lib().laser_model_set_w4(self._h, layer, which, w4._h if w4 is not None else None), "laser_model_set_w4")
+        self._keep[layer, which] = w4
 
     def aborted(self, stream=None) -> bool:
         v = C.c_int()

@@ -174,4 +174,9 @@ int launch_kv4_attend(AttendArgs a, int dh, int dtype, int max_tokens, hipStream
 int launch_kv4_compact(const KV* kv, const int32_t* ids_dev, const int32_t* accept_len, const int32_t* accept_path, int B, int K, hipStream_t stream);
 size_t kv4_part_floats(int dh);
 
+// ---- products with 4-bit weights (w4.hip) ----------------------------------------------------------
+struct W4 { int N, Kd, group, nkb; uint8_t* blocks; };
+enum { W4_STORE, W4_F32, W4_ADD_F32, W4_SWIGLU };    // results in the rows' type; as fp32; added to fp32; fp16 silu(gate) up, W's rows being gate | up
+int launch_w4(const W4* w, const void* x, int64_t x_stride, int M, int dtype, int epi, void* out, int64_t out_stride, hipStream_t stream);
+
 }  // namespace laser

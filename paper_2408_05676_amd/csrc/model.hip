@@ -778,6 +778,8 @@ static void copies_for_few_rows(Model* m, hipStream_t stream) {
     if (m->no_few_copies) (void)hipGetLastError();
 }
 
+static const W4* w4_of(const Model* m, int layer, int which) { return m->w4.empty() ? nullptr : (const W4*)m->w4[4 * layer + which]; }
+
 // A layer's rotary positions, cache write and attention on a 4-bit cache. The qkv rows (the sums of n_part arrays, see RopeArgs) go in as
 // fp32; rotated queries replace the first array's and are read back by the attention, whose result is split into two planes.
 static int four_bit_attention(Model* m, KV* kv, const int32_t* ids_dev, const RopeArgs& ra, int layer, int B, int R, int max_tokens, hipStream_t stream) {
@@ -821,7 +823,8 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
                        m->row_pos, m->row_slot, m->row_anc);
     hipLaunchKernelGGL(embed_rmsnorm_kernel, dim3(M), dim3(256), 0, stream, d.emb, d.g1, pending, drafts, draft_len,
                        R, dm, d.vocab, d.eps, m->x, m->xn, m->xn_lo);
-    if (M > kSkinnyMaxRows && m->f16_copies && !m->w16[0]) {
+    const bool all_w4 = m->w4_set == 4 * d.n_layers;                // then no projection is read as bf16, and none is copied
+    if (M > kSkinnyMaxRows && m->f16_copies && !m->w16[0] && !all_w4) {
         if (const int rc = widen_copies(m, kProjections, stream)) return rc;
     }
     if (M > 16 && !m->kpart) {
@@ -857,7 +860,10 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
         const bool many = M > 16 && m->w16[0];      // tiled path: weights from the fp16 copy (if kept)
         GemmArgs g{d.wqkv + (size_t)l * 3 * dm * dm, many ? m->w16[0] + (size_t)l * 3 * dm * dm : nullptr, m->xn, m->xn_lo, M, 3 * dm, dm, 1, m->qkv, nullptr};
         g.part = m->kpart; g.part_floats = m->kpart_floats; g.want_split = m->ksplit_opt[0]; g.mid_waves = m->mid_waves; g.want_tile = m->tile;
-        if ((rc = launch_gemm<EPI_F32>(g, stream))) return rc;
+        if (const W4* w = w4_of(m, l, 0)) {
+            g.n_part = 0;
+            if ((rc = launch_w4(w, m->xn, dm, M, LASER_F16, W4_F32, m->qkv, 3 * dm, stream))) return rc;
+        } else if ((rc = launch_gemm<EPI_F32>(g, stream))) return rc;
         RopeArgs ra{g.n_part ? m->kpart : m->qkv, m->row_pos, m->row_slot, ids_dev, kv->block_table, m->rope, m->q, m->q_lo, kv->kpages, kv->klpages, kv->vpages,
                     R, dm, d.n_heads, m->dh, kv->d.max_pages_per_seq, l, kv->d.n_pages,
                     M, std::max(1, std::min(4, dm / 2048)), B, std::max(1, g.n_part), (size_t)M * 3 * dm};
@@ -894,7 +900,10 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
         }
         GemmArgs go{d.wo + (size_t)l * dm * dm, many ? m->w16[1] + (size_t)l * dm * dm : nullptr, m->attn, m->attn_lo, M, dm, dm, 1, m->x, nullptr};
         go.part = m->kpart; go.part_floats = m->kpart_floats; go.want_split = m->ksplit_opt[1]; go.mid_waves = m->mid_waves; go.want_tile = m->tile;
-        if ((rc = launch_gemm<EPI_RESID>(go, stream))) return rc;
+        if (const W4* w = w4_of(m, l, 1)) {
+            go.n_part = 0;
+            if ((rc = launch_w4(w, m->attn, dm, M, LASER_F16, W4_ADD_F32, m->x, dm, stream))) return rc;
+        } else if ((rc = launch_gemm<EPI_RESID>(go, stream))) return rc;
         launch_rmsnorm(M, stream, m->x, d.g2 + (size_t)l * dm, dm, d.eps, m->xn, m->xn_lo, (const float*)m->kpart, go.n_part, (size_t)M * dm);
         // On the tiled many-row path a split operand doubles the matrix work; gate/up (45 % of the layer's
         // flops) takes the single fp16 rows there unless option "split_ffn" asks for the split (see set_option).
@@ -903,11 +912,16 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
         gg.mid_waves = m->mid_waves; gg.want_tile = m->tile;
         const bool prof = m->prof_on && m->prof_n < m->prof_cap;
         if (prof) LASER_HIP_CHECK(hipEventRecord(m->prof_ev[2 * m->prof_n], stream));
-        if ((rc = launch_gemm<EPI_SWIGLU>(gg, stream))) return rc;
+        if (const W4* w = w4_of(m, l, 2)) {
+            if ((rc = launch_w4(w, m->xn, dm, M, LASER_F16, W4_SWIGLU, m->act, F, stream))) return rc;
+        } else if ((rc = launch_gemm<EPI_SWIGLU>(gg, stream))) return rc;
         if (prof) { LASER_HIP_CHECK(hipEventRecord(m->prof_ev[2 * m->prof_n + 1], stream)); ++m->prof_n; }
         GemmArgs gd{d.wdown + (size_t)l * dm * F, many ? m->w16[3] + (size_t)l * dm * F : nullptr, m->act, nullptr, M, dm, F, 1, m->x, nullptr};
         gd.part = m->kpart; gd.part_floats = m->kpart_floats; gd.want_split = m->ksplit_opt[2]; gd.mid_waves = m->mid_waves; gd.want_tile = m->tile;
-        if ((rc = launch_gemm<EPI_RESID>(gd, stream))) return rc;
+        if (const W4* w = w4_of(m, l, 3)) {
+            gd.n_part = 0;
+            if ((rc = launch_w4(w, m->act, F, M, LASER_F16, W4_ADD_F32, m->x, dm, stream))) return rc;
+        } else if ((rc = launch_gemm<EPI_RESID>(gd, stream))) return rc;
         pend = gd.n_part;        // added to the residual by the next norm (next layer's, or the final one)
     }
     launch_rmsnorm(M, stream, m->x, d.gf, dm, d.eps, m->xn, nullptr, (const float*)m->kpart, pend, (size_t)M * dm);
@@ -1045,8 +1059,8 @@ static int verify_impl(laser_model* mh, laser_kv* kh, const int32_t* seq_ids, co
     }
     const int32_t* ids_dev = nullptr;
     if ((rc = kv->stage_ids(seq_ids, B, stream, &ids_dev))) return rc;
-    const bool fused = m->use_fused && !kv->pages4 && fused_supported(m, B, K, max_ub);
-    if (fused || (B * R > 16 && B * R <= kSkinnyMaxRows)) copies_for_few_rows(m, stream);
+    const bool fused = m->use_fused && !kv->pages4 && m->w4_set == 0 && fused_supported(m, B, K, max_ub);
+    if (fused || (B * R > 16 && B * R <= kSkinnyMaxRows && m->w4_set < 4 * m->d.n_layers)) copies_for_few_rows(m, stream);
     if (fused) {
         if (parent)          // token tree: positions (depth) and ancestor masks of the rows
             hipLaunchKernelGGL(rows_kernel, dim3((B * R + 255) / 256), dim3(256), 0, stream, parent, draft_len, ids_dev, kv->len, B, R,
@@ -1172,6 +1186,22 @@ extern "C" int laser_model_set_option(laser_model* mh, const char* name, int val
         }
     set_error("unknown option %s", name);
     return LASER_E_INVALID_ARG;
+}
+
+extern "C" int laser_model_set_w4(laser_model* mh, int layer, int which, const laser_w4* wh) {
+    Model* m = reinterpret_cast<Model*>(mh);
+    const W4* w = reinterpret_cast<const W4*>(wh);
+    LASER_REQUIRE(m != nullptr, LASER_E_INVALID_ARG, "model is NULL");
+    LASER_REQUIRE(layer >= 0 && layer < m->d.n_layers, LASER_E_INVALID_ARG, "layer %d out of range", layer);
+    LASER_REQUIRE(which >= 0 && which <= 3, LASER_E_INVALID_ARG, "matrix %d: LASER_W_QKV, LASER_W_O, LASER_W_GU or LASER_W_DOWN", which);
+    const int dm = m->d.d_model, F = m->d.ffn;
+    const int N = which == 0 ? 3 * dm : which == 2 ? 2 * F : dm, Kd = which == 3 ? F : dm;
+    LASER_REQUIRE(!w || (w->N == N && w->Kd == Kd), LASER_E_SHAPE, "the matrix is [%d][%d], not [%d][%d]", w ? w->N : 0, w ? w->Kd : 0, N, Kd);
+    if (m->w4.empty()) m->w4.assign((size_t)4 * m->d.n_layers, nullptr);
+    const void*& at = m->w4[4 * (size_t)layer + which];
+    m->w4_set += (w != nullptr) - (at != nullptr);
+    at = w;
+    return LASER_OK;
 }
 
 extern "C" int laser_model_status(laser_model* mh, void* stream, int* aborted) {

@@ -105,6 +105,8 @@ struct Model {
                                        // until the handle is destroyed: a captured graph holds its address
     bool no_few_copies = false;        // they could not be made for a step of up to 80 rows, which does without
     int f16_copies = 1;                // 0: the tiled kernels stream the bf16 weights and widen them in the loop (no copies)
+    std::vector<const void*> w4;       // laser_model_set_w4: 4-bit matrices instead of wqkv, wo, wgu, wdown, four a layer; NULL: none. Empty: never set
+    int w4_set = 0;                    // how many of them are not NULL
     float* kpart = nullptr;            // partial results of reduction-split tiled GEMMs (many-row path), [parts][rows][N]
     size_t kpart_floats = 0;
     int ksplit_opt[3] = {0, 0, 0};     // forced reduction parts for QKV, O, down (0 = choose from the tile count)

@@ -14,8 +14,6 @@
 
 namespace laser {
 
-struct W4 { int N, Kd, group, nkb; uint8_t* blocks; };
-
 constexpr int block_bytes(int ng) { return 1024 + 64 * ng; }      // ng = groups of a block
 
 // ------------------------------------------------------------------------------------------------
@@ -67,9 +65,10 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const uint16_t* w, siz
 // ------------------------------------------------------------------------------------------------
 struct W4Args {
     const uint8_t* blocks;
-    const uint16_t* x; uint16_t* out;
+    const uint16_t* x; void* out;
     int64_t x_stride, out_stride;
-    int M, N, Kd, nkb, tiles;
+    int M, N, Kd, nkb, tiles;                                      // W4_SWIGLU: N and tiles of a half
+    int epi, up_tile;                                              // the first tile of the up half, W4_SWIGLU only
 };
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -88,11 +87,13 @@ __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
     constexpr int CPG = 4 / NG;                                    // pieces of a group
     extern __shared__ float lds[];                                 // [WK / 2][NT][MT][16 rows][16 outputs]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int tile0 = blockIdx.x * NT, row0 = blockIdx.y * (MT * 16);
+    // A wave's tiles side by side; W4_SWIGLU: half of them gate, the other half their up tiles (NT is even then).
+    const bool swiglu = NT > 1 && a.epi == W4_SWIGLU;
+    const int own = swiglu ? NT / 2 : NT, tile0 = blockIdx.x * own, row0 = blockIdx.y * (MT * 16);
     const int k0 = (int)((long)a.nkb * wave / WK), k1 = (int)((long)a.nkb * (wave + 1) / WK);
     const uint8_t* wp[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) wp[n] = a.blocks + (size_t)min(tile0 + n, a.tiles - 1) * a.nkb * block_bytes(NG);
+    for (int n = 0; n < NT; ++n) wp[n] = a.blocks + (size_t)(n < own ? min(tile0 + n, a.tiles - 1) : a.up_tile + min(tile0 + n - own, a.tiles - 1)) * a.nkb * block_bytes(NG);
     const uint16_t* xp[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) xp[m] = a.x + (size_t)min(row0 + m * 16 + (SWAP ? lane >> 2 : r), a.M - 1) * a.x_stride + 8 * (SWAP ? lane & 3 : g);
@@ -210,20 +211,30 @@ __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) *place(wave, n, m) = acc[n][m] + *place(wave, n, m);
     __syncthreads();
-    for (int idx = threadIdx.x; idx < NT * MT * 256; idx += WK * 64) {
-        const int o = idx & 15, n = idx >> 4 & (NT - 1), row = idx / (16 * NT);        // outputs of a row side by side
-        const int at = (n * MT + (row >> 4)) * 256 + (row & 15) * 16 + o;
+    auto sum = [&](int at) {
         float v = lds[at];
 #pragma unroll
         for (int w = 1; w < WK / 2; ++w) v += lds[w * NT * MT * 256 + at];
+        return v;
+    };
+    for (int idx = threadIdx.x; idx < own * MT * 256; idx += WK * 64) {
+        const int o = idx & 15, n = idx >> 4 & (own - 1), row = idx / (16 * own);      // outputs of a row side by side
+        const int at = (n * MT + (row >> 4)) * 256 + (row & 15) * 16 + o;
         const int gr = row0 + row, gn = (tile0 + n) * 16 + o;
-        if (gr < a.M && gn < a.N) a.out[(size_t)gr * a.out_stride + gn] = BF ? f32_to_bf16(v) : f32_to_f16(v);
+        if (gr >= a.M || gn >= a.N) continue;
+        const float v = sum(at);
+        const size_t to = (size_t)gr * a.out_stride + gn;
+        if (a.epi == W4_STORE) ((uint16_t*)a.out)[to] = BF ? f32_to_bf16(v) : f32_to_f16(v);
+        else if (a.epi == W4_F32) ((float*)a.out)[to] = v;
+        else if (a.epi == W4_ADD_F32) ((float*)a.out)[to] += v;
+        else if (swiglu) ((uint16_t*)a.out)[to] = f32_to_f16(v / (1.f + __expf(-v)) * sum(at + own * MT * 256));
     }
 }
 
 template <bool BF, int NG, bool SWAP, int MT, int NT, int WK>
-static void launch_w4(const W4Args& a, hipStream_t stream) {
-    const dim3 grid((unsigned)((a.tiles + NT - 1) / NT), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
+static void launch_kernel(const W4Args& a, hipStream_t stream) {
+    const int own = a.epi == W4_SWIGLU ? NT / 2 : NT;
+    const dim3 grid((unsigned)((a.tiles + own - 1) / own), (unsigned)((a.M + MT * 16 - 1) / (MT * 16)));
     hipLaunchKernelGGL((w4_matmul_kernel<BF, NG, SWAP, MT, NT, WK>), grid, dim3(WK * 64), WK / 2 * NT * MT * 1024, stream, a);
 }
 
@@ -233,13 +244,28 @@ static void launch_w4(const W4Args& a, hipStream_t stream) {
 //   2048 -> 6144 15.9 / 10.2. And where one tile is taken, with two: 1 row 4096 -> 4096 4.3 / 5.2, 72 rows 11008 -> 4096 28.1 / 29.9.
 template <bool BF, int NG>
 static void launch_rows(const W4Args& a, hipStream_t stream) {
-    const int mt = std::min(5, (a.M + 15) / 16);
-    if (a.M <= 4) a.tiles >= 1024 ? launch_w4<BF, NG, false, 1, 2, 4>(a, stream) : launch_w4<BF, NG, false, 1, 1, 8>(a, stream);
-    else if (mt == 1) a.tiles >= 1024 ? launch_w4<BF, NG, true, 1, 2, 4>(a, stream) : launch_w4<BF, NG, true, 1, 1, 8>(a, stream);
-    else if (mt == 2) a.tiles >= 512 ? launch_w4<BF, NG, true, 2, 4, 8>(a, stream) : launch_w4<BF, NG, true, 2, 1, 8>(a, stream);
-    else if (mt == 3) a.tiles >= 512 ? launch_w4<BF, NG, true, 3, 4, 8>(a, stream) : launch_w4<BF, NG, true, 3, 1, 8>(a, stream);
-    else if (mt == 4) a.tiles >= 320 ? launch_w4<BF, NG, true, 4, 2, 8>(a, stream) : launch_w4<BF, NG, true, 4, 1, 8>(a, stream);
-    else a.tiles >= 320 ? launch_w4<BF, NG, true, 5, 2, 8>(a, stream) : launch_w4<BF, NG, true, 5, 1, 8>(a, stream);
+    const int mt = std::min(5, (a.M + 15) / 16), tiles = a.epi == W4_SWIGLU ? 1 << 20 : a.tiles;      // (gate and up tiles share a wave)
+    if (a.M <= 4) tiles >= 1024 ? launch_kernel<BF, NG, false, 1, 2, 4>(a, stream) : launch_kernel<BF, NG, false, 1, 1, 8>(a, stream);
+    else if (mt == 1) tiles >= 1024 ? launch_kernel<BF, NG, true, 1, 2, 4>(a, stream) : launch_kernel<BF, NG, true, 1, 1, 8>(a, stream);
+    else if (mt == 2) tiles >= 512 ? launch_kernel<BF, NG, true, 2, 4, 8>(a, stream) : launch_kernel<BF, NG, true, 2, 1, 8>(a, stream);
+    else if (mt == 3) tiles >= 512 ? launch_kernel<BF, NG, true, 3, 4, 8>(a, stream) : launch_kernel<BF, NG, true, 3, 1, 8>(a, stream);
+    else if (mt == 4) tiles >= 320 ? launch_kernel<BF, NG, true, 4, 2, 8>(a, stream) : launch_kernel<BF, NG, true, 4, 1, 8>(a, stream);
+    else tiles >= 320 ? launch_kernel<BF, NG, true, 5, 2, 8>(a, stream) : launch_kernel<BF, NG, true, 5, 1, 8>(a, stream);
+}
+
+int launch_w4(const W4* w, const void* x, int64_t x_stride, int M, int dtype, int epi, void* out, int64_t out_stride, hipStream_t stream) {
+    const int N = epi == W4_SWIGLU ? w->N / 2 : w->N;
+    const W4Args a{w->blocks, (const uint16_t*)x, out, x_stride, out_stride, M, N, w->Kd, w->nkb, (N + 15) / 16, epi, N / 16};
+    auto go = [&](auto bf) {
+        constexpr bool BF = decltype(bf)::value;
+        if (w->group == 128) launch_rows<BF, 1>(a, stream);
+        else if (w->group == 64) launch_rows<BF, 2>(a, stream);
+        else launch_rows<BF, 4>(a, stream);
+    };
+    if (dtype == LASER_BF16) go(std::true_type{});
+    else go(std::false_type{});
+    LASER_HIP_CHECK(hipGetLastError());
+    return LASER_OK;
 }
 
 }  // namespace laser
@@ -300,15 +326,5 @@ extern "C" int laser_w4_matmul(const laser_w4* h, const void* x, int64_t x_strid
     if (M == 0) return LASER_OK;
     LASER_REQUIRE(x && out, LASER_E_INVALID_ARG, "NULL argument");
     LASER_REQUIRE((uintptr_t)x % 2 == 0 && (uintptr_t)out % 2 == 0, LASER_E_INVALID_ARG, "x or out is not aligned to its elements");
-    const W4Args a{w->blocks, (const uint16_t*)x, (uint16_t*)out, x_stride, out_stride, M, w->N, w->Kd, w->nkb, (w->N + 15) / 16};
-    auto go = [&](auto bf) {
-        constexpr bool BF = decltype(bf)::value;
-        if (w->group == 128) launch_rows<BF, 1>(a, (hipStream_t)stream);
-        else if (w->group == 64) launch_rows<BF, 2>(a, (hipStream_t)stream);
-        else launch_rows<BF, 4>(a, (hipStream_t)stream);
-    };
-    if (dtype == LASER_BF16) go(std::true_type{});
-    else go(std::false_type{});
-    LASER_HIP_CHECK(hipGetLastError());
-    return LASER_OK;
+    return launch_w4(w, x, x_stride, M, dtype, W4_STORE, out, out_stride, (hipStream_t)stream);
 }

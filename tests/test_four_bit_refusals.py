@@ -58,6 +58,7 @@ def test_null_and_misaligned_arguments(lib):
     assert lib.laser_w4_create(p, C.c_void_p(65), p, 16, 128, 32, None, C.byref(out)) == E_ARG
     assert lib.laser_w4_matmul(None, p, C.c_int64(128), 1, 0, p, C.c_int64(16), None) == E_ARG
     assert lib.laser_w4_destroy(None) == 0
+    assert lib.laser_model_set_w4(None, 0, 0, None) == E_ARG
     assert lib.laser_rope_table(None, 4, 64, C.c_double(1e4), None) == E_ARG
     for size, dim, base in ((0, 64, 1e4), (4, 63, 1e4), (4, 0, 1e4), (4, 64, 0.0)):
         assert lib.laser_rope_table(p, size, dim, C.c_double(base), None) == E_ARG

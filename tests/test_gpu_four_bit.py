@@ -476,9 +476,9 @@ def test_product_refusals():
 
 
 # ------------------------------------------------------------------------------------------------ the model on a 4-bit cache
-def reference_step(w, sh, kv, lens, tokens, parent):
+def reference_step(w, sh, kv, lens, tokens, parent, stored=True):
     """Logits [B][R][V] of a step in 64 bits, with the keys and values that the cache holds after it, and the largest distance of these from
-    the step's own keys and values, in steps of their group's codes."""
+    the step's own keys and values, in steps of their group's codes. stored False: with the step's own keys and values as they are."""
     L, d, H, dh = sh.n_layers, sh.d, sh.n_heads, sh.head_dim
     B, R = tokens.shape
     f = {n: t.double() for n, t in w.items()}
@@ -495,6 +495,9 @@ def reference_step(w, sh, kv, lens, tokens, parent):
             q, k, v = qkv[b].view(R, 3, H, dh).unbind(1)
             q, k = ref.rotate(q, table, dh, pos), ref.rotate(k, table, dh, pos)
             ck, cv = laser.kv_read(kv, layer, [b], lens[b] + R, start=0, dtype=F32)
+            if not stored:
+                ck, cv = ck.double(), cv.double()
+                ck[0, lens[b]:], cv[0, lens[b]:] = k, v
             for own, have in ((k, ck[0, lens[b]:].double()), (v, cv[0, lens[b]:].double())):
                 span = own.unflatten(-1, (-1, 32))
                 span = (span.amax(-1) - span.amin(-1)).repeat_interleave(32, -1) / 15
@@ -537,6 +540,66 @@ def test_model_steps_on_a_four_bit_cache(B, K, tree):
     assert worst <= 0.5 + 3 * 15 * 2.0 ** -11, worst
     laser.kv_commit_tree(kv, range(B), acc, path) if tree else laser.kv_commit(kv, range(B), acc)
     assert kv.read_lens(range(B)).tolist() == [t + int(a) + 1 for t, a in zip(lens, acc.tolist())]
+
+
+@pytest.mark.parametrize("B, K, tree, four_bit_cache, which", [
+    (2, 4, False, True, "wqkv wo wgu wdown"), (1, 0, False, False, "wqkv wo wgu wdown"), (4, 10, True, True, "wqkv wo wgu wdown"),
+    (3, 40, False, False, "wqkv wo wgu wdown"), (2, 7, False, False, "wgu"), (5, 7, True, False, "wo wdown"), (2, 2, False, True, "wqkv")])
+def test_model_steps_with_four_bit_weights(B, K, tree, four_bit_cache, which):
+    import synth
+    from tests.gpu_util import gpu_weights, logits_close
+    sh = synth.SHAPES["tiny"]
+    w = gpu_weights(sh)
+    lens = [20 + 9 * b for b in range(B)]
+    R = K + 1
+    model = laser.Model(sh.n_layers, sh.d, sh.n_heads, sh.ffn, sh.vocab, w, B * R, B, 512, eps=sh.eps, rope_base=sh.rope_base)
+    what = dict(w)
+    groups = dict(wqkv=32, wo=64, wgu=128, wdown=128)
+    for name in which.split():
+        what[name] = torch.empty(w[name].shape, dtype=torch.float64, device="cuda")
+        for layer in range(sh.n_layers):
+            codes, s, m = laser.w4_quantize(w[name][layer].contiguous(), groups[name])
+            model.set_w4(layer, name, laser.W4(codes, s, m))
+            what[name][layer] = ref.values(torch.stack([codes & 15, codes >> 4], -1).flatten(1).double(), s, m)
+    g = gen(40 + K)
+    # the reference takes its cache contents from laser_kv_read: a 4-bit copy of a plain cache's imports would differ, so these are what
+    # a 4-bit cache stands for in both
+    kv = make_kv(B, sh.n_heads, sh.head_dim, lens, 2 * R, layers=sh.n_layers)
+    plain = laser.KVCache(sh.n_layers, sh.n_heads, sh.head_dim, 200, B, 40)
+    for b in range(B):
+        plain.reserve(b, lens[b] + 2 * R)
+        plain.set_len(b, lens[b])
+    for layer in range(sh.n_layers):
+        fill(kv, lens, sh.n_heads, sh.head_dim, g, layer)
+        for b in range(B):
+            k, v = laser.kv_read(kv, layer, [b], lens[b], start=0)
+            plain.import_layer(b, layer, k[0], v[0])
+    r = np.random.default_rng(K)
+    tokens = torch.tensor(r.integers(0, sh.vocab, (B, R)), dtype=torch.int32, device="cuda")
+    n = torch.full((B,), K, dtype=torch.int32, device="cuda")
+    drafts = tokens[:, 1:].contiguous()
+    parent = torch.tensor([[int(r.integers(-1, i)) if i else -1 for i in range(K)] for _ in range(B)], dtype=torch.int32, device="cuda") if tree else None
+    use = kv if four_bit_cache else plain
+
+    def step():
+        if tree:
+            return laser.verify_tree(model, use, range(B), tokens[:, 0].contiguous(), drafts, parent, n, 2, 0.1, 0, want_logits=True)[-1]
+        return laser.verify_step(model, use, range(B), tokens[:, 0].contiguous(), drafts, n, 2, 0.1, 0, want_logits=True)[-1]
+    logits = step()
+    want = reference_step(what, sh, kv, lens, tokens, parent, stored=four_bit_cache)[0]
+    ok, err, rel = logits_close(logits.cpu().double().numpy(), want.cpu().numpy())
+    assert ok, (err, rel)
+    for name in which.split():                                   # and back
+        for layer in range(sh.n_layers):
+            model.set_w4(layer, name, None)
+    want = reference_step(w, sh, kv, lens, tokens, parent, stored=False)[0]
+    if not four_bit_cache:
+        ok, err, rel = logits_close(step().cpu().double().numpy(), want.cpu().numpy())
+        assert ok, (err, rel)
+    with pytest.raises(laser.LaserError, match="not"):
+        model.set_w4(0, "wo", laser.W4(*laser.w4_quantize(w["wqkv"][0].contiguous(), 128)))
+    with pytest.raises(laser.LaserError, match="layer"):
+        model.set_w4(sh.n_layers, "wo", None)
 
 
 def test_generation_on_a_four_bit_cache():
