@@ -17,7 +17,8 @@
  *     nothing accepted) are results, not errors.
  *   - Token ids are int32 >= 0; -1 pads. bf16 / fp16 = bfloat16 / IEEE half bit patterns in uint16.
  *   - Numerics: weights bf16 as given; activations that feed matrix products and the KV cache are
- *     fp16; accumulation, softmax, norms and the residual stream are fp32.
+ *     fp16; accumulation, softmax, norms and the residual stream are fp32. Weights and caches may be held in four bits instead
+ *     (laser_w4_create, laser_kv_create_4bit).
  *   - A handle must not be used from two streams or two host threads at the same time (the model
  *     handle owns activation workspace, the KV handle owns host-side page bookkeeping).
  */
@@ -232,7 +233,7 @@ int laser_kv_seq_reserve(laser_kv* kv, int seq, int n_tokens, void* stream);
 /* Return the slot's pages to the pool and set its length to 0. */
 int laser_kv_seq_release(laser_kv* kv, int seq, void* stream);
 /* Load externally produced keys/values (already rotated) for tokens [0, n_tokens) of one layer:
- * k, v [dev] fp16 [n_tokens][n_heads][head_dim]. Needs reserved capacity; does not change `len`. */
+ * k, v [dev] fp16 [n_tokens][n_heads][head_dim] (a 4-bit cache quantises them). Needs reserved capacity; does not change `len`. */
 int laser_kv_import(laser_kv* kv, int seq, int layer, const uint16_t* k, const uint16_t* v,
                     int n_tokens, void* stream);
 /* Set the committed length of a slot (after laser_kv_import, or to roll back). */
@@ -273,7 +274,8 @@ int laser_rope_table(float* table, int max_pos, int rope_dim, double base, void*
  *   n_rows      [dev]  int32[B] or NULL (R each): rows a sequence has, cut to 0..R; nothing is read or written for the others
  *   tree_parent [dev]  int32[B][R-1] or NULL (chains): as for laser_verify_tree
  *   R           1..LASER_MAX_DRAFT + 1
- *   k, v        key/value heads of the cache; q, q_out: n_heads query heads, rotated into q_out (which may be q); n_heads 0: none
+ *   k, v        key/value heads of the cache; q, q_out: n_heads query heads, rotated into q_out (q itself, or memory that overlaps none of
+ *               the inputs); n_heads 0: none
  *   rope        [dev] float[max_pos][rope_dim / 2][2] (laser_rope_table), 8-byte aligned; channel i < rope_dim / 2 is paired with i + rope_dim / 2,
  *               channels from rope_dim on are not rotated. rope_dim: 0 (no rotation), head_dim, or 64 of 128. Positions must stay below
  *               max_pos (checked against the host's bound of len, LASER_E_LIMIT; a replayed graph's are cut to it).
@@ -286,7 +288,7 @@ int laser_kv_append(laser_kv* kv, int layer, const int32_t* seq_ids, const int32
 /* laser_kv_attend: out = softmax(scale q . k) v of a step's rows over a 4-bit cache: row r of sequence b attends to the committed
  * slots 0..len-1 and, of its own step's slots len..len+R-1 (laser_kv_append), to itself and its ancestors (tree_parent; NULL: rows 0..r).
  * n_heads query heads, a multiple of the cache's: query head j uses key/value head j / (n_heads / cache heads).
- * Other arguments as for laser_kv_append; rows beyond n_rows are left as they are. out has q's type and may be q. Sums, softmax and
+ * Other arguments as for laser_kv_append; rows beyond n_rows are left as they are. out has q's type and is q itself or memory that does not overlap it. Sums, softmax and
  * scores are fp32. Contexts are split over workgroups by the host's bounds of len: results may differ in the last bits between launches
  * whose bounds differ, and are the same for the same ones. Uses the handle's workspace. */
 int laser_kv_attend(laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* n_rows, const int32_t* tree_parent, int B, int R,
@@ -307,8 +309,9 @@ int laser_w4_create(const uint8_t* codes, const uint16_t* scales, const uint16_t
 int laser_w4_destroy(laser_w4* w);
 int laser_w4_quantize(const uint16_t* w, int N, int Kd, int group, uint8_t* codes, uint16_t* scales, uint16_t* offsets, void* stream);
 /* laser_w4_matmul: out[r][n] = sum over i of x[r][i] W[n][i] for M rows; x and out in `dtype` (LASER_F16 or LASER_BF16), rows
- * x_stride >= Kd and out_stride >= N elements apart, aligned to their elements. fp32 sums. Keeps no workspace: calls on several
- * streams may share a handle. Made for few rows (every weight is read once up to 80 rows, again for every 80 further ones). */
+ * x_stride >= Kd and out_stride >= N elements apart, aligned to their elements; out must not overlap x. fp32 sums; a row of x that is not
+ * finite gives results that are not. Keeps no workspace: calls on several streams may share a handle. Made for few rows (every weight is read once
+ * up to 80 rows, again for every 80 further ones). */
 int laser_w4_matmul(const laser_w4* w, const void* x, int64_t x_stride, int M, int dtype, void* out, int64_t out_stride, void* stream);
 
 /* laser_model_set_w4: from the next call on, steps of the model multiply with `w` instead of the bf16 matrix `which` of the layer (NULL: with the

@@ -10,7 +10,13 @@
 //   values   O[row][ch] += sum over t of (p[row][t] s[t][c]) codes[t][ch]: p s in fp16 (two planes where the output has more than eight bits) is the first
 //            operand as it stands in the lanes, since the page order gives both products the same tokens per lane; plus p m, one more
 //            instruction for all groups.
-// Waves of a workgroup share a context, workgroups split it further when there are few rows; a second kernel joins the parts.
+// Waves of a workgroup share a context, workgroups split it further when there are few rows; a second kernel joins the parts. Pages come
+// straight into LDS, two pairs ahead of a wave, so that 60 KB a compute unit are on their way (through registers, one pair ahead, 64
+// sequences took 55 us of what follows).
+// Bound: vector instructions, some 300 a pair of pages (of them 80 take codes out of words, 64 apply the keys' scales, 48 the values'), beside
+// the pages' way from memory. 64 sequences of 11 rows, 32 heads, 448 tokens in the mean 42.7 us (150 MB, 3.5 TB/s; vector units busy
+// for 26 us of it); one row of 32 + 8 heads behind 65000 tokens 19.3 + 4.1 (83 MB, 4.3 TB/s); 64 rows of 32 + 8 heads behind 8000 tokens, four
+// sequences, 90 us (0.33 PFLOP/s).
 #include <algorithm>
 
 #include "four_bit.h"
@@ -111,7 +117,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     constexpr int kWaveLds = 2 * Ring<DH>::kSlot > J * kStride * 4 ? 2 * Ring<DH>::kSlot : J * kStride * 4;
     __shared__ float sm_m[kWaves][J], sm_l[kWaves][J];
     __shared__ __attribute__((aligned(1024))) char lds[kWaves * kWaveLds];      // a wave's ring, later its results [J][kStride]
-    const int h = blockIdx.x / a.nt, tile = blockIdx.x % a.nt, b = blockIdx.y, split = blockIdx.z;
+    // (heads side by side: with a multiple of eight of them, the tiles of a head, which read the same pages, share an XCD and its cache)
+    const int h = blockIdx.x % a.H, tile = blockIdx.x / a.H, b = blockIdx.y, split = blockIdx.z;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4, j = r / CG, cc = r % CG;
     // (what the whole wave shares is kept in scalar registers: addresses, loop bounds and branches)
