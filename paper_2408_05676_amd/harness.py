@@ -32,17 +32,24 @@ class Engine:
     state (pending token, context tail) lives on the device."""
 
     def __init__(self, shape, weights: dict, batch: int, K: int, max_len: int, n_max: int = 3,
-                 prefill_chunk: int = 16, own_text_cap: int = 0):
+                 prefill_chunk: int = 16, own_text_cap: int = 0, four_bit_cache: bool = False, w4_group: int = 0):
         """own_text_cap > 0: keep each sequence's own text (prompt + emitted tokens, the most recent own_text_cap of
-        them) on the device and search it as a temporary branch at every retrieval (Sec. 3.2)."""
+        them) on the device and search it as a temporary branch at every retrieval (Sec. 3.2).
+        four_bit_cache: keys and values in four bits. w4_group 32, 64 or 128: the projections in four bits, quantised here from the bf16 weights
+        in groups of that many inputs (the embedding and the head stay bf16)."""
         self.shape, self.B, self.K, self.n_max = shape, batch, K, n_max
         R = max(K + 1, prefill_chunk)
         pages_per_seq = (max_len + 15) // 16 + 1
         self.model = L.Model(shape.n_layers, shape.d, shape.n_heads, shape.ffn, shape.vocab, weights,
                              max_rows=batch * R, max_batch=batch, max_pos=pages_per_seq * 16,
                              eps=shape.eps, rope_base=shape.rope_base)
-        self.kv = L.KVCache(shape.n_layers, shape.n_heads, shape.head_dim, n_pages=batch * pages_per_seq,
-                            max_seqs=batch, max_pages_per_seq=pages_per_seq)
+        if w4_group:
+            for l in range(shape.n_layers):
+                for name in ("wqkv", "wo", "wgu", "wdown"):
+                    self.model.set_w4(l, name, L.W4(*L.w4_quantize(weights[name][l], w4_group)))
+        cache = L.KVCache4 if four_bit_cache else L.KVCache
+        self.kv = cache(shape.n_layers, shape.n_heads, shape.head_dim, n_pages=batch * pages_per_seq,
+                        max_seqs=batch, max_pages_per_seq=pages_per_seq)
         self.seq_ids = np.arange(batch, dtype=np.int32)
         for s in range(batch):
             self.kv.reserve(s, pages_per_seq * 16)

@@ -602,6 +602,32 @@ def test_model_steps_with_four_bit_weights(B, K, tree, four_bit_cache, which):
         model.set_w4(sh.n_layers, "wo", None)
 
 
+def test_engine_in_four_bits():
+    """Prompts in pieces, then a step, all through the Engine, with 4-bit weights and a 4-bit cache."""
+    import synth
+    from paper_2408_05676_amd.harness import Engine
+    from tests.gpu_util import gpu_weights, logits_close
+    sh = synth.SHAPES["tiny"]
+    w = gpu_weights(sh)
+    what = dict(w)
+    for name in ("wqkv", "wo", "wgu", "wdown"):
+        what[name] = torch.stack([ref.values(*ref.quantize(w[name][layer].double(), 64)) for layer in range(sh.n_layers)])
+    B, K, T = 3, 5, 40
+    eng = Engine(sh, w, B, K, T + 20, prefill_chunk=16, four_bit_cache=True, w4_group=64)
+    r = np.random.default_rng(8)
+    prompts = r.integers(0, sh.vocab, (B, T))
+    eng.prefill(prompts)
+    assert eng.kv.read_lens(eng.seq_ids).tolist() == [T - 1] * B
+    drafts = torch.tensor(r.integers(0, sh.vocab, (B, K)), dtype=torch.int32, device="cuda")
+    n = torch.full((B,), K, dtype=torch.int32, device="cuda")
+    logits = laser.verify_step(eng.model, eng.kv, eng.seq_ids, eng.pending, drafts, n, 2, 0.1, want_logits=True)[-1]
+    want, worst = reference_step(what, sh, eng.kv, [T - 1] * B, torch.cat([eng.pending[:, None], drafts], 1), None)
+    ok, err, rel = logits_close(logits.cpu().double().numpy(), want.cpu().numpy())
+    assert ok, (err, rel)
+    assert worst <= 0.5 + 3 * 15 * 2.0 ** -11, worst
+    eng.close()
+
+
 def test_generation_on_a_four_bit_cache():
     """laser_generate with strict acceptance emits what one-token steps on the same kind of cache emit, drafts or not: a row's scores
     are the same numbers however many rows its step has, up to the order of fp32 sums."""
