@@ -342,9 +342,21 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
             }
         }
         if (over > 0.f && __any(large)) {
-            over = -1.f;
-            back = -4.f;
-            rescale(ref + 8.f);
+            large = false;                           // of tokens of the sequence: what lies behind them is someone else's and changes nothing
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int here = len + nr - (p + u) * kPageSize - 4 * g;
+                if constexpr (CG == 1) large |= sm_scale(vsm[u][0]) > 511.f && (r & 3) < here;
+                else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) large |= sm_scale(vsm[u][i]) > 511.f && i < here;
+                }
+            }
+            if (__any(large)) {
+                over = -1.f;
+                back = -4.f;
+                rescale(ref + 8.f);
+            }
         }
         const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
         if (__any(mx > limit)) rescale(fmaxf(ref, max_over_rows(mx) * cs - back));

@@ -265,6 +265,27 @@ def test_pages_that_another_sequence_left():
     check_attend(kv, [0], [k[0, :0].double()], [v[0, :0].double()], k.double(), v.double(), q, None, None, dh ** -0.5, out, out, True)
 
 
+@pytest.mark.parametrize("G", [1, 4, 16])
+def test_what_lies_behind_the_last_token_changes_nothing(G):
+    """Values whose scales pass 511 switch the factor of the weights: not if they are in slots behind the step's."""
+    H, dh, n = 2, 128, 37
+    g = gen(14)
+    k, v = normal(g, n, H, dh, dtype=F16), normal(g, n, H, dh, dtype=F16, scale=1e-3)
+    q, nk, nv = normal(g, 1, 2, H * G, dh, dtype=F16), normal(g, 1, 2, H, dh, dtype=F16), normal(g, 1, 2, H, dh, dtype=F16, scale=1e-3)
+    outs = []
+    for stale in (0.0, 60000.0):
+        kv = make_kv(1, H, dh, [n], 11)
+        full = torch.full((48, H, dh), stale, dtype=F16, device="cuda")
+        full[:, :, ::2] = -stale
+        kv.import_layer(0, 0, full, full)
+        kv.import_layer(0, 0, k, v)
+        kv.set_len(0, n)
+        laser.kv_append(kv, 0, [0], nk, nv)
+        outs.append(laser.kv_attend(kv, 0, [0], q))
+    assert torch.equal(outs[0], outs[1])
+    check_attend(kv, [n], [k.double()], [v.double()], nk.double(), nv.double(), q, None, None, dh ** -0.5, outs[1], outs[1], True)
+
+
 def test_many_sequences_in_one_call():
     """More sequences than ride in one launch's arguments."""
     B, H, dh = 300, 1, 64
