@@ -249,7 +249,7 @@ int laser_kv_read_lens(laser_kv* kv, const int32_t* seq_ids /*[host] B*/, int B,
  * laser_kv_create_4bit: a cache whose keys and values are held that way, 32 channels of a token and head to a group (1.25
  * bytes per token, layer and channel instead of 5). n_heads is the number of key/value heads. All laser_kv_* calls take such a handle;
  * laser_verify_step, laser_verify_tree and laser_generate do too (on the general path, whose attention is then laser_kv_attend's),
- * and results carry the cache's rounding: about 7 % of a key's or value's spread. Beside the pages it holds 17 MB (9 at head_dim 64) of workspace.
+ * and results carry the cache's rounding: about 8 % of a key's or value's standard deviation. Beside the pages it holds 17 MB (9 at head_dim 64) of workspace.
  * Stored for a group x: s = fp16((max - min) / 15), m = fp16(min), c = (x - m) / s rounded to nearest even within 0..15 (s = 0: c = 0), from
  * 64-bit intermediate values (s and m rounded to fp32 and from there to fp16); magnitudes beyond 65504 saturate. A key or value that is not finite makes its token's
  * key in that head NaN (its value as if that element were 0): rows that see the token get NaN from that head, other rows are not touched. */
@@ -303,7 +303,8 @@ int laser_kv_read(laser_kv* kv, int layer, const int32_t* seq_ids, int B, int st
  * laser_w4_create lays codes, scales and offsets out for the products (the handle keeps its own copy; synchronises `stream`):
  *   codes   [dev] uint8[N][Kd / 2]      two to a byte, the first in the low four bits
  *   scales  [dev] fp16[N][Kd / group];  offsets [dev] fp16[N][Kd / group]   (a zero point z is an offset of -s z)
- * laser_w4_quantize makes them from bf16 weights [N][Kd], by the rule of laser_kv_create_4bit. */
+ * laser_w4_quantize makes them from bf16 weights [N][Kd], by the rule of laser_kv_create_4bit; a group with a weight that is not finite
+ * becomes NaN as a whole. Up to 2^23 blocks of 16 x 128 weights a matrix (LASER_E_LIMIT). */
 typedef struct laser_w4 laser_w4;
 int laser_w4_create(const uint8_t* codes, const uint16_t* scales, const uint16_t* offsets, int N, int Kd, int group, void* stream, laser_w4** out);
 int laser_w4_destroy(laser_w4* w);

@@ -201,8 +201,11 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
     }
 }
 
+constexpr long kMaxThreads = (1l << 32) - 256;                           // of a launch's dimension
+
 int launch_kv4_append(const AppendArgs& a, int dh, int dtype, hipStream_t stream) {
     const long threads = (long)a.B * a.R * 4 * (dh / 64) * std::max(a.H, a.Hq);
+    LASER_REQUIRE(threads <= kMaxThreads, LASER_E_LIMIT, "%ld rows and heads in one call", threads / (4 * (dh / 64)));
     const dim3 grid((unsigned)((threads + 255) / 256), a.Hq > 0 ? 3 : 2);
     auto go = [&](auto dhc) {
         constexpr int D = decltype(dhc)::value;
@@ -384,7 +387,7 @@ extern "C" int laser_rope_table(float* table, int max_pos, int rope_dim, double 
     LASER_REQUIRE(table != nullptr, LASER_E_INVALID_ARG, "table is NULL");
     LASER_REQUIRE(max_pos > 0 && rope_dim > 0 && rope_dim % 2 == 0 && base > 0.0, LASER_E_INVALID_ARG, "bad size or base");
     const size_t n = (size_t)max_pos * (rope_dim / 2);
-    LASER_REQUIRE((n + 255) / 256 < (1ull << 31), LASER_E_LIMIT, "table too large");
+    LASER_REQUIRE(n <= kMaxThreads, LASER_E_LIMIT, "table too large");
     hipLaunchKernelGGL(rope_table4_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, (hipStream_t)stream, (float2*)table, max_pos, rope_dim / 2, base);
     LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
@@ -479,7 +482,9 @@ extern "C" int laser_kv_read(laser_kv* h, int layer, const int32_t* seq_ids, int
         a.pages = layer_pages(kv, layer);
         a.k = heads_from(k, b0, dtype); a.v = heads_from(v, b0, dtype);
         a.n = n; a.H = kv->d.n_heads; a.mpps = kv->d.max_pages_per_seq; a.start = start;
-        const dim3 grid((unsigned)(((long)a.B * n * a.H * 4 * (kv->d.head_dim / 64) + 255) / 256), 2);
+        const long threads = (long)a.B * n * a.H * 4 * (kv->d.head_dim / 64);
+        LASER_REQUIRE(threads <= kMaxThreads, LASER_E_LIMIT, "%ld tokens and heads in one call", threads / (4 * (kv->d.head_dim / 64)));
+        const dim3 grid((unsigned)((threads + 255) / 256), 2);
         auto go = [&](auto dhc) {
             constexpr int D = decltype(dhc)::value;
             if (dtype == DT_F16) hipLaunchKernelGGL((kv4_read_kernel<D, DT_F16>), grid, dim3(256), 0, (hipStream_t)stream, a);

@@ -45,24 +45,26 @@ __global__ __launch_bounds__(256) void w4_layout_kernel(const uint8_t* codes, co
     }
 }
 
-// Eight threads per group of a bf16 matrix.
+// Eight threads per group of a bf16 matrix. A group with a weight that is not finite: offset NaN, scale and codes 0.
 __global__ __launch_bounds__(256) void w4_quantize_kernel(const uint16_t* w, size_t groups, int group, uint8_t* codes, uint16_t* scales, uint16_t* offsets) {
     const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) >> 3;
     const int lane = threadIdx.x & 7, per = group / 8;            // elements a thread takes: 4, 8 or 16
     if (i >= groups) return;                                      // (eight lanes together)
     const uint16_t* p = w + i * group + lane * per;
     float lo = INFINITY, hi = -INFINITY;
-    for (int j = 0; j < per; ++j) { const float x = bf16_to_f32(p[j]); lo = fminf(lo, x); hi = fmaxf(hi, x); }
+    int bad = 0;
+    for (int j = 0; j < per; ++j) { const float x = bf16_to_f32(p[j]); lo = fminf(lo, x); hi = fmaxf(hi, x); bad |= !__builtin_isfinite(x); }
 #pragma unroll
-    for (int o = 1; o < 8; o *= 2) { lo = fminf(lo, __shfl_xor(lo, o)); hi = fmaxf(hi, __shfl_xor(hi, o)); }
+    for (int o = 1; o < 8; o *= 2) { lo = fminf(lo, __shfl_xor(lo, o)); hi = fmaxf(hi, __shfl_xor(hi, o)); bad |= __shfl_xor(bad, o); }
+    if (bad) lo = hi = 0.f;
     const _Float16 s = f64_to_f16(fmin(((double)hi - (double)lo) / 15.0, 65504.0)), m = (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f);
     auto code = [&](uint16_t h) {
         const double n = rint(((double)bf16_to_f32(h) - (double)(float)m) / (double)(float)s);
-        return (float)s > 0.f ? (uint32_t)fmin(fmax(n, 0.0), 15.0) : 0u;
+        return (float)s > 0.f && !bad ? (uint32_t)fmin(fmax(n, 0.0), 15.0) : 0u;
     };
     uint8_t* q = codes + (i * group + lane * per) / 2;
     for (int j = 0; j < per; j += 2) q[j / 2] = (uint8_t)(code(p[j]) | (code(p[j + 1]) << 4));
-    if (lane == 0) { scales[i] = __builtin_bit_cast(uint16_t, s); offsets[i] = __builtin_bit_cast(uint16_t, m); }
+    if (lane == 0) { scales[i] = __builtin_bit_cast(uint16_t, s); offsets[i] = bad ? 0x7E00 : __builtin_bit_cast(uint16_t, m); }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -279,7 +281,7 @@ static int check_w4(int N, int Kd, int group) {
     LASER_REQUIRE(group == 32 || group == 64 || group == 128, LASER_E_SHAPE, "group %d: 32, 64 or 128", group);
     LASER_REQUIRE(N > 0 && Kd > 0, LASER_E_INVALID_ARG, "N and Kd must be positive");
     LASER_REQUIRE(Kd % group == 0, LASER_E_SHAPE, "Kd %d is not a multiple of the group, %d", Kd, group);
-    LASER_REQUIRE(((long)N + 15) / 16 * ((Kd + 127) / 128) < (1l << 31), LASER_E_LIMIT, "matrix too large");
+    LASER_REQUIRE(((long)N + 15) / 16 * (((long)Kd + 127) / 128) < (1l << 23), LASER_E_LIMIT, "matrix too large");       // (a launch has less than 2^32 threads)
     return LASER_OK;
 }
 

@@ -44,7 +44,8 @@ def test_cache_shapes(lib, field, value, code):
 
 
 @pytest.mark.parametrize("N, Kd, group, code", [(16, 128, 16, E_SHAPE), (16, 128, 256, E_SHAPE), (16, 96, 64, E_SHAPE), (16, 0, 32, E_ARG), (0, 128, 32, E_ARG),
-                                                (-1, 128, 32, E_ARG), (16, 100, 32, E_SHAPE), (2 ** 31 - 1, 2 ** 31 - 128, 128, E_LIMIT)])
+                                                (-1, 128, 32, E_ARG), (16, 100, 32, E_SHAPE), (2 ** 31 - 1, 2 ** 31 - 128, 128, E_LIMIT),
+                                                (2 ** 27, 128, 128, E_LIMIT), (16, 2 ** 30, 32, E_LIMIT)])
 def test_weight_shapes(lib, N, Kd, group, code):
     out, p = C.c_void_p(), C.c_void_p(64)
     assert lib.laser_w4_create(p, p, p, N, Kd, group, None, C.byref(out)) == code and not out.value
@@ -60,6 +61,7 @@ def test_null_and_misaligned_arguments(lib):
     assert lib.laser_w4_destroy(None) == 0
     assert lib.laser_model_set_w4(None, 0, 0, None) == E_ARG
     assert lib.laser_rope_table(None, 4, 64, C.c_double(1e4), None) == E_ARG
+    assert lib.laser_rope_table(p, 2 ** 27, 64, C.c_double(1e4), None) == E_LIMIT
     for size, dim, base in ((0, 64, 1e4), (4, 63, 1e4), (4, 0, 1e4), (4, 64, 0.0)):
         assert lib.laser_rope_table(p, size, dim, C.c_double(base), None) == E_ARG
 

@@ -479,6 +479,30 @@ def test_products_at_the_model_widths():
         assert bool(((got - want).abs() <= tol + ref.EPS[dtype] * (want.abs() + tol) + 2.0 ** -25).all()), (N, Kd)
 
 
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_weights_that_are_not_finite_reach_their_own_output_only(dtype, group):
+    """A group with such a weight is NaN: so is its output, and no other."""
+    g = gen(15)
+    w, x = normal(g, 48, 256, dtype=BF16, scale=0.05), normal(g, 7, 256, dtype=dtype)
+    want = laser.w4_matmul(laser.W4(*laser.w4_quantize(w, group)), x)
+    bad = {3: (0, float("nan")), 17: (255, float("inf")), 40: (130, float("-inf"))}
+    for n, (i, value) in bad.items():
+        w[n, i] = value
+    w[33, :group] = float("nan")
+    codes, s, m = laser.w4_quantize(w, group)
+    assert s.isfinite().all()
+    for n, (i, _) in bad.items():
+        assert m[n].isnan().nonzero().tolist() == [[i // group]] and s[n, i // group] == 0
+        assert not codes[n, i // group * group // 2:(i // group + 1) * group // 2].any()
+    got = laser.w4_matmul(laser.W4(codes, s, m), x)
+    rows = torch.tensor([*bad, 33], device="cuda")
+    assert got[:, rows].isnan().all()
+    keep = torch.ones(48, dtype=torch.bool, device="cuda")
+    keep[rows] = False
+    assert torch.equal(got[:, keep], want[:, keep])
+
+
 def test_product_refusals():
     g = gen(21)
     h = laser.W4(*laser.w4_quantize(normal(g, 32, 128, dtype=BF16), 64))
