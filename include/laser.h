@@ -309,10 +309,10 @@ typedef struct laser_w4 laser_w4;
 int laser_w4_create(const uint8_t* codes, const uint16_t* scales, const uint16_t* offsets, int N, int Kd, int group, void* stream, laser_w4** out);
 int laser_w4_destroy(laser_w4* w);
 int laser_w4_quantize(const uint16_t* w, int N, int Kd, int group, uint8_t* codes, uint16_t* scales, uint16_t* offsets, void* stream);
-/* laser_w4_matmul: out[r][n] = sum over i of x[r][i] W[n][i] for M rows; x and out in `dtype` (LASER_F16 or LASER_BF16), rows
+/* laser_w4_matmul: out[r][n] = sum over i of x[r][i] W[n][i] for M rows (up to 65535 * 32); x and out in `dtype` (LASER_F16 or LASER_BF16), rows
  * x_stride >= Kd and out_stride >= N elements apart, aligned to their elements; out must not overlap x. fp32 sums; a row of x that is not
  * finite gives results that are not. Keeps no workspace: calls on several streams may share a handle. Made for few rows (every weight is read once
- * up to 80 rows, again for every 80 further ones). */
+ * up to 16 rows, and again for every 32, 48 or 80 of more). */
 int laser_w4_matmul(const laser_w4* w, const void* x, int64_t x_stride, int M, int dtype, void* out, int64_t out_stride, void* stream);
 
 /* laser_model_set_w4: from the next call on, steps of the model multiply with `w` instead of the bf16 matrix `which` of the layer (NULL: with the

@@ -8,7 +8,7 @@
 // exponent of 128 and stands for 128 + c, which the offset m - 128 s takes back.
 // Bound: up to four rows the weights' way from memory (4096 -> 22016, group 128, one row: 48 MB in 12.0 us, 4.0 TB/s where a long read reaches 5.5);
 // with more rows theirs as well, from L2 once a workgroup (9 rows 13.0 us, 11008 -> 4096 10.1 us); from 17 rows on the matrix and vector
-// instructions of too few waves (72 rows 2048 -> 6144 10.2 us, 4096 -> 22016 42 us, 0.31 PFLOP/s).
+// instructions of the waves that fit (72 rows 2048 -> 6144 10.3 us, 4096 -> 22016 36 us, 0.36 PFLOP/s).
 // Staging a block's rows in LDS for four waves, behind a barrier a block, was slower at every size (72 rows 2048 -> 6144 17.8 us).
 #include <algorithm>
 #include <vector>
@@ -243,19 +243,31 @@ static void launch_kernel(const W4Args& a, hipStream_t stream) {
     hipLaunchKernelGGL((w4_matmul_kernel<BF, NG, SWAP, MT, NT, WK>), grid, dim3(WK * 64), WK / 2 * NT * MT * 1024, stream, a);
 }
 
-// Output tiles per wave (NT) and waves to a workgroup (WK): several tiles share a wave's rows where there are tiles enough for every
-// compute unit all the same. bf16, group 128, us with one tile and eight waves / as taken here:
-//   1 row 4096 -> 22016 14.4 / 11.9, 9 rows 15.8 / 13.0;   24 rows 4096 -> 12288 14.8 / 11.4, 40 rows 20.7 / 14.4;   72 rows 4096 -> 22016 66.8 / 39.7,
-//   2048 -> 6144 15.9 / 10.2. And where one tile is taken, with two: 1 row 4096 -> 4096 4.3 / 5.2, 72 rows 11008 -> 4096 28.1 / 29.9.
+// Tiles of rows (MT) and outputs (NT) per wave, waves to a workgroup (WK). Up to 16 rows: two output tiles where there are tiles enough for
+// every compute unit all the same (1 row 4096 -> 22016 one tile and eight waves 14.4 us, so 11.9; 9 rows 15.8, 13.0; 1 row 4096 -> 4096 4.3, with two 5.2).
+// More rows: the smallest tile of a wave with which workgroups of eight waves are at most one for each of 256 compute units; a larger one leaves
+// units idle, a smaller one gives some a second workgroup. us as taken / with the next smaller / the next larger tile, bf16, group 128:
+//   1 x 2 (outputs x rows) 40 rows 2048 -> 2048 5.1 / - / 5.9;        2 x 2 40 rows 4096 -> 4096 8.4 / 10.2 / 10.7;
+//   2 x 3 72 rows 11008 -> 4096 21.8 / 24.6 / 27.5;                   4 x 3 72 rows 4096 -> 8192 15.4 / 20.0 / 18.3 (4 x 3, four waves)
+// Where no tile is large enough, four waves: 4 x 3, with at least two workgroups a unit unless the rows fill such tiles much better than pairs, and not if they fill
+// them much worse (72 rows 4096 -> 22016 35.9, 2 x 2 40.8; 40 rows 25.0 and 28.8), else 2 x 2 (240 rows 4096 -> 4096 21.2, 4 x 3 24.9; 24 rows
+// 4096 -> 22016 17.1 and 24.6; 112 rows, group 32, 73.2 and 84.8). Groups of 32 leave fewer registers: 2 x 5 and eight waves where the rows fill that better
+// (72 rows 4096 -> 22016 47.9, 4 x 3 54.9).
 template <bool BF, int NG>
 static void launch_rows(const W4Args& a, hipStream_t stream) {
-    const int mt = std::min(5, (a.M + 15) / 16), tiles = a.epi == W4_SWIGLU ? 1 << 20 : a.tiles;      // (gate and up tiles share a wave)
-    if (a.M <= 4) tiles >= 1024 ? launch_kernel<BF, NG, false, 1, 2, 4>(a, stream) : launch_kernel<BF, NG, false, 1, 1, 8>(a, stream);
-    else if (mt == 1) tiles >= 1024 ? launch_kernel<BF, NG, true, 1, 2, 4>(a, stream) : launch_kernel<BF, NG, true, 1, 1, 8>(a, stream);
-    else if (mt == 2) tiles >= 512 ? launch_kernel<BF, NG, true, 2, 4, 8>(a, stream) : launch_kernel<BF, NG, true, 2, 1, 8>(a, stream);
-    else if (mt == 3) tiles >= 512 ? launch_kernel<BF, NG, true, 3, 4, 8>(a, stream) : launch_kernel<BF, NG, true, 3, 1, 8>(a, stream);
-    else if (mt == 4) tiles >= 320 ? launch_kernel<BF, NG, true, 4, 2, 8>(a, stream) : launch_kernel<BF, NG, true, 4, 1, 8>(a, stream);
-    else tiles >= 320 ? launch_kernel<BF, NG, true, 5, 2, 8>(a, stream) : launch_kernel<BF, NG, true, 5, 1, 8>(a, stream);
+    const bool pairs = a.epi == W4_SWIGLU;                           // (gate and up tiles share a wave)
+    const long tiles = pairs ? 2l * a.tiles : a.tiles, by2 = (a.M + 31) / 32, by3 = (a.M + 47) / 48, by5 = (a.M + 79) / 80, cus = 256;
+    const bool threes = 3 * by3 * 8 < 2 * by2 * (tiles * by3 < 8 * cus ? 7 : 9);
+    if (a.M <= 4) tiles >= 1024 || pairs ? launch_kernel<BF, NG, false, 1, 2, 4>(a, stream) : launch_kernel<BF, NG, false, 1, 1, 8>(a, stream);
+    else if (a.M <= 16) tiles >= 1024 || pairs ? launch_kernel<BF, NG, true, 1, 2, 4>(a, stream) : launch_kernel<BF, NG, true, 1, 1, 8>(a, stream);
+    else if (tiles * by2 <= cus && !pairs) launch_kernel<BF, NG, true, 2, 1, 8>(a, stream);
+    else if (tiles * by2 <= 2 * cus) launch_kernel<BF, NG, true, 2, 2, 8>(a, stream);
+    else if (tiles * by3 <= 2 * cus) launch_kernel<BF, NG, true, 3, 2, 8>(a, stream);
+    else if (tiles * by2 <= 4 * cus) launch_kernel<BF, NG, true, 2, 4, 8>(a, stream);
+    else if (tiles * by3 <= 4 * cus) launch_kernel<BF, NG, true, 3, 4, 8>(a, stream);
+    else if (NG == 4 && 5 * by5 < std::min(3 * by3, 2 * by2)) launch_kernel<BF, NG, true, NG == 4 ? 5 : 3, NG == 4 ? 2 : 4, NG == 4 ? 8 : 4>(a, stream);
+    else if (threes) launch_kernel<BF, NG, true, 3, 4, 4>(a, stream);
+    else launch_kernel<BF, NG, true, 2, 2, 4>(a, stream);
 }
 
 int launch_w4(const W4* w, const void* x, int64_t x_stride, int M, int dtype, int epi, void* out, int64_t out_stride, hipStream_t stream) {
@@ -326,7 +338,7 @@ extern "C" int laser_w4_matmul(const laser_w4* h, const void* x, int64_t x_strid
     const W4* w = reinterpret_cast<const W4*>(h);
     LASER_REQUIRE(w != nullptr, LASER_E_INVALID_ARG, "w is NULL");
     LASER_REQUIRE(dtype == LASER_F16 || dtype == LASER_BF16, LASER_E_INVALID_ARG, "dtype %d: LASER_F16 or LASER_BF16", dtype);
-    LASER_REQUIRE(M >= 0 && M <= 65535 * 80, LASER_E_INVALID_ARG, "M %d out of range", M);
+    LASER_REQUIRE(M >= 0 && M <= 65535 * 32, LASER_E_INVALID_ARG, "M %d out of range", M);
     LASER_REQUIRE(x_stride >= w->Kd && out_stride >= w->N, LASER_E_INVALID_ARG, "rows overlap: strides %lld, %lld", (long long)x_stride, (long long)out_stride);
     if (M == 0) return LASER_OK;
     LASER_REQUIRE(x && out, LASER_E_INVALID_ARG, "NULL argument");

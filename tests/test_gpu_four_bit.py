@@ -465,6 +465,14 @@ def test_products(N, Kd, group, M, dtype):
     assert torch.equal(laser.w4_matmul(h, x), out[:M, 2:N + 2])
 
 
+@pytest.mark.parametrize("N, M", [(4100, 17), (4100, 65), (8185, 33), (6150, 50), (11260, 20), (12270, 40), (22010, 24), (22010, 35), (22010, 75), (9003, 170)])
+@pytest.mark.parametrize("Kd, group", [(160, 32), (320, 64), (384, 128)])
+def test_products_of_every_tile_of_a_wave(N, Kd, group, M):
+    """Widths and rows that the choice of tiles falls to either side for, neither whole tiles."""
+    test_products(N, Kd, group, M, F16)
+    test_products(N, Kd, group, M, BF16)
+
+
 def test_products_at_the_model_widths():
     g = gen(20)
     for N, Kd, group, M, dtype in ((22016, 4096, 128, 1, BF16), (4096, 11008, 64, 9, F16), (6144, 2048, 128, 72, BF16), (12288, 4096, 32, 33, F16)):
