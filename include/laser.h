@@ -279,8 +279,9 @@ int laser_rope_table(float* table, int max_pos, int rope_dim, double base, void*
  *   rope        [dev] float[max_pos][rope_dim / 2][2] (laser_rope_table), 8-byte aligned; channel i < rope_dim / 2 is paired with i + rope_dim / 2,
  *               channels from rope_dim on are not rotated. rope_dim: 0 (no rotation), head_dim, or 64 of 128. Positions must stay below
  *               max_pos (checked against the host's bound of len, LASER_E_LIMIT; a replayed graph's are cut to it).
- * seq_ids and the reservations are part of the launch: a captured append keeps those of its capture, and leaves out rows for which
- * a length that has grown under replays has no reserved slot. */
+ * seq_ids are part of the launch: a captured append keeps those of its capture. It leaves out rows for which a length that has grown under
+ * replays has no slot reserved at the time; so do laser_kv_attend, laser_kv_read and a captured step of a model on a 4-bit cache, and
+ * laser_kv_commit_tree (on either kind of cache) moves no token there. */
 int laser_kv_append(laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* n_rows, const int32_t* tree_parent, int B, int R,
                     int dtype, const laser_heads* k, const laser_heads* v, const laser_heads* q, const laser_heads* q_out, int n_heads,
                     const float* rope, int rope_dim, int max_pos, void* stream);

@@ -37,14 +37,13 @@ __host__ __device__ constexpr int page4_vsm(int dh) { return 18 * dh; }
 __host__ __device__ constexpr int sm_index(int dh, int t, int c) { return (t >> 2) * (dh / 8) + c * 4 + (t & 3); }
 
 // [host] ids of up to kSeqChunk sequences ride in the kernel arguments: nothing is staged, and a captured launch keeps its own.
-// cap: tokens the sequence's pages hold; slots beyond are neither read nor written, whatever the length on the device says.
+// cap: tokens that a slot's pages hold as the launch runs; slots beyond are neither read nor written, whatever the length on the device says.
 constexpr int kSeqChunk = 256;
 struct SeqList {
-    const int32_t* dev;                              // ids on the device instead (a step of the model), all slots reserved
-    int32_t cap_all;                                 // their cap
-    int32_t id[kSeqChunk], cap[kSeqChunk];
+    const int32_t* dev;                              // ids on the device instead (a step of the model)
+    const int32_t* cap;                              // [dev] of all slots (KV::cap)
+    int32_t id[kSeqChunk];
     __device__ int slot(int b) const { return dev ? dev[b] : id[b]; }
-    __device__ int tokens(int b) const { return dev ? cap_all : cap[b]; }
 };
 
 struct Heads { void* p; int64_t seq, row, head; };   // element (b, r, h, c) at p + b seq + r row + h head + c

@@ -50,12 +50,13 @@ __global__ void commit_kernel(int32_t* len, const int32_t* seq_ids, const int32_
 // rows (accept_path[b][0 .. accept_len[b]), ascending node indices) move to slots len + 1, len + 2, .. behind the
 // pending token before the length grows. A thread owns one channel of one (sequence, layer, head) and moves its
 // elements branch position by branch position: sources never lie before their destinations (path[j] >= j), and a
-// destination is never a later source, so the in-place order j = 0, 1, .. is safe.
+// destination is never a later source, so the in-place order j = 0, 1, .. is safe. A replayed graph's length may have passed the
+// reservation: nothing is moved from or to slots beyond it.
 __global__ void kv_compact_kernel(uint16_t* kpages, uint8_t* klpages, uint16_t* vpages, const int32_t* block_table,
-                                  const int32_t* len, const int32_t* seq_ids, const int32_t* accept_len,
+                                  const int32_t* len, const int32_t* cap, const int32_t* seq_ids, const int32_t* accept_len,
                                   const int32_t* accept_path, int K, int H, int dh, int mpps, int n_pages) {
     const int h = blockIdx.x, l = blockIdx.y, b = blockIdx.z, c = threadIdx.x;
-    const int slot = seq_ids[b], len0 = len[slot];
+    const int slot = seq_ids[b], len0 = len[slot], have = cap[slot];
     int a = accept_len[b];
     a = a < 0 ? 0 : (a > K ? K : a);
     const int32_t* bt = block_table + (size_t)slot * mpps;
@@ -64,6 +65,7 @@ __global__ void kv_compact_kernel(uint16_t* kpages, uint8_t* klpages, uint16_t* 
         if (i < j || i >= K) break;                     // not a branch of this step's tree: nothing more to move
         if (i == j) continue;
         const int src = len0 + 1 + i, dst = len0 + 1 + j;
+        if (src >= have) break;                         // (dst < src < later sources)
         const size_t sb = (((size_t)l * n_pages + bt[src / kPageSize]) * H + h) * kPageSize * dh;
         const size_t db = (((size_t)l * n_pages + bt[dst / kPageSize]) * H + h) * kPageSize * dh;
         const int st = src % kPageSize, dt = dst % kPageSize;
@@ -164,6 +166,7 @@ static int create_impl(const laser_kv_desc* desc, bool four_bit, void* stream_, 
     }
     KV_TRY(hipMalloc((void**)&kv->block_table, bt * 4));
     KV_TRY(hipMalloc((void**)&kv->len, (size_t)d.max_seqs * 4));
+    KV_TRY(hipMalloc((void**)&kv->cap, (size_t)d.max_seqs * 4));
     KV_TRY(hipMalloc((void**)&kv->ids_dev, (size_t)kIdSlots * d.max_seqs * 4));
     KV_TRY(hipHostMalloc((void**)&kv->ids_pinned, (size_t)kIdSlots * d.max_seqs * 4));
     for (int i = 0; i < kIdSlots; ++i) KV_TRY(hipEventCreateWithFlags(&kv->ids_ev[i], hipEventDisableTiming));
@@ -177,6 +180,7 @@ static int create_impl(const laser_kv_desc* desc, bool four_bit, void* stream_, 
     }
     KV_TRY(hipMemsetAsync(kv->block_table, 0, bt * 4, stream));
     KV_TRY(hipMemsetAsync(kv->len, 0, (size_t)d.max_seqs * 4, stream));
+    KV_TRY(hipMemsetAsync(kv->cap, 0, (size_t)d.max_seqs * 4, stream));
     KV_TRY(hipStreamSynchronize(stream));
 #undef KV_TRY
     kv->h_block_table.assign(bt, 0);
@@ -197,7 +201,7 @@ extern "C" int laser_kv_destroy(laser_kv* h) {
     KV* kv = reinterpret_cast<KV*>(h);
     (void)hipFree(kv->pages4); (void)hipFree(kv->part4);
     (void)hipFree(kv->kpages); (void)hipFree(kv->klpages); (void)hipFree(kv->vpages); (void)hipFree(kv->block_table);
-    (void)hipFree(kv->len); (void)hipFree(kv->ids_dev);
+    (void)hipFree(kv->len); (void)hipFree(kv->cap); (void)hipFree(kv->ids_dev);
     if (kv->ids_pinned) (void)hipHostFree(kv->ids_pinned);
     for (int i = 0; i < kIdSlots; ++i) if (kv->ids_ev[i]) (void)hipEventDestroy(kv->ids_ev[i]);
     delete kv;
@@ -227,6 +231,8 @@ extern "C" int laser_kv_seq_reserve(laser_kv* h, int seq, int n_tokens, void* st
     // until the next reserve/release of this slot, which enqueue behind this copy
     LASER_HIP_CHECK(hipMemcpyAsync(kv->block_table + (size_t)seq * kv->d.max_pages_per_seq + have, row + have,
                                    (size_t)(need - have) * 4, hipMemcpyHostToDevice, (hipStream_t)stream));
+    hipLaunchKernelGGL(fill_i32_kernel, dim3(1), dim3(64), 0, (hipStream_t)stream, kv->cap + seq, need * kPageSize, (size_t)1);
+    LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
 }
 
@@ -239,6 +245,7 @@ extern "C" int laser_kv_seq_release(laser_kv* h, int seq, void* stream) {
     kv->h_npages[seq] = 0;
     kv->h_len_ub[seq] = 0;
     kv->h_last_rows[seq] = 0;
+    hipLaunchKernelGGL(fill_i32_kernel, dim3(1), dim3(64), 0, (hipStream_t)stream, kv->cap + seq, 0, (size_t)1);
     hipLaunchKernelGGL(fill_i32_kernel, dim3(1), dim3(64), 0, (hipStream_t)stream, kv->len + seq, 0, (size_t)1);
     LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
@@ -320,7 +327,7 @@ static int commit_impl(laser_kv* h, const int32_t* seq_ids, const int32_t* accep
         if ((rc = launch_kv4_compact(kv, ids_dev, accept_len, accept_path, B, K, (hipStream_t)stream))) return rc;
     } else if (accept_path && K > 0 && kv->d.n_layers > 0)
         hipLaunchKernelGGL(kv_compact_kernel, dim3(kv->d.n_heads, kv->d.n_layers, B), dim3(kv->d.head_dim), 0, (hipStream_t)stream,
-                           kv->kpages, kv->klpages, kv->vpages, kv->block_table, kv->len, ids_dev, accept_len, accept_path, K,
+                           kv->kpages, kv->klpages, kv->vpages, kv->block_table, kv->len, kv->cap, ids_dev, accept_len, accept_path, K,
                            kv->d.n_heads, kv->d.head_dim, kv->d.max_pages_per_seq, kv->d.n_pages);
     hipLaunchKernelGGL(commit_kernel, dim3((B + 63) / 64), dim3(64), 0, (hipStream_t)stream, kv->len, ids_dev, accept_len, B, max_rows - 1);
     LASER_HIP_CHECK(hipGetLastError());

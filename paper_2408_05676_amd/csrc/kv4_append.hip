@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(AppendArgs a) {
     const int slot_id = a.seqs.slot(b);
     const int len = a.start >= 0 ? a.start : a.lens[slot_id];
     const int slot = len + r;
-    if (what < 2 && (slot >= a.seqs.tokens(b) || slot < 0)) return;
+    if (what < 2 && (slot >= a.seqs.cap[slot_id] || slot < 0)) return;
 
     // ---- positions; (cos, sin) of the eight channels of a rotated group c: turn + 32 c (c counts within the first half of the rotated ones)
     const int hg = a.rope_dim / 64;                                      // groups in half of the rotated channels
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
     const int b = (int)(row / a.n), r = (int)(row % a.n);
     const int id = a.seqs.slot(b);
     const int slot = (a.start >= 0 ? a.start : a.lens[id]) + r;
-    if (slot < 0 || slot >= a.seqs.tokens(b)) return;
+    if (slot < 0 || slot >= a.seqs.cap[id]) return;
     const int tp = slot % kPageSize;
     const int pg = a.block_table[(size_t)id * a.mpps + slot / kPageSize];
     const uint8_t* page = a.pages + ((size_t)pg * a.H + h) * page4_bytes(DH);
@@ -276,10 +276,10 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(ReadArgs a) {
 
 // laser_kv_commit_tree's move of the accepted branch (see kv_compact_kernel): a lane owns one key byte and one value byte of a
 // token's dh / 2, four of them a word of sm, and moves them branch position by branch position.
-__global__ void kv4_compact_kernel(uint8_t* pages, const int32_t* block_table, const int32_t* len, const int32_t* seq_ids,
+__global__ void kv4_compact_kernel(uint8_t* pages, const int32_t* block_table, const int32_t* len, const int32_t* cap, const int32_t* seq_ids,
                                    const int32_t* accept_len, const int32_t* accept_path, int K, int H, int dh, int mpps, int n_pages) {
     const int h = blockIdx.x, l = blockIdx.y, b = blockIdx.z, c = threadIdx.x, ng = dh / 32;
-    const int id = seq_ids[b], len0 = len[id];
+    const int id = seq_ids[b], len0 = len[id], have = cap[id];
     int acc = accept_len[b];
     acc = acc < 0 ? 0 : (acc > K ? K : acc);
     const int32_t* bt = block_table + (size_t)id * mpps;
@@ -289,6 +289,7 @@ __global__ void kv4_compact_kernel(uint8_t* pages, const int32_t* block_table, c
         if (i < j || i >= K) break;
         if (i == j) continue;
         const int src = len0 + 1 + i, dst = len0 + 1 + j, st = src % kPageSize, dt = dst % kPageSize;
+        if (src >= have) break;                             // (dst < src < later sources)
         const uint8_t* sp = pages + (((size_t)l * n_pages + bt[src / kPageSize]) * H + h) * page4_bytes(dh);
         uint8_t* dp = pages + (((size_t)l * n_pages + bt[dst / kPageSize]) * H + h) * page4_bytes(dh);
         if (c < dh / 2) {
@@ -304,7 +305,7 @@ __global__ void kv4_compact_kernel(uint8_t* pages, const int32_t* block_table, c
 }
 
 int launch_kv4_compact(const KV* kv, const int32_t* ids_dev, const int32_t* accept_len, const int32_t* accept_path, int B, int K, hipStream_t stream) {
-    hipLaunchKernelGGL(kv4_compact_kernel, dim3(kv->d.n_heads, kv->d.n_layers, B), dim3(64), 0, stream, kv->pages4, kv->block_table, kv->len,
+    hipLaunchKernelGGL(kv4_compact_kernel, dim3(kv->d.n_heads, kv->d.n_layers, B), dim3(64), 0, stream, kv->pages4, kv->block_table, kv->len, kv->cap,
                        ids_dev, accept_len, accept_path, K, kv->d.n_heads, kv->d.head_dim, kv->d.max_pages_per_seq, kv->d.n_pages);
     LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
@@ -349,8 +350,8 @@ static Heads heads_from(const laser_heads* t, int b0, int dtype) {
 
 static void fill_seqs(const KV* kv, const int32_t* ids, int B, SeqList& s) {
     s.dev = nullptr;
-    s.cap_all = 0;
-    for (int b = 0; b < B; ++b) { s.id[b] = ids[b]; s.cap[b] = kv->h_npages[ids[b]] * kPageSize; }
+    s.cap = kv->cap;
+    std::copy(ids, ids + B, s.id);
 }
 
 static int check_rows(const KV* kv, const int32_t* seq_ids, int B, int R) {

@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = lane & 15, g = lane >> 4, j = r / CG, cc = r % CG;
     // (what the whole wave shares is kept in scalar registers: addresses, loop bounds and branches)
-    const int slot = __builtin_amdgcn_readfirstlane(a.seqs.slot(b)), len = ((scalar_ints)a.lens)[slot], cap = a.seqs.tokens(b);
+    const int slot = __builtin_amdgcn_readfirstlane(a.seqs.slot(b)), len = ((scalar_ints)a.lens)[slot], cap = ((scalar_ints)a.seqs.cap)[slot];
     int nr = a.n_rows ? min(max(a.n_rows[b], 0), a.R) : a.R;
     nr = __builtin_amdgcn_readfirstlane(max(0, min(nr, cap - len)));      // (a length beyond the pages: rows that have no slot are left out)
     const int P = nr * a.G;                          // packed rows
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttendArgs a) {
     const int row = blockIdx.x % a.J, tile = blockIdx.x / a.J % a.nt, h = blockIdx.x / a.J / a.nt, b = blockIdx.y, pi = tile * a.J + row;
     const int slot = a.seqs.slot(b), len = a.lens[slot];
     int nr = a.n_rows ? min(max(a.n_rows[b], 0), a.R) : a.R;
-    nr = max(0, min(nr, a.seqs.tokens(b) - len));
+    nr = max(0, min(nr, a.seqs.cap[slot] - len));
     if (pi >= nr * a.G || len < 0) return;
     const float* part = a.part + (((size_t)b * a.H + h) * a.nt + tile) * a.nsplit * part_floats(DH);
     const int c = threadIdx.x % C, s0 = threadIdx.x / C;

@@ -788,7 +788,7 @@ static int four_bit_attention(Model* m, KV* kv, const int32_t* ids_dev, const Ro
     float* qkv = const_cast<float*>(ra.qkv);
     AppendArgs ap{};
     ap.seqs.dev = ids_dev;
-    ap.seqs.cap_all = kv->d.max_pages_per_seq * kPageSize;
+    ap.seqs.cap = kv->cap;
     ap.lens = kv->len; ap.block_table = kv->block_table;
     ap.pages = kv->pages4 + (size_t)layer * kv->d.n_pages * H * page4_bytes(dh);
     ap.row_pos = m->row_pos;

@@ -34,6 +34,7 @@ struct KV {
     float* part4 = nullptr;           // the attention's results of context parts, of a fixed size
     int32_t* block_table = nullptr;   // [dev] [max_seqs][max_pages_per_seq]
     int32_t* len = nullptr;           // [dev] [max_seqs] committed tokens
+    int32_t* cap = nullptr;           // [dev] [max_seqs] tokens that the pages reserved now hold; entries of block_table beyond are anyone's
     // host bookkeeping
     std::vector<int32_t> h_block_table;
     std::vector<int32_t> h_npages;    // pages owned per slot
