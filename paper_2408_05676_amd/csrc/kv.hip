@@ -11,7 +11,27 @@ namespace laser {
 
 int kv4_import(KV* kv, int seq, int layer, const uint16_t* k, const uint16_t* v, int n_tokens, hipStream_t stream);
 
+struct IdList { int32_t id[256]; };
+__global__ void store_ids_kernel(int32_t* to, IdList ids, int n) {
+    if ((int)threadIdx.x < n) to[threadIdx.x] = ids.id[threadIdx.x];
+}
+
 int KV::stage_ids(const int32_t* host_ids, int B, hipStream_t stream, const int32_t** dev_out) {
+    hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+    LASER_HIP_CHECK(hipStreamIsCapturing(stream, &capturing));
+    if (capturing != hipStreamCaptureStatusNone) {
+        // A replay must find this call's ids, whatever the staging slots hold by then, and leave those slots alone: the ids ride in
+        // kernel arguments to memory that only graphs use, each before it reads them (one handle, one stream at a time).
+        for (int b = 0; b < B; b += 256) {
+            IdList list;
+            const int n = std::min(256, B - b);
+            std::copy(host_ids + b, host_ids + b + n, list.id);
+            hipLaunchKernelGGL(store_ids_kernel, dim3(1), dim3(256), 0, stream, ids_graph + b, list, n);
+        }
+        LASER_HIP_CHECK(hipGetLastError());
+        *dev_out = ids_graph;
+        return LASER_OK;
+    }
     // The same ids on the same stream as the staging before (the steady state of a decoding loop, where verify and
     // commit alternate over one batch): that device copy is still intact and ordered before this call.
     if (ids_last >= 0 && ids_last_n == B && ids_last_stream == stream &&
@@ -168,6 +188,7 @@ static int create_impl(const laser_kv_desc* desc, bool four_bit, void* stream_, 
     KV_TRY(hipMalloc((void**)&kv->len, (size_t)d.max_seqs * 4));
     KV_TRY(hipMalloc((void**)&kv->cap, (size_t)d.max_seqs * 4));
     KV_TRY(hipMalloc((void**)&kv->ids_dev, (size_t)kIdSlots * d.max_seqs * 4));
+    KV_TRY(hipMalloc((void**)&kv->ids_graph, (size_t)d.max_seqs * 4));
     KV_TRY(hipHostMalloc((void**)&kv->ids_pinned, (size_t)kIdSlots * d.max_seqs * 4));
     for (int i = 0; i < kIdSlots; ++i) KV_TRY(hipEventCreateWithFlags(&kv->ids_ev[i], hipEventDisableTiming));
     // Pages start as zeros: masked-out cache slots are multiplied by probability 0 in the value
@@ -201,7 +222,7 @@ extern "C" int laser_kv_destroy(laser_kv* h) {
     KV* kv = reinterpret_cast<KV*>(h);
     (void)hipFree(kv->pages4); (void)hipFree(kv->part4);
     (void)hipFree(kv->kpages); (void)hipFree(kv->klpages); (void)hipFree(kv->vpages); (void)hipFree(kv->block_table);
-    (void)hipFree(kv->len); (void)hipFree(kv->cap); (void)hipFree(kv->ids_dev);
+    (void)hipFree(kv->len); (void)hipFree(kv->cap); (void)hipFree(kv->ids_dev); (void)hipFree(kv->ids_graph);
     if (kv->ids_pinned) (void)hipHostFree(kv->ids_pinned);
     for (int i = 0; i < kIdSlots; ++i) if (kv->ids_ev[i]) (void)hipEventDestroy(kv->ids_ev[i]);
     delete kv;

@@ -49,6 +49,7 @@ struct KV {
     int ids_last = -1, ids_last_n = 0;            // most recently staged slot, its id count and stream
     hipStream_t ids_last_stream = nullptr;
     int ids_next = 0;
+    int32_t* ids_graph = nullptr;                 // [max_seqs] those of captured calls, written by a kernel of the graph
 
     int stage_ids(const int32_t* host_ids, int B, hipStream_t stream, const int32_t** dev_out);
     size_t page_elems() const { return (size_t)d.n_heads * kPageSize * d.head_dim; }

@@ -146,3 +146,39 @@ def test_tree_commits_on_a_cache_of_sixteen_bits():
     assert kv.read_lens([0, 1]).tolist() == [103, 25]
     kv.set_len(0, 0)
     assert torch.equal(answer(), want)
+
+
+@pytest.mark.parametrize("same_stream", [False, True])
+def test_captured_commits_keep_their_sequences(same_stream):
+    """Calls for other sequences on the same handle come in between, more of them than the host stages lists of ids for."""
+    H, dh = 1, 64
+    kv = laser.KVCache4(1, H, dh, 6, 3, 2)
+    for s in range(3):
+        kv.reserve(s, 32)
+    k, none, two = normal(9, 1, 2, H, dh), i32([-1]), i32([1])
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        def step(s, accept):
+            laser.kv_append(kv, 0, [s], k, k)
+            laser.kv_commit(kv, [s], accept)
+        step(0, none)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream if same_stream else None):
+            step(0, two)
+        assert kv.read_lens([0, 1, 2]).tolist() == [0, 0, 0]
+        step(0, none)                                            # what the capture staged was not copied by it
+        for rounds in range(3):
+            graph.replay()
+            assert kv.read_lens([0, 1, 2]).tolist() == [2 * rounds + 2, 0, 0]
+            for i in range(70):
+                step(1 + i % 2, none)
+                kv.read_lens([1, 2])
+            step(1, none)
+            graph.replay()                                       # must not change the ids that the next call finds staged
+            kv.set_len(0, 2 * rounds + 2)
+            step(1, two)
+            assert kv.read_lens([0, 1, 2]).tolist() == [2 * rounds + 2, 2, 0]
+            kv.set_len(1, 0)
+        stream.synchronize()
