@@ -208,18 +208,22 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     }
     const float cs = a.scale_log2 == 0.f ? 1.f : fmaxf(ldexpf(fabsf(a.scale_log2) * (CG == 1 ? 1.f / kSumUnit : kCodeUnit), -e), 1e-37f);
 
-    // ---- the walk. Weights are p = 2^(score - ref); ref moves, and what was summed with it, when a score passes it by more than `over`,
-    // and is then set to `back` below the row's largest score. p s is thus at most 2^over s: within fp16 while s <= 511, and beyond, once a larger scale
-    // has been met, with over = -1.
+    // ---- the walk. Weights are p = 2^(score - ref); ref moves, and what was summed with it, when a score passes it by more than kOver,
+    // and is then set to kBack below the row's largest score: a row's largest p is 2^11 to 2^14. Values' scales are multiplied by `lift`, a power of
+    // 16 for each group that brings the largest scale met so far into [1/8, 2), and what was summed with it when a larger one comes. p and p s lift thus
+    // stay within fp16, and what it rounds to 0 is below 2^-36 of the largest weight and 2^-33 of that weight times the group's largest scale: a long
+    // tail of small weights keeps its share however small the values are. (Steps of 16: the first pair of pages sets it, and few change it.)
+    constexpr float kOver = 14.f, kBack = 11.f;
     float4_t acc[NT], accm = {0.f, 0.f, 0.f, 0.f};
-    float ref = -INFINITY, limit = -INFINITY, l_run = 0.f, over = 7.f, back = 4.f;       // limit: (ref + over) in units of the scores before cs
+    float ref = -INFINITY, limit = -INFINITY, l_run = 0.f;               // limit: (ref + kOver) in units of the scores before cs
+    float lift = 16777216.f;                         // of group r / 4 (CG > 1: the lane's own); the smallest scale above 0 is 2^-24
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
     auto rescale = [&](float ref_new) {
         const float alpha = ref == ref_new ? 1.f : __builtin_amdgcn_exp2f(ref - ref_new);
         l_run *= alpha;
         ref = ref_new;
-        limit = (ref_new + over) / cs;
+        limit = (ref_new + kOver) / cs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float al = __shfl(alpha, 4 * g + i);                   // accumulator rows are the score columns 4 g + i
@@ -326,6 +330,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
 
         // ---- weights in place of scores, and their sums with the offsets
         Frag8 vm;                                    // offsets as an operand: column 4 c is group c (CG > 1: column r is group r % CG)
+        constexpr int VS = CG == 1 ? 1 : 4;
+        float vs[2][VS];                             // the values' scales, lifted
         bool large = false;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -333,33 +339,56 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
                 const uint32_t e0 = vsm[u][0], e1 = row_ahead<1>(e0), e2 = row_ahead<2>(e0), e3 = row_ahead<3>(e0);
                 vm.w[2 * u] = __builtin_amdgcn_perm(e1, e0, 0x07060302u);
                 vm.w[2 * u + 1] = __builtin_amdgcn_perm(e3, e2, 0x07060302u);
-                large |= sm_scale(e0) > 511.f;
             } else {
                 vm.w[2 * u] = __builtin_amdgcn_perm(vsm[u][1], vsm[u][0], 0x07060302u);
                 vm.w[2 * u + 1] = __builtin_amdgcn_perm(vsm[u][3], vsm[u][2], 0x07060302u);
+            }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) large |= sm_scale(vsm[u][i]) > 511.f;
+            for (int i = 0; i < VS; ++i) {
+                vs[u][i] = sm_scale(vsm[u][i]) * lift;
+                large |= vs[u][i] >= 2.f;
             }
         }
-        if (over > 0.f && __any(large)) {
-            large = false;                           // of tokens of the sequence: what lies behind them is someone else's and changes nothing
+        if (__any(large)) {
+            float top = 0.f;                         // of tokens of the sequence: what lies behind them is someone else's and changes nothing
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int here = len + nr - (p + u) * kPageSize - 4 * g;
-                if constexpr (CG == 1) large |= sm_scale(vsm[u][0]) > 511.f && (r & 3) < here;
-                else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) large |= sm_scale(vsm[u][i]) > 511.f && i < here;
-                }
+                for (int i = 0; i < VS; ++i) top = fmaxf(top, (CG == 1 ? (r & 3) : i) < here ? sm_scale(vsm[u][i]) : 0.f);
             }
-            if (__any(large)) {
-                over = -1.f;
-                back = -4.f;
-                rescale(ref + 8.f);
+            if constexpr (CG == 1) {
+                top = fmaxf(top, __shfl_xor(top, 1));
+                top = fmaxf(top, __shfl_xor(top, 2));
             }
+            top = max_over_rows(top);
+            const int want = (127 - (int)(__float_as_uint(top) >> 23)) & ~3;     // exponent: top 2^want in [1/8, 2) (top = 0: large, lift stays)
+            const float to = fminf(lift, __uint_as_float((unsigned)(127 + min(want, 24)) << 23));
+            const float ratio = __uint_as_float(__float_as_uint(to) - __float_as_uint(lift) + 0x3F800000u);
+            lift = to;
+            if (p >= p0 + kStep) {                   // (else nothing has been summed)
+                if constexpr (CG == 1)
+                    static_for<0, NG>([&](auto ci) {
+                        constexpr int c = decltype(ci)::value;
+                        const float al = row_lane<4 * c>(ratio);
+                        acc[2 * c] *= al;
+                        acc[2 * c + 1] *= al;
+                    });
+                else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float al = __shfl(ratio, 4 * g + i);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) acc[n][i] *= al;
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < VS; ++i) vs[u][i] = sm_scale(vsm[u][i]) * lift;
         }
         const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-        if (__any(mx > limit)) rescale(fmaxf(ref, max_over_rows(mx) * cs - back));
+        if (__any(mx > limit)) rescale(fmaxf(ref, max_over_rows(mx) * cs - kBack));
         const float mu = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -382,8 +411,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
             float ps[8];
             static_for<0, 8>([&](auto ii) {
                 constexpr int i = decltype(ii)::value;
-                if constexpr (CG == 1) ps[i] = row_lane<c * 4 + i % 4>(sm_scale(vsm[i / 4][0])) * s[i];
-                else ps[i] = sm_scale(vsm[i / 4][i % 4]) * s[i];
+                if constexpr (CG == 1) ps[i] = row_lane<c * 4 + i % 4>(vs[i / 4][0]) * s[i];
+                else ps[i] = vs[i / 4][i % 4] * s[i];
             });
             pv = pack8(ps);
             if constexpr (kTwoP) {
@@ -418,14 +447,17 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     float* const res = reinterpret_cast<float*>(mine);
     const float l = sum_over_rows(l_run);
     if (g == 0 && cc == 0) { sm_m[wave][j] = ref; sm_l[wave][j] = l; }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
+    const float unlift = __uint_as_float(0x7F000000u - __float_as_uint(lift));           // 1 / lift
+    static_for<0, NT>([&](auto ni) {
+        constexpr int n = decltype(ni)::value, at = (CG == 1 ? 4 : 1) * (n / 2);         // of group n / 2 in a row of lanes
+        const float unit = row_lane<at>(unlift) * (n & 1 ? kCodeUnit / 16.f : kCodeUnit);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (CG == 1 || i % CG == n / 2) {    // (row 4 g + i is group i % CG of query row (4 g + i) / CG)
-                const float om = __shfl(accm[i], 16 * g + (CG == 1 ? 4 : 1) * (n / 2));
-                res[(4 * g + i) / CG * kStride + 16 * n + r] = fmaf(acc[n][i], n & 1 ? kCodeUnit / 16.f : kCodeUnit, om);
+                const float om = __shfl(accm[i], 16 * g + at);
+                res[(4 * g + i) / CG * kStride + 16 * n + r] = fmaf(acc[n][i], unit, om);
             }
+    });
     __syncthreads();
     for (int idx = threadIdx.x; idx < J * DH / 4; idx += kWaves * 64) {
         const int row = idx / (DH / 4), c = idx % (DH / 4) * 4;

@@ -1,0 +1,82 @@
+"""Attention over a 4-bit cache where the sizes of values, weights and queries are far apart."""
+import math
+
+import pytest
+import torch
+
+import paper_2408_05676_amd as laser
+from tests import four_bit_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+def normal(gen, *dims):
+    return torch.empty(dims, device="cuda").normal_(0, 1, generator=gen)
+
+
+def attend(q, k, v, scale, dtype):
+    """q [Hq][dh], k, v [T][H][dh] float64: what one row that sees all tokens gets, and how far a result in dtype may be off it.
+
+    Weights times scales, and weights, are rounded to fp16 (half a step 2^-11; in two planes, where dtype is not bfloat16, 2^-21): that part of
+    sum(p (s c + |m|)) / sum(p). What fp16 rounds to 0 is 2^-25 at most of a weight whose largest is 2^11 or more, times a scale whose
+    largest in its group is 1/8 or more and codes up to 15, and of a weight times an offset: T 2^-33 (15 s + |m|), the largest of the channel's
+    group. Scores are fp32 sums of under 2^6 roundings of terms |q| (s c + |m|): 2^-18 of these, to the result as twice that relative change of the weights."""
+    (c, s, m), T = ref.quantize(v, 32), v.shape[0]
+    held_v, span = ref.values(c, s, m), ref.values(c, s, m.abs())
+    most = (15 * s.double() + m.double().abs()).amax(0).repeat_interleave(32, -1)           # [H][dh]
+    held_k, k_span = ref.held(k), ref.spans(k)
+    G, out, tol = q.shape[0] // k.shape[1], torch.empty_like(q), torch.empty_like(q)
+    for h in range(q.shape[0]):
+        x = held_k[:, h // G] @ q[h] * scale
+        p = (x - x.max()).exp()
+        p = p / p.sum()
+        out[h] = p @ held_v[:, h // G]
+        delta = 2.0 ** -18 * abs(scale) * float((k_span[:, h // G] @ q[h].abs()).max())
+        tol[h] = ((2.0 ** -11 if dtype == BF16 else 2.0 ** -21) + 2 * delta) * (p @ span[:, h // G]) + T * 2.0 ** -33 * most[h // G]
+    tol = tol + ref.EPS[dtype] * (out.abs() + tol) + (2.0 ** -25 if dtype == F16 else 0)
+    return out, tol
+
+
+def one_row(k, v, q, scale, dtype):
+    """q's single row behind T - 1 imported tokens and one appended."""
+    T, H, dh = k.shape
+    kv = laser.KVCache4(1, H, dh, -(-T // 16), 1, -(-T // 16))
+    kv.reserve(0, T)
+    kv.import_layer(0, 0, k[:-1].half().contiguous(), v[:-1].half().contiguous())
+    kv.set_len(0, T - 1)
+    laser.kv_append(kv, 0, [0], k[None, -1:], v[None, -1:])
+    got = laser.kv_attend(kv, 0, [0], q[None, None].to(dtype), scale=scale)[0, 0].double()
+    want, tol = attend(q.to(dtype).double(), k.double(), v.double(), scale, dtype)
+    err = (got - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+@pytest.mark.parametrize("T, dh, G", [(12000, 64, 2), (12000, 128, 8), (30000, 128, 1), (65000, 128, 4)])
+@pytest.mark.parametrize("sigma", [1.0, 1e-3, 1e-4])
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_a_tail_of_small_weights_keeps_its_share(T, dh, G, sigma, dtype):
+    """One token's score is some 11 above the others', which together weigh about as much: their values must not be lost, however small."""
+    gen = torch.Generator(device="cuda").manual_seed(T + G)
+    base = normal(gen, dh)
+    q = base + 0.05 * normal(gen, 2 * G, dh)
+    k, v = 0.02 * normal(gen, T, 2, dh), sigma * (normal(gen, T, 2, dh) + 0.5)
+    k[0] = base * (11 * math.sqrt(dh) / float(base @ base))
+    one_row(k.half().float(), v.half().float(), q, dh ** -0.5, dtype)
+
+
+@pytest.mark.parametrize("dh, G", [(64, 1), (128, 4), (128, 8)])
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("first", [1e-4, 60000.0])
+def test_groups_of_very_different_sizes(dh, G, dtype, first):
+    """Scales of one group grow or shrink by orders along the context, those of the others stay small: each group keeps its precision."""
+    gen = torch.Generator(device="cuda").manual_seed(dh + G)
+    T = 12000
+    base = normal(gen, dh)
+    q = base + 0.05 * normal(gen, 2 * G, dh)
+    k, v = 0.02 * normal(gen, T, 2, dh), 1e-4 * normal(gen, T, 2, dh)
+    k[5] = base * (9 * math.sqrt(dh) / float(base @ base))
+    v[:, :, :32] = normal(gen, T, 2, 32).clamp(-1, 1)
+    v[:, :, :32] *= torch.logspace(math.log10(first), math.log10(6.0 / first), T, device="cuda")[:, None, None]
+    one_row(k.half().float(), v.half().float(), q, dh ** -0.5, dtype)
