@@ -290,7 +290,7 @@ int laser_kv_append(laser_kv* kv, int layer, const int32_t* seq_ids, const int32
  * slots 0..len-1 and, of its own step's slots len..len+R-1 (laser_kv_append), to itself and its ancestors (tree_parent; NULL: rows 0..r).
  * n_heads query heads, a multiple of the cache's: query head j uses key/value head j / (n_heads / cache heads).
  * Other arguments as for laser_kv_append; rows beyond n_rows are left as they are. out has q's type and is q itself or memory that does not overlap it. Sums, softmax and
- * scores are fp32. Contexts are split over workgroups by the host's bounds of len: results may differ in the last bits between launches
+ * scores are fp32: a row with a score that fp32 does not hold becomes NaN. Contexts are split over workgroups by the host's bounds of len: results may differ in the last bits between launches
  * whose bounds differ, and are the same for the same ones. Uses the handle's workspace. */
 int laser_kv_attend(laser_kv* kv, int layer, const int32_t* seq_ids, const int32_t* n_rows, const int32_t* tree_parent, int B, int R,
                     int n_heads, int dtype, const laser_heads* q, float scale, const laser_heads* out, void* stream);

@@ -442,7 +442,7 @@ extern "C" int laser_kv_attend(laser_kv* h, int layer, const int32_t* seq_ids, c
     if ((rc = check_heads(q, "q", dtype)) || (rc = check_heads(out, "out", dtype))) return rc;
     LASER_REQUIRE(n_heads > 0 && n_heads % kv->d.n_heads == 0, LASER_E_SHAPE, "n_heads %d is not a multiple of the cache's %d", n_heads, kv->d.n_heads);
     LASER_REQUIRE(n_heads / kv->d.n_heads <= 256, LASER_E_LIMIT, "more than 256 query heads per key/value head");
-    LASER_REQUIRE(std::isfinite(scale), LASER_E_INVALID_ARG, "scale is not finite");
+    LASER_REQUIRE(std::isfinite(scale * 1.44269504f), LASER_E_INVALID_ARG, "scale is not finite, or too large");
     for (int b0 = 0; b0 < B; b0 += kSeqChunk) {
         AttendArgs a{};
         a.B = std::min(kSeqChunk, B - b0);

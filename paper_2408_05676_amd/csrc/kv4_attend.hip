@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     }
     mx = max_over_rows(mx);
     int e = 0;
-    if (mx > 0.f && mx < INFINITY) { (void)frexpf(mx, &e); e = min(max(15 - e, -80), 100); }
+    if (mx > 0.f && mx < INFINITY) { (void)frexpf(mx, &e); e = min(15 - e, 100); }
     const float up = ldexpf(a.scale_log2 < 0.f ? -1.f : a.scale_log2 > 0.f ? 1.f : 0.f, e);
     Frag8 ones;
 #pragma unroll
@@ -206,7 +206,14 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
         const half2_t two = {hi, (_Float16)(own - (float)hi)};
         qsum.v4 = u32x4{__builtin_bit_cast(uint32_t, two), 0u, 0u, 0u};
     }
-    const float cs = a.scale_log2 == 0.f ? 1.f : fmaxf(ldexpf(fabsf(a.scale_log2) * (CG == 1 ? 1.f / kSumUnit : kCodeUnit), -e), 1e-37f);
+    // (queries near the largest fp32 numbers: a power of two that cs cannot hold waits in sm_l)
+    int se = 0;
+    (void)frexpf(a.scale_log2, &se);
+    const int sh = (CG == 1 ? 8 : 24) - e, beyond = max(0, se + sh - 120);
+    const float cs = a.scale_log2 == 0.f ? 1.f : fmaxf(ldexpf(fabsf(a.scale_log2), sh - beyond), 1e-37f);
+    const bool huge = __any(beyond > 0);
+    if (huge && g == 0 && cc == 0) sm_l[wave][j] = ldexpf(1.f, min(beyond, 127));
+
 
     // ---- the walk. Weights are p = 2^(score - ref); ref moves, and what was summed with it, when a score passes it by more than kOver,
     // and is then set to kBack below the row's largest score: a row's largest p is 2^11 to 2^14. Values' scales are multiplied by `lift`, a power of
@@ -216,6 +223,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     constexpr float kOver = 14.f, kBack = 11.f;
     float4_t acc[NT], accm = {0.f, 0.f, 0.f, 0.f};
     float ref = -INFINITY, limit = -INFINITY, l_run = 0.f;               // limit: (ref + kOver) in units of the scores before cs
+    bool far = false;                                // some row's reference is so large that fp32 holds it to 2^-7 or less: see below
     float lift = 16777216.f;                         // of group r / 4 (CG > 1: the lane's own); the smallest scale above 0 is 2^-24
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = float4_t{0.f, 0.f, 0.f, 0.f};
@@ -223,6 +231,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
         const float alpha = ref == ref_new ? 1.f : __builtin_amdgcn_exp2f(ref - ref_new);
         l_run *= alpha;
         ref = ref_new;
+        far = __any(fabsf(ref_new) > 131072.f && ref_new != -INFINITY);
         limit = (ref_new + kOver) / cs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -312,20 +321,26 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
                 for (int i = 0; i < 4; ++i) s[4 * u + i] = sum_over_groups<CG>(fmaf(sm_scale(ksm[u][i]), d[i], sm_offset(ksm[u][i]) * qs));
             }
         }
-        if ((p + 2) * kPageSize > len) {             // slots behind the committed ones: along the row's own branch only
+        const bool tail = (p + 2) * kPageSize > len;
+        if (tail || huge || p + 1 >= p1) {
+            if (huge)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                // the lane's four slots start rel behind the committed length: bits rel .. rel + 3 of the row's mask, ones below 0
-                const int rel = p + u < p1 ? (p + u) * kPageSize + 4 * g - len : 64;
-                const int up = min(max(rel, 0), 63), under = min(max(-rel, 0), 4);
-                const unsigned ahead = rel < 64 ? (unsigned)(anc >> up) : 0u, behind = ((unsigned)anc << under) | ((1u << under) - 1u);
-                const unsigned seen = rel >= 0 ? ahead : behind;
+                for (int i = 0; i < 8; ++i) s[i] *= sm_l[wave][j];
+            if (tail) {                              // slots behind the committed ones: along the row's own branch only
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * u + i] = (seen >> i) & 1u ? s[4 * u + i] : -INFINITY;
+                for (int u = 0; u < 2; ++u) {
+                    // the lane's four slots start rel behind the committed length: bits rel .. rel + 3 of the row's mask, ones below 0
+                    const int rel = p + u < p1 ? (p + u) * kPageSize + 4 * g - len : 64;
+                    const int up = min(max(rel, 0), 63), under = min(max(-rel, 0), 4);
+                    const unsigned ahead = rel < 64 ? (unsigned)(anc >> up) : 0u, behind = ((unsigned)anc << under) | ((1u << under) - 1u);
+                    const unsigned seen = rel >= 0 ? ahead : behind;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[4 * u + i] = (seen >> i) & 1u ? s[4 * u + i] : -INFINITY;
+                }
+            } else if (p + 1 >= p1) {                // an odd number of pages
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 + i] = -INFINITY;
             }
-        } else if (p + 1 >= p1) {                    // an odd number of pages
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[4 + i] = -INFINITY;
         }
 
         // ---- weights in place of scores, and their sums with the offsets
@@ -388,11 +403,21 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
                 for (int i = 0; i < VS; ++i) vs[u][i] = sm_scale(vsm[u][i]) * lift;
         }
         const float mx = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-        if (__any(mx > limit)) rescale(fmaxf(ref, max_over_rows(mx) * cs - kBack));
-        const float mu = ref == -INFINITY ? 0.f : ref;
+        if (far || __any(mx > limit)) {
+            if (__any(mx > limit)) rescale(fmaxf(ref, max_over_rows(mx) * cs - kBack));
+            if (far) {                               // ref was rounded: the scores against it must be too, and stay within fp16
+#pragma clang fp contract(off)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x = s[i] * cs, t = x - (ref == -INFINITY ? 0.f : ref);
+                    s[i] = t > kOver ? kOver : t;    // (NaN stays)
+                }
+            }
+        }
+        const float mu = far || ref == -INFINITY ? 0.f : ref, unit = far ? 1.f : cs;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], cs, -mu));
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], unit, -mu));
             l_run += s[i];
         }
         const Frag8 ph = pack8(s);

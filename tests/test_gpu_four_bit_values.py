@@ -80,3 +80,45 @@ def test_groups_of_very_different_sizes(dh, G, dtype, first):
     v[:, :, :32] = normal(gen, T, 2, 32).clamp(-1, 1)
     v[:, :, :32] *= torch.logspace(math.log10(first), math.log10(6.0 / first), T, device="cuda")[:, None, None]
     one_row(k.half().float(), v.half().float(), q, dh ** -0.5, dtype)
+
+
+@pytest.mark.parametrize("dtype, size, scale", [
+    (F16, 6e4, 1.0), (F16, 6e4, -0.1), (BF16, 1e9, 0.1), (BF16, 2.0 ** 95, 0.1), (BF16, 1e36, 0.1), (BF16, 1e36, -1e-3), (F32, 3e7, 1.0), (F32, 1e9, 1.0),
+    (F32, 2.0 ** 95, 0.1), (F32, 3e36, 0.1), (F32, 3e37, -1e-3), (F32, 1e30, 1e6), (F32, 1.0, 1e30)])
+@pytest.mark.parametrize("dh, G", [(64, 1), (64, 8), (128, 2), (128, 8)])
+def test_scores_far_beyond_what_fp32_holds_to_a_unit(dtype, size, scale, dh, G):
+    """The largest score wins by more than its own rounding: its token's value comes out, whatever the size of the queries."""
+    gen = torch.Generator(device="cuda").manual_seed(dh + G)
+    T, H = 700, 2
+    base = normal(gen, dh)
+    q = ((base + 0.01 * normal(gen, H * G, dh)).clamp(-3, 3) / 4 * size).to(dtype)
+    big = 2e4 if dtype == F16 else 1.0
+    k, v = big * 0.05 * normal(gen, T, H, dh), normal(gen, T, H, dh)
+    k[:, 1] = k[:, 0]
+    k[345] = big * base * (1 if scale > 0 else -1)
+    k = k.half().float()
+    # the gap: more than 2^-8 of the sum of the terms' sizes, of which fp32 loses 2^-18
+    held, span = ref.held(k), ref.spans(k)
+    for h in range(H * G):
+        x = held[:, h // G] @ q[h].double() * scale
+        top = x.sort(descending=True).values
+        assert int(x.argmax()) == 345 and float(top[0] - top[1]) > max(60.0, 2.0 ** -8 * abs(scale) * float((span[:, h // G] @ q[h].double().abs()).max()))
+    kv = laser.KVCache4(1, H, dh, 44, 1, 44)
+    kv.reserve(0, T)
+    kv.import_layer(0, 0, k[:-1].half().contiguous(), v[:-1].half().contiguous())
+    kv.set_len(0, T - 1)
+    laser.kv_append(kv, 0, [0], k[None, -1:], v[None, -1:])
+    got = laser.kv_attend(kv, 0, [0], q[None, None], scale=scale)[0, 0].double()
+    c, s, m = ref.quantize(v.half().double(), 32)
+    want, size_v = ref.values(c, s, m)[345].repeat_interleave(G, 0), ref.values(c, s, m.abs())[345].repeat_interleave(G, 0)
+    tol = (2.0 ** -11 if dtype == BF16 else 2.0 ** -21) * size_v
+    assert bool(((got - want).abs() <= tol + ref.EPS[dtype] * (want.abs() + tol)).all()), (got - want).abs().max()
+
+
+def test_scales_that_fp32_does_not_hold_in_units_of_log_2():
+    kv = laser.KVCache4(1, 1, 64, 1, 1, 1)
+    kv.reserve(0, 16)
+    q = torch.zeros((1, 1, 1, 64), device="cuda")
+    laser.kv_append(kv, 0, [0], q, q)
+    with pytest.raises(laser.LaserError, match="scale"):
+        laser.kv_attend(kv, 0, [0], q, scale=3e38)
