@@ -261,7 +261,8 @@ int laser_kv_create_4bit(const laser_kv_desc* desc, void* stream, laser_kv** out
 #define LASER_F32  2
 
 /* Keys, values, queries or results of B sequences with R rows each: [dev] element (b, r, h, c) lies at
- * data + b * seq + r * row + h * head + c (strides in elements, >= 0). Needs the alignment of its elements only. */
+ * data + b * seq + r * row + h * head + c (strides in elements, >= 0). Needs the alignment of its elements only. Inputs may be
+ * broadcast (stride 0); results of which two heads share memory are refused. */
 typedef struct laser_heads { void* data; int64_t seq, row, head; } laser_heads;
 
 /* laser_rope_table: table [dev] float[max_pos][rope_dim / 2][2] = (cos, sin) of position * base^(-2 i / rope_dim), angles in 64 bits. */

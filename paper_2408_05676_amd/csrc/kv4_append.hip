@@ -8,6 +8,8 @@
 // a token's codes of a head lie in 64 places (four_bit.h). 64 tokens of 32 + 32 heads of 128 6.8 us (1.7 MB), 1024 rows of 8 + 32 heads 12.2 us (20 MB);
 // with all of a head's channels in four threads, keys and values one after the other, 11.3 and 24.4. Reading back 4.3 and 4.7.
 #include <algorithm>
+#include <utility>
+#include <vector>
 
 #include "four_bit.h"
 
@@ -343,6 +345,31 @@ static int check_heads(const laser_heads* t, const char* name, int dtype) {
     return LASER_OK;
 }
 
+// Results: no two heads of dh elements may share memory.
+static int check_apart(const laser_heads* t, const char* name, long B, long R, long H, int dh) {
+    std::pair<int64_t, long> dims[3] = {{t->seq, B}, {t->row, R}, {t->head, H}};
+    std::sort(dims, dims + 3);
+    int64_t extent = dh;                                                 // of what the strides so far reach over
+    bool nested = true;
+    for (const auto& [stride, n] : dims) {
+        if (n <= 1) continue;
+        nested &= stride >= extent;
+        extent += stride * (n - 1);
+    }
+    if (nested) return LASER_OK;
+    std::vector<int64_t> at;                                             // strides that interleave: by looking
+    if (B * R * H <= 1l << 22) {
+        for (long b = 0; b < B; ++b)
+            for (long r = 0; r < R; ++r)
+                for (long h = 0; h < H; ++h) at.push_back(b * t->seq + r * t->row + h * t->head);
+        std::sort(at.begin(), at.end());
+    }
+    bool apart = !at.empty();
+    for (size_t i = 1; i < at.size(); ++i) apart &= at[i] - at[i - 1] >= dh;
+    LASER_REQUIRE(apart, LASER_E_INVALID_ARG, "%s: rows or heads overlap (strides %lld, %lld, %lld)", name, (long long)t->seq, (long long)t->row, (long long)t->head);
+    return LASER_OK;
+}
+
 static Heads heads_from(const laser_heads* t, int b0, int dtype) {
     if (!t || !t->data) return Heads{nullptr, 0, 0, 0};
     return Heads{(char*)t->data + (size_t)b0 * t->seq * dtype_bytes(dtype), t->seq, t->row, t->head};
@@ -404,7 +431,7 @@ extern "C" int laser_kv_append(laser_kv* h, int layer, const int32_t* seq_ids, c
     if (B == 0) return LASER_OK;
     if ((rc = check_heads(k, "k", dtype)) || (rc = check_heads(v, "v", dtype))) return rc;
     LASER_REQUIRE(n_heads >= 0 && n_heads <= (1 << 20), LASER_E_INVALID_ARG, "n_heads %d out of range", n_heads);
-    if (n_heads > 0 && ((rc = check_heads(q, "q", dtype)) || (rc = check_heads(q_out, "q_out", dtype)))) return rc;
+    if (n_heads > 0 && ((rc = check_heads(q, "q", dtype)) || (rc = check_heads(q_out, "q_out", dtype)) || (rc = check_apart(q_out, "q_out", B, R, n_heads, kv->d.head_dim)))) return rc;
     const int dh = kv->d.head_dim;
     LASER_REQUIRE(rope_dim == 0 || rope_dim == dh || (rope_dim == 64 && dh == 128), LASER_E_SHAPE, "rope_dim %d: 0, 64 or head_dim", rope_dim);
     if (rope_dim) {
@@ -441,6 +468,7 @@ extern "C" int laser_kv_attend(laser_kv* h, int layer, const int32_t* seq_ids, c
     if (B == 0) return LASER_OK;
     if ((rc = check_heads(q, "q", dtype)) || (rc = check_heads(out, "out", dtype))) return rc;
     LASER_REQUIRE(n_heads > 0 && n_heads % kv->d.n_heads == 0, LASER_E_SHAPE, "n_heads %d is not a multiple of the cache's %d", n_heads, kv->d.n_heads);
+    if ((rc = check_apart(out, "out", B, R, n_heads, kv->d.head_dim))) return rc;
     LASER_REQUIRE(n_heads / kv->d.n_heads <= 256, LASER_E_LIMIT, "more than 256 query heads per key/value head");
     LASER_REQUIRE(std::isfinite(scale * 1.44269504f), LASER_E_INVALID_ARG, "scale is not finite, or too large");
     for (int b0 = 0; b0 < B; b0 += kSeqChunk) {
@@ -475,6 +503,9 @@ extern "C" int laser_kv_read(laser_kv* h, int layer, const int32_t* seq_ids, int
     }
     if (B == 0 || n == 0) return LASER_OK;
     if ((rc = check_heads(k, "k", dtype)) || (rc = check_heads(v, "v", dtype))) return rc;
+    const int H = kv->d.n_heads, dh = kv->d.head_dim;
+    if ((rc = check_apart(k, "k", B, n, H, dh)) || (rc = check_apart(v, "v", B, n, H, dh))) return rc;
+    LASER_REQUIRE(k->data != v->data, LASER_E_INVALID_ARG, "k and v are the same memory");
     for (int b0 = 0; b0 < B; b0 += kSeqChunk) {
         ReadArgs a{};
         a.B = std::min(kSeqChunk, B - b0);
