@@ -8,6 +8,7 @@ import ctypes as C
 from array import array
 import sys
 import os
+import weakref
 
 import numpy as np
 import torch
@@ -240,7 +241,7 @@ class Model:
                  max_pos: int, eps: float = 1e-6, rope_base: float = 10000.0, stream=None):
         self.n_layers, self.d, self.n_heads, self.ffn, self.vocab = n_layers, d_model, n_heads, ffn, vocab
         self.max_rows, self.max_batch = max_rows, max_batch
-        self._keep = dict(weights)
+        self._keep, self._w4 = dict(weights), set()
         d = _ModelDesc(n_layers, d_model, n_heads, ffn, vocab, max_rows, max_batch, max_pos, eps, rope_base)
         for name in ("wqkv", "wo", "wgu", "wdown", "emb", "wlm"):
             t = weights.get(name)
@@ -256,6 +257,7 @@ class Model:
                     continue
                 raise LaserError(f"missing weight {name}")
             setattr(d, name, _dev(t, torch.float32, name))
+        self.device = weights["wlm"].get_device()
         self._h = C.c_void_p()
         _check(lib().laser_model_create(C.byref(d), _stream(stream), C.byref(self._h)), "laser_model_create")
 
@@ -263,10 +265,20 @@ class Model:
         _check(lib().laser_model_set_option(self._h, name.encode(), value), "laser_model_set_option")
 
     def set_w4(self, layer: int, name: str, w4) -> None:
-        """laser_model_set_w4: name is wqkv, wo, wgu or wdown, w4 a W4 (kept alive by this object) or None."""
-        which = ("wqkv", "wo", "wgu", "wdown").index(name)
-        _check(lib().laser_model_set_w4(self._h, layer, which, w4._h if w4 is not None else None), "laser_model_set_w4")
-        self._keep[layer, which] = w4
+        """laser_model_set_w4: name is wqkv, wo, wgu or wdown, w4 a W4 or None. A W4 is kept alive until this object is closed, also after
+        another has taken its place: a captured graph may still read it."""
+        names = ("wqkv", "wo", "wgu", "wdown")
+        if name not in names:
+            raise LaserError(f"no matrix {name!r}: {', '.join(names)}")
+        if w4 is not None:
+            if not isinstance(w4, W4) or not w4._h:
+                raise LaserError("w4 must be a W4 that has not been closed, or None")
+            if w4.device != self.device:
+                raise LaserError(f"the matrix is on device {w4.device}, the model on {self.device}")
+        _check(lib().laser_model_set_w4(self._h, layer, names.index(name), w4._h if w4 is not None else None), "laser_model_set_w4")
+        if w4 is not None:
+            self._w4.add(w4)
+            w4._models.add(self)
 
     def aborted(self, stream=None) -> bool:
         v = C.c_int()
@@ -293,6 +305,7 @@ class Model:
         if getattr(self, "_h", None) is not None and self._h:
             lib().laser_model_destroy(self._h)
             self._h = C.c_void_p()
+            self._w4.clear()
 
     def __del__(self):
         # at interpreter shutdown the HIP runtime may already be gone; the process frees everything
@@ -515,7 +528,7 @@ class W4:
     """laser_w4_create / laser_w4_destroy: a matrix of 4-bit weights laid out for w4_matmul (see laser.h for the three arrays)."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, offsets: torch.Tensor, stream=None):
-        self._h = C.c_void_p()
+        self._h, self._models = C.c_void_p(), weakref.WeakSet()
         if codes.dim() != 2 or scales.dim() != 2 or scales.shape != offsets.shape or scales.shape[0] != codes.shape[0] or not scales.shape[1]:
             raise LaserError("codes must be [N][Kd / 2], scales and offsets [N][Kd / group]")
         for t, n in ((codes, "codes"), (scales, "scales"), (offsets, "offsets")):
@@ -530,6 +543,11 @@ class W4:
                                      self.N, self.Kd, self.group, _stream(stream), C.byref(self._h)), "laser_w4_create")
 
     def close(self):
+        if any(m._h for m in getattr(self, "_models", ())):
+            raise LaserError("the matrix is in use by a model: close that first")
+        self._free()
+
+    def _free(self):
         if getattr(self, "_h", None) is not None and self._h:
             lib().laser_w4_destroy(self._h)
             self._h = C.c_void_p()
@@ -537,7 +555,7 @@ class W4:
     def __del__(self):
         # at interpreter shutdown the HIP runtime may already be gone; the process frees everything
         if not sys.is_finalizing():
-            self.close()
+            self._free()
 
 
 def w4_matmul(w: W4, x: torch.Tensor, out=None, stream=None) -> torch.Tensor:

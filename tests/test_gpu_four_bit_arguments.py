@@ -63,3 +63,43 @@ def test_keys_read_into_the_memory_of_the_values(step):
     t = torch.zeros((2, 3, 2, 64), dtype=F16, device="cuda")
     with pytest.raises(laser.LaserError, match="same memory"):
         laser.kv_read(kv, 0, [0, 1], 3, out=(t, t))
+
+
+def test_matrices_of_a_model(monkeypatch):
+    import gc
+    import weakref
+
+    import synth
+    from tests.gpu_util import gpu_weights
+    sh = synth.SHAPES["tiny"]
+    w = gpu_weights(sh)
+    model = laser.Model(sh.n_layers, sh.d, sh.n_heads, sh.ffn, sh.vocab, w, 4, 1, 64, eps=sh.eps, rope_base=sh.rope_base)
+    make = lambda: laser.W4(*laser.w4_quantize(w["wo"][0].contiguous(), 64))  # noqa: E731
+    closed, first, second = make(), make(), make()
+    closed.close()
+    with pytest.raises(laser.LaserError, match="closed"):            # not the bf16 matrix in silence
+        model.set_w4(0, "wo", closed)
+    with pytest.raises(laser.LaserError, match="closed"):
+        model.set_w4(0, "wo", w["wo"][0])
+    with pytest.raises(laser.LaserError, match="wq"):
+        model.set_w4(0, "wq", first)
+    monkeypatch.setattr(second, "device", 1)
+    with pytest.raises(laser.LaserError, match="device"):
+        model.set_w4(0, "wo", second)
+    monkeypatch.undo()
+    model.set_w4(0, "wo", first)
+    with pytest.raises(laser.LaserError, match="in use"):
+        first.close()
+    model.set_w4(0, "wo", second)
+    alive = weakref.ref(first)
+    del first
+    gc.collect()
+    assert alive() is not None and alive()._h                        # a captured step may read it
+    model.set_w4(0, "wo", None)
+    with pytest.raises(laser.LaserError, match="in use"):
+        second.close()
+    model.close()
+    gc.collect()
+    assert alive() is None
+    second.close()
+    second.close()
