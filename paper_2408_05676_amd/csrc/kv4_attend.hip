@@ -429,6 +429,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
             accm = mfma_16x16x32(pack8(lo), vm, accm);
         }
 
+        // (kTwoP: all codes in bits 4..7, see four_bit.h: as bits 0..3 they cost the sums 2^-20, and a result is the small difference of two
+        // such sums: one row behind 65000 tokens came out three times as far off the formula as one rounding)
         // ---- values: operand fragments of tokens 4 g .. 4 g + 3 of both pages, p s of the group (CG > 1: of the lane's own) against them
         Frag8 pv, pl;
         auto weigh = [&](auto ci) {
@@ -454,8 +456,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint32_t a0 = vw[u][c], a1 = a0 >> 8;
-                va.w[2 * u] = a0 & kCodeLo;
-                va.w[2 * u + 1] = a1 & kCodeLo;
+                va.w[2 * u] = kTwoP ? (a0 << 4) & kCodeHi : a0 & kCodeLo;
+                va.w[2 * u + 1] = kTwoP ? (a0 >> 4) & kCodeHi : a1 & kCodeLo;
                 vb.w[2 * u] = a0 & kCodeHi;
                 vb.w[2 * u + 1] = a1 & kCodeHi;
             }
@@ -475,7 +477,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     const float unlift = __uint_as_float(0x7F000000u - __float_as_uint(lift));           // 1 / lift
     static_for<0, NT>([&](auto ni) {
         constexpr int n = decltype(ni)::value, at = (CG == 1 ? 4 : 1) * (n / 2);         // of group n / 2 in a row of lanes
-        const float unit = row_lane<at>(unlift) * (n & 1 ? kCodeUnit / 16.f : kCodeUnit);
+        const float unit = row_lane<at>(unlift) * (kTwoP || n & 1 ? kCodeUnit / 16.f : kCodeUnit);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (CG == 1 || i % CG == n / 2) {    // (row 4 g + i is group i % CG of query row (4 g + i) / CG)

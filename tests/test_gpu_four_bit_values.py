@@ -122,3 +122,38 @@ def test_scales_that_fp32_does_not_hold_in_units_of_log_2():
     laser.kv_append(kv, 0, [0], q, q)
     with pytest.raises(laser.LaserError, match="scale"):
         laser.kv_attend(kv, 0, [0], q, scale=3e38)
+
+
+@pytest.mark.parametrize("B, R, H, G, dh, T", [(1, 1, 2, 4, 128, 65000), (1, 1, 4, 2, 64, 65000), (1, 64, 1, 4, 128, 30000), (2, 40, 2, 4, 64, 8000), (4, 16, 8, 8, 128, 4000)])
+@pytest.mark.parametrize("dtype", [F16, F32])
+def test_sums_over_many_tokens(B, R, H, G, dh, T, dtype):
+    """Values of both signs behind many tokens nearly cancel: codes and offsets must be summed as well as fp32 does. In the mean over the results the error is that of
+    the last rounding, and of the sums no more than 2^-21, four times the largest rounding of a number in fp32, of sum(p (s c + |m|))."""
+    gen = torch.Generator(device="cuda").manual_seed(T + dh)
+    pages = -(-(T + R) // 16)
+    kv = laser.KVCache4(1, H, dh, B * pages, B, pages)
+    q = (normal(gen, B, R, H * G, dh) * (0.5 * normal(gen, H * G, dh)).exp()).to(dtype)
+    nk, nv = normal(gen, B, R, H, dh).half(), normal(gen, B, R, H, dh).half()
+    cached = []
+    for b in range(B):
+        kv.reserve(b, T + R)
+        k, v = (normal(gen, T, H, dh) * (0.5 * normal(gen, H, dh)).exp()).half(), normal(gen, T, H, dh).half()
+        kv.import_layer(b, 0, k, v)
+        kv.set_len(b, T)
+        cached.append((k, v))
+    laser.kv_append(kv, 0, range(B), nk, nv)
+    got = laser.kv_attend(kv, 0, range(B), q).double()
+    err = rounding = sums = 0.0
+    for b in range(B):
+        k, v = (torch.cat([x, y[b]]) for x, y in zip(cached[b], (nk, nv)))
+        (c, s, m), held_k = ref.quantize(v.double(), 32), ref.held(k)
+        held_v, span = ref.values(c, s, m), ref.values(c, s, m.abs())
+        later = torch.arange(T + R, device="cuda")[None, :] > T + torch.arange(R, device="cuda")[:, None]
+        for h in range(H * G):
+            x = (q[b, :, h].double() @ held_k[:, h // G].T * dh ** -0.5).masked_fill(later, -math.inf)
+            p = torch.softmax(x, -1)
+            want = p @ held_v[:, h // G]
+            err += float((got[b, :, h] - want).square().sum())
+            rounding += float((want.to(dtype).double() - want).square().sum())
+            sums += float((p @ span[:, h // G]).square().sum())
+    assert err ** 0.5 <= rounding ** 0.5 + 2.0 ** -21 * sums ** 0.5, (err ** 0.5 / sums ** 0.5, rounding ** 0.5 / sums ** 0.5)
