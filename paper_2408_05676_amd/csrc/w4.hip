@@ -4,8 +4,9 @@
 // hold a matrix operand (lane (r = lane % 16, g = lane / 16): output r, inputs 32 c + 8 g .. + 7 in word c) and the 16 x (128 / group)
 // scales and offsets. A wave streams the blocks of its tiles over its share of the inputs; per group
 //   D = sum c x (matrix instructions on the bare codes), X = sum x (one more, with ones), acc += s D + m X in fp32.
-// Codes enter as 16-bit floats: for fp16 rows a code masked out of its word is the subnormal c 2^-24, for bf16 rows it is put under the
-// exponent of 128 and stands for 128 + c, which the offset m - 128 s takes back.
+// Codes enter as 16-bit floats: for fp16 rows a code masked out of its word is the subnormal c 2^-20 (in bits 0..3, as c 2^-24, an activation 3000 times
+// the others' cost their sum three times the error of fp32 sums: four_bit.h), for bf16 rows it is put under the exponent of 128
+// and stands for 128 + c, which the offset m - 128 s takes back.
 // Bound: up to four rows the weights' way from memory (4096 -> 22016, group 128, one row: 48 MB in 12.0 us, 4.0 TB/s where a long read reaches 5.5);
 // with more rows theirs as well, from L2 once a workgroup (9 rows 13.0 us, 11008 -> 4096 10.1 us); from 17 rows on the matrix and vector
 // instructions of the waves that fit (72 rows 2048 -> 6144 10.3 us, 4096 -> 22016 36 us, 0.36 PFLOP/s).
@@ -135,7 +136,6 @@ __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
     Frag8 ones;
 #pragma unroll
     for (int i = 0; i < 4; ++i) ones.w[i] = BF ? 0x3F803F80u : 0x3C003C00u;
-    constexpr uint32_t kBias = BF ? 0x43004300u : 0u;
 
     float4_t acc[NT][MT];
 #pragma unroll
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         const float sc = sm_scale(smq[s][n]);
-                        ss[n] = BF ? sc : sc * kCodeUnit;
+                        ss[n] = BF ? sc : sc * (kCodeUnit / 16.f);
                         mm[n] = BF ? fmaf(-128.f, sc, sm_offset(smq[s][n])) : sm_offset(smq[s][n]);
                     }
                     static_for<0, NG>([&](auto gg) {
@@ -180,7 +180,8 @@ __global__ __launch_bounds__(WK * 64) void w4_matmul_kernel(W4Args a) {
                             for (int n = 0; n < NT; ++n) {
                                 Frag8 wf;
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) wf.w[j] = ((wq[s][n][c] >> (4 * j)) & kCodeLo) | kBias;
+                                for (int j = 0; j < 4; ++j)
+                                    wf.w[j] = BF ? ((wq[s][n][c] >> (4 * j)) & kCodeLo) | 0x43004300u : (j ? wq[s][n][c] >> (4 * j - 4) : wq[s][n][c] << 4) & kCodeHi;
 #pragma unroll
                                 for (int m = 0; m < MT; ++m) D[n][m] = mfma_x<BF>(wf, xf[m], D[n][m]);
                             }
