@@ -113,6 +113,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     constexpr int NG = DH / 32, NT = DH / 16;        // groups, 16-channel tiles
     constexpr int J = 16 / CG;                       // rows of a tile
     constexpr bool kTwoQ = IN == DT_F32, kTwoP = OUT != DT_BF16;
+    constexpr float kOdd = kTwoP ? 1.f : 16.f, kKeyUnit = kTwoP ? kCodeUnit / 16.f : kCodeUnit;       // of key codes: odd groups against even ones, even ones
     constexpr int kStride = DH + 4;                  // of a row in LDS: four rows apart are sixteen banks apart
     constexpr int kWaveLds = 2 * Ring<DH>::kSlot > J * kStride * 4 ? 2 * Ring<DH>::kSlot : J * kStride * 4;
     __shared__ float sm_m[kWaves][J], sm_l[kWaves][J];
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     // larger); cs > 0 takes scores back to the exponents of 2 (the sign of the scale has gone into the queries)
     Frag8 q[NG], ql[NG];
     Frag8 qsum;                                  // CG = 1, operand of the offsets: first input 8 g is the sum of group g, in two parts
-    constexpr float kUnit = CG == 1 ? kCodeUnit * kSumUnit : 1.f;         // of the keys' scales: scores come in units of kSumUnit, else 2^-24
+    constexpr float kUnit = CG == 1 ? kKeyUnit * kSumUnit : 1.f;          // of the keys' scales: scores come in units of kSumUnit, else 1 / kKeyUnit
     const int pi = min(tile * J + j, P - 1), row = row_of(a, pi), hq = h * a.G + pi - row * a.G;
     const unsigned anc_lo = __shfl((unsigned)anc_l, row), anc_hi = __shfl((unsigned)(anc_l >> 32), row);
     const unsigned long long anc = ((unsigned long long)anc_hi << 32) | anc_lo;
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
 #pragma unroll
     for (int c = 0; c < NG; ++c) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[c][i] *= c & 1 ? up * (1.f / 16.f) : up;
+        for (int i = 0; i < 8; ++i) x[c][i] *= c & 1 ? up / kOdd : up;
         q[c] = pack8(x[c]);
         float4_t sum = mfma_16x16x32(ones, q[c], float4_t{0.f, 0.f, 0.f, 0.f});          // of the lane's query row
         if constexpr (kTwoQ) {
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
             ql[c] = pack8(x[c]);
             sum = mfma_16x16x32(ones, ql[c], sum);
         }
-        if (c == (CG == 1 ? g : cc)) own = sum[0] * ((c & 1 ? 16.f : 1.f) * (CG == 1 ? kSumUnit : 1.f / kCodeUnit));
+        if (c == (CG == 1 ? g : cc)) own = sum[0] * ((c & 1 ? kOdd : 1.f) * (CG == 1 ? kSumUnit : 1.f / kKeyUnit));
         if (CG > 1 && c != cc) {
             q[c].v4 = u32x4{0, 0, 0, 0};
             if constexpr (kTwoQ) ql[c].v4 = u32x4{0, 0, 0, 0};
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     // (queries near the largest fp32 numbers: a power of two that cs cannot hold waits in sm_l)
     int se = 0;
     (void)frexpf(a.scale_log2, &se);
-    const int sh = (CG == 1 ? 8 : 24) - e, beyond = max(0, se + sh - 120);
+    const int sh = (CG == 1 ? 8 : kTwoP ? 20 : 24) - e, beyond = max(0, se + sh - 120);
     const float cs = a.scale_log2 == 0.f ? 1.f : fmaxf(ldexpf(fabsf(a.scale_log2), sh - beyond), 1e-37f);
     const bool huge = __any(beyond > 0);
     if (huge && g == 0 && cc == 0) sm_l[wave][j] = ldexpf(1.f, min(beyond, 127));
@@ -288,8 +289,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
                     const uint32_t a0 = kw[u][c + w], a1 = a0 >> 8;
-                    kf[c].w[2 * w] = a0 & kCodeLo;
-                    kf[c].w[2 * w + 1] = a1 & kCodeLo;
+                    kf[c].w[2 * w] = kTwoP ? (a0 << 4) & kCodeHi : a0 & kCodeLo;
+                    kf[c].w[2 * w + 1] = kTwoP ? (a0 >> 4) & kCodeHi : a1 & kCodeLo;
                     kf[c + 1].w[2 * w] = a0 & kCodeHi;
                     kf[c + 1].w[2 * w + 1] = a1 & kCodeHi;
                 }

@@ -157,3 +157,36 @@ def test_sums_over_many_tokens(B, R, H, G, dh, T, dtype):
             rounding += float((want.to(dtype).double() - want).square().sum())
             sums += float((p @ span[:, h // G]).square().sum())
     assert err ** 0.5 <= rounding ** 0.5 + 2.0 ** -21 * sums ** 0.5, (err ** 0.5 / sums ** 0.5, rounding ** 0.5 / sums ** 0.5)
+
+
+@pytest.mark.parametrize("R", [1, 8])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("size", [1.0, 30.0, 300.0, 3000.0])
+@pytest.mark.parametrize("key", [0.0, 3.0])
+def test_queries_with_one_large_channel(R, dh, size, key):
+    """That channel is nearly the same in all keys and says nothing; the others must not be lost beside it. Values are ones at one token a channel, so that
+    results are weights. In the mean over them scores are off by no more than 2^-21, an eighth of the bound of fp32 sums, of sum(|q| (s c + |m|)).
+    (The large channel's key is held to half a code, so that at 3000 weights reach e^-80: of the row's largest, 2^-33 may be missing anywhere, as in attend.)"""
+    gen = torch.Generator(device="cuda").manual_seed(dh + R)
+    k, v = normal(gen, dh, 1, dh), torch.eye(dh, device="cuda")[:, None]
+    k[:, :, 5] = key * (1 + 0.01 * normal(gen, dh, 1))
+    k = k.half()
+    q = 0.3 * normal(gen, 1, R, 4, dh)
+    q[..., 5] = size
+    q = q.half().float()
+    kv = laser.KVCache4(1, 1, dh, 16, 1, 16)
+    kv.reserve(0, dh + R)
+    kv.import_layer(0, 0, k, v.half().contiguous())
+    kv.set_len(0, dh)
+    zeros = torch.zeros((1, R, 1, dh), device="cuda")
+    laser.kv_append(kv, 0, [0], zeros, zeros)
+    got = laser.kv_attend(kv, 0, [0], q)[0].double()
+    held, span, one = ref.held(k)[:, 0], ref.spans(k)[:, 0], float(ref.held(v).max())
+    for r in range(R):
+        for h in range(4):
+            x = torch.cat([held @ q[0, r, h].double() * dh ** -0.5, torch.zeros(r + 1, dtype=torch.float64, device="cuda")])
+            p = torch.softmax(x, 0)
+            want = p[:dh]
+            bound = 2.0 ** -21 * (1 + dh ** -0.5 * float((span @ q[0, r, h].double().abs()).max()))
+            off = ((got[r, h] / one - want) / (want + 2.0 ** -33 / bound * p.max())).square().mean().sqrt()
+            assert float(off) <= bound, (r, h, float(off), bound)
