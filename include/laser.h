@@ -236,7 +236,8 @@ int laser_kv_seq_release(laser_kv* kv, int seq, void* stream);
  * k, v [dev] fp16 [n_tokens][n_heads][head_dim] (a 4-bit cache quantises them). Needs reserved capacity; does not change `len`. */
 int laser_kv_import(laser_kv* kv, int seq, int layer, const uint16_t* k, const uint16_t* v,
                     int n_tokens, void* stream);
-/* Set the committed length of a slot (after laser_kv_import, or to roll back). */
+/* Set the committed length of a slot (after laser_kv_import, or to roll back). Reservations are checked when a call is made: replays of a captured
+ * step on a 16-bit cache must stay within what is reserved (a 4-bit cache leaves out the rows beyond, see laser_kv_append). */
 int laser_kv_seq_set_len(laser_kv* kv, int seq, int len, void* stream);
 /* Read back the committed lengths of B slots (synchronises `stream`) and tighten the host bounds. */
 int laser_kv_read_lens(laser_kv* kv, const int32_t* seq_ids /*[host] B*/, int B,
@@ -251,8 +252,8 @@ int laser_kv_read_lens(laser_kv* kv, const int32_t* seq_ids /*[host] B*/, int B,
  * laser_verify_step, laser_verify_tree and laser_generate do too (on the general path, whose attention is then laser_kv_attend's),
  * and results carry the cache's rounding: about 8 % of a key's or value's standard deviation. Beside the pages it holds 17 MB (9 at head_dim 64) of workspace.
  * Stored for a group x: s = fp16((max - min) / 15), m = fp16(min), c = (x - m) / s rounded to nearest even within 0..15 (s = 0: c = 0), from
- * 64-bit intermediate values (s and m rounded to fp32 and from there to fp16); magnitudes beyond 65504 saturate. A key or value that is not finite makes its token's
- * key in that head NaN (its value as if that element were 0): rows that see the token get NaN from that head, other rows are not touched. */
+ * 64-bit intermediate values (s and m rounded to fp32 and from there to fp16); s and m saturate at 65504, and m + s c
+ * may be larger (results in fp16 are then infinite). A key or value that is not finite makes its token's key in that head NaN (its value as if that element were 0): rows that see the token get NaN from that head, other rows are not touched. */
 int laser_kv_create_4bit(const laser_kv_desc* desc, void* stream, laser_kv** out);
 
 /* Element types of laser_kv_append, laser_kv_attend, laser_kv_read and laser_w4_matmul. */
@@ -313,14 +314,14 @@ int laser_w4_destroy(laser_w4* w);
 int laser_w4_quantize(const uint16_t* w, int N, int Kd, int group, uint8_t* codes, uint16_t* scales, uint16_t* offsets, void* stream);
 /* laser_w4_matmul: out[r][n] = sum over i of x[r][i] W[n][i] for M rows (up to 65535 * 32); x and out in `dtype` (LASER_F16 or LASER_BF16), rows
  * x_stride >= Kd and out_stride >= N elements apart, aligned to their elements; out must not overlap x. fp32 sums; a row of x that is not
- * finite gives results that are not. Keeps no workspace: calls on several streams may share a handle. Made for few rows (every weight is read once
+ * finite gives results that are not, and so does a bf16 row whose sum of 143 |x| over a group passes what fp32 holds. Keeps no workspace: calls on several streams may share a handle. Made for few rows (every weight is read once
  * up to 16 rows, and again for every 32, 48 or 80 of more). */
 int laser_w4_matmul(const laser_w4* w, const void* x, int64_t x_stride, int M, int dtype, void* out, int64_t out_stride, void* stream);
 
 /* laser_model_set_w4: from the next call on, steps of the model multiply with `w` instead of the bf16 matrix `which` of the layer (NULL: with the
  * bf16 matrix again); shapes as in laser_model_desc. The handle is borrowed and must live while the model (or a graph captured from its
  * steps) may use it. Steps of a model with any such matrix take the general path, rows enter these products as single fp16 values, and
- * a model whose projections are all set makes no fp16 copies of them. */
+ * a model whose projections are all set makes no fp16 copies of them. The bf16 matrices of laser_model_desc are needed all the same (NULL goes back to them). */
 #define LASER_W_QKV  0
 #define LASER_W_O    1
 #define LASER_W_GU   2

@@ -5,7 +5,7 @@
 // Keys are rotated in 64 bits: products of 24-bit operands are exact there, so that a value half-way between two codes falls to the side that
 // the formula puts it on, whatever the order of the operations.
 // Bound: latency (a chain of length, page number, inputs, four shuffles, page) until there are some thousand rows, then the values' single bytes:
-// a token's codes of a head lie in 64 places (four_bit.h). 64 tokens of 32 + 32 heads of 128 6.8 us (1.7 MB), 1024 rows of 8 + 32 heads 12.2 us (20 MB);
+// a token's codes of a head lie in 64 places (four_bit.h). 64 tokens of 32 + 32 heads of 128 6.6 us (1.7 MB), 1024 rows of 8 + 32 heads 12.2 us (20 MB);
 // with all of a head's channels in four threads, keys and values one after the other, 11.3 and 24.4. Reading back 4.3 and 4.7.
 #include <algorithm>
 #include <utility>

@@ -2,21 +2,22 @@
 //
 // Query rows of one key/value head (row r of the step, query head j of the group: packed row r G + j) form tiles of 16. A wave
 // walks its share of the context 32 tokens (two pages) at a time:
-//   scores   S[t][row] = sum over groups c of s[t][c] (codes[t][c] . q[row][c]) + m[t][c] sum(q[row][c]): one matrix instruction
-//            per group and page, K as the first operand, then two multiply-adds per score and group in fp32; the scales of four tokens
+//   scores   S[t][row] = sum over groups c of s[t][c] (codes[t][c] . q[row][c]) + m[t][c] sum(q[row][c]): one matrix instruction per group and page,
+//            K as the first operand, one for the offsets of all groups, then a multiply-add per score and group in fp32; the scales of four tokens
 //            come out of the lane's row of sixteen by a lane broadcast that the multiply-add does itself. Queries are multiplied by a power of two of
 //            their row so that fp16 holds them (bf16 exactly down to 2^-14 of the row's largest); fp32 queries are two planes.
-//   softmax  against a reference m_ref per row that moves only when a score exceeds it by 8x: else nothing crosses lanes.
-//   values   O[row][ch] += sum over t of (p[row][t] s[t][c]) codes[t][ch]: p s in fp16 (two planes where the output has more than eight bits) is the first
-//            operand as it stands in the lanes, since the page order gives both products the same tokens per lane; plus p m, one more
-//            instruction for all groups.
+//   softmax  against a reference m_ref per row that moves only when a score (an exponent of 2) exceeds it by 14: else nothing crosses lanes.
+//   values   O[row][ch] += sum over t of (p[row][t] s[t][c]) codes[t][ch]: p s in fp16 is the first operand as it stands in the lanes, since the page order
+//            gives both products the same tokens per lane; plus p m, one more instruction for all groups. p s and p are two planes where the output has more
+//            than eight bits. One plane each for bf16 results: that rounding leaves them 4 to 8 % further off the formula than their own does
+//            (two planes: 115 us against 87 for the prompt pieces below).
 // Waves of a workgroup share a context, workgroups split it further when there are few rows; a second kernel joins the parts. Pages come
 // straight into LDS, two pairs ahead of a wave, so that 60 KB a compute unit are on their way (through registers, one pair ahead, 64
 // sequences took 55 us of what follows).
 // Bound: vector instructions, some 300 a pair of pages (of them 80 take codes out of words, 64 apply the keys' scales, 48 the values'), beside
-// the pages' way from memory. 64 sequences of 11 rows, 32 heads, 448 tokens in the mean 42.7 us (150 MB, 3.5 TB/s; vector units busy
-// for 26 us of it); one row of 32 + 8 heads behind 65000 tokens 19.3 + 4.1 (83 MB, 4.3 TB/s); 64 rows of 32 + 8 heads behind 8000 tokens, four
-// sequences, 90 us (0.33 PFLOP/s).
+// the pages' way from memory. Calls in a row, bf16: 64 sequences of 11 rows, 32 heads, 448 tokens in the mean 42.3 us (150 MB, 3.5 TB/s; vector units
+// busy for 25 us of it), fp16 47.4; one row of 32 + 8 heads behind 65000 tokens 21.9 with the joining (83 MB, 3.8 TB/s); 64 rows of 32 + 8 heads behind
+// 8000 tokens, four sequences, 87 us (0.34 PFLOP/s), fp16 115.
 #include <algorithm>
 
 #include "four_bit.h"

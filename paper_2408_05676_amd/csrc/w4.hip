@@ -7,9 +7,10 @@
 // Codes enter as 16-bit floats: for fp16 rows a code masked out of its word is the subnormal c 2^-20 (in bits 0..3, as c 2^-24, an activation 3000 times
 // the others' cost their sum three times the error of fp32 sums: four_bit.h), for bf16 rows it is put under the exponent of 128
 // and stands for 128 + c, which the offset m - 128 s takes back.
-// Bound: up to four rows the weights' way from memory (4096 -> 22016, group 128, one row: 48 MB in 12.0 us, 4.0 TB/s where a long read reaches 5.5);
-// with more rows theirs as well, from L2 once a workgroup (9 rows 13.0 us, 11008 -> 4096 10.1 us); from 17 rows on the matrix and vector
-// instructions of the waves that fit (72 rows 2048 -> 6144 10.3 us, 4096 -> 22016 36 us, 0.36 PFLOP/s).
+// Bound (calls one after the other in a captured graph, bf16, group 128): up to four rows the weights' way from memory (4096 -> 22016, one row: 48 MB in
+// 12.0 us, 4.0 TB/s where a long read reaches 5.5); with more rows theirs as well, from L2 once a workgroup (9 rows 12.7 us, 11008 -> 4096 9.3 us); from 17
+// rows on the matrix and vector instructions of the waves that fit (72 rows 2048 -> 6144 10.1 us, 4096 -> 22016 36 us, 0.36 PFLOP/s).
+// Groups of 64 and 32 have two and four times the scales to apply: 72 rows 4096 -> 22016 41 and 48 us, 704 rows 256 and 339 (group 128 226).
 // Staging a block's rows in LDS for four waves, behind a barrier a block, was slower at every size (72 rows 2048 -> 6144 17.8 us).
 #include <algorithm>
 #include <vector>
@@ -244,6 +245,7 @@ static void launch_kernel(const W4Args& a, hipStream_t stream) {
     hipLaunchKernelGGL((w4_matmul_kernel<BF, NG, SWAP, MT, NT, WK>), grid, dim3(WK * 64), WK / 2 * NT * MT * 1024, stream, a);
 }
 
+// All sizes that follow are those of 256 compute units, in the rule as well.
 // Tiles of rows (MT) and outputs (NT) per wave, waves to a workgroup (WK). Up to 16 rows: two output tiles where there are tiles enough for
 // every compute unit all the same (1 row 4096 -> 22016 one tile and eight waves 14.4 us, so 11.9; 9 rows 15.8, 13.0; 1 row 4096 -> 4096 4.3, with two 5.2).
 // More rows: the smallest tile of a wave with which workgroups of eight waves are at most one for each of 256 compute units; a larger one leaves
