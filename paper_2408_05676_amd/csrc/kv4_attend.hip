@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     constexpr int NG = DH / 32, NT = DH / 16;        // groups, 16-channel tiles
     constexpr int J = 16 / CG;                       // rows of a tile
     constexpr bool kTwoQ = IN == DT_F32, kTwoP = OUT != DT_BF16;
-    constexpr float kOdd = kTwoP ? 1.f : 16.f, kKeyUnit = kTwoP ? kCodeUnit / 16.f : kCodeUnit;       // of key codes: odd groups against even ones, even ones
+    constexpr float kOdd = kTwoP ? 1.f : 16.f, kKeyUnit = kTwoP ? kCodeUnit / 16.f : kCodeUnit;       // of key codes (kTwoP: all in bits 4..7): odd groups by even ones; 1 / even ones
     constexpr int kStride = DH + 4;                  // of a row in LDS: four rows apart are sixteen banks apart
     constexpr int kWaveLds = 2 * Ring<DH>::kSlot > J * kStride * 4 ? 2 * Ring<DH>::kSlot : J * kStride * 4;
     __shared__ float sm_m[kWaves][J], sm_l[kWaves][J];
@@ -160,8 +160,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
         }
     }
 
-    // ---- queries: multiplied by a power of two of their row, to below 2^15 (and by 1/16 in odd groups, whose codes come out 16 times
-    // larger); cs > 0 takes scores back to the exponents of 2 (the sign of the scale has gone into the queries)
+    // ---- queries: multiplied by a power of two of their row, to below 2^15 (and by 1 / kOdd in odd groups, whose codes come out that
+    // many times larger); cs > 0 takes scores back to the exponents of 2 (the sign of the scale has gone into the queries)
     Frag8 q[NG], ql[NG];
     Frag8 qsum;                                  // CG = 1, operand of the offsets: first input 8 g is the sum of group g, in two parts
     constexpr float kUnit = CG == 1 ? kKeyUnit * kSumUnit : 1.f;          // of the keys' scales: scores come in units of kSumUnit, else 1 / kKeyUnit
@@ -215,7 +215,6 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
     const float cs = a.scale_log2 == 0.f ? 1.f : fmaxf(ldexpf(fabsf(a.scale_log2), sh - beyond), 1e-37f);
     const bool huge = __any(beyond > 0);
     if (huge && g == 0 && cc == 0) sm_l[wave][j] = ldexpf(1.f, min(beyond, 127));
-
 
     // ---- the walk. Weights are p = 2^(score - ref); ref moves, and what was summed with it, when a score passes it by more than kOver,
     // and is then set to kBack below the row's largest score: a row's largest p is 2^11 to 2^14. Values' scales are multiplied by `lift`, a power of
@@ -431,9 +430,9 @@ __global__ __launch_bounds__(kWaves * 64, 3) void kv4_attend_kernel(AttendArgs a
             accm = mfma_16x16x32(pack8(lo), vm, accm);
         }
 
-        // (kTwoP: all codes in bits 4..7, see four_bit.h: as bits 0..3 they cost the sums 2^-20, and a result is the small difference of two
-        // such sums: one row behind 65000 tokens came out three times as far off the formula as one rounding)
         // ---- values: operand fragments of tokens 4 g .. 4 g + 3 of both pages, p s of the group (CG > 1: of the lane's own) against them
+        // (kTwoP: all codes in bits 4..7, see four_bit.h: in bits 0..3 they cost the sums 2^-20, and a result is the small difference of two
+        // such sums: one row behind 65000 tokens came out three times as far off the formula as its rounding)
         Frag8 pv, pl;
         auto weigh = [&](auto ci) {
             constexpr int c = decltype(ci)::value;
