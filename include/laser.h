@@ -328,6 +328,38 @@ int laser_w4_matmul(const laser_w4* w, const void* x, int64_t x_stride, int M, i
 #define LASER_W_DOWN 3
 int laser_model_set_w4(laser_model* model, int layer, int which, const laser_w4* w);
 
+/* ------------------------------------------------------------------------------------------------
+ * Rows and weights in 8-bit integers. A code c = -127..127 stands for s c, with one fp32 scale s for a row of activations or for the
+ * weights of an output. For a row u with m = max |u|: c = 127 u / m rounded to nearest even and s = fp32(m / 127), both from 64-bit values; a row of
+ * zeros has s = 0 and codes 0, a row with an element that is not finite s = NaN and codes 0.
+ *
+ * laser_q8_rows: M rows of N elements, codes [dev] int8 rows codes_stride >= N apart, scales [dev] float[M]. laser_w8_matmul wants codes
+ * aligned to 16 bytes with codes_stride a multiple of 128, and reads (and ignores) what lies between N and the next multiple of 128; the calls here write
+ * N codes a row. x in `dtype` (LASER_F16, LASER_BF16, LASER_F32), rows x_stride >= 0 elements apart, aligned to its elements.
+ * M 0..65535 * 32, N 1..2^30, strides below 2^36, here and in the next two calls. Results must not overlap inputs or each other. */
+int laser_q8_rows(const void* x, int64_t x_stride, int M, int N, int dtype, int8_t* codes, int64_t codes_stride, float* scales, void* stream);
+/* laser_q8_norm: the residual's addition, the root-mean-square norm and laser_q8_rows in one pass: h = x + res, res_out = h,
+ * u = h / sqrt(mean(h^2) + eps) * gain, from 64-bit values (h is rounded to res_out's type only in res_out).
+ *   res, res_out  rows of res_dtype (x's type or LASER_F32), or both NULL: h = x. res_out may be res itself or x itself (same stride and type)
+ *   gain          [dev] float[N];  eps >= 0 */
+int laser_q8_norm(const void* x, int64_t x_stride, int dtype, const void* res, int64_t res_stride, void* res_out, int64_t res_out_stride, int res_dtype,
+                  const float* gain, float eps, int M, int N, int8_t* codes, int64_t codes_stride, float* scales, void* stream);
+/* laser_q8_read: out[r][i] = scales[r] codes[r][i] in `dtype`. */
+int laser_q8_read(const int8_t* codes, int64_t codes_stride, const float* scales, int M, int N, int dtype, void* out, int64_t out_stride, void* stream);
+
+/* laser_w8_quantize: codes [dev] int8[N][Kd] and scales [dev] float[N] of bf16 weights [N][Kd], a row of weights as a row above.
+ * laser_w8_create lays them out for the products (the handle keeps its own copy; synchronises `stream`); codes may be -128 too. gated = 1: the first
+ * N / 2 outputs are gates, the others the up projection. Kd below 2^17 (sums are 32-bit integers, exact), up to 2^23 blocks of 16 x 128 weights (LASER_E_LIMIT). */
+typedef struct laser_w8 laser_w8;
+int laser_w8_create(const int8_t* codes, const float* scales, int N, int Kd, int gated, void* stream, laser_w8** out);
+int laser_w8_destroy(laser_w8* w);
+int laser_w8_quantize(const uint16_t* w, int N, int Kd, int8_t* codes, float* scales, void* stream);
+/* laser_w8_matmul: p[r][n] = x_scales[r] scales[n] sum over i of x[r][i] codes[n][i] for M rows (up to 65535 * 32); out[r][n] = p[r][n] for all N
+ * outputs or, gated, p[r][n] / (1 + exp(-p[r][n])) p[r][n + N / 2] for N / 2. out in `dtype` (LASER_F16, LASER_BF16, LASER_F32), rows out_stride
+ * elements apart, aligned to its elements; it must not overlap x. x [dev] int8 rows of Kd codes (laser_q8_rows, laser_q8_norm), x_stride bytes apart.
+ * Keeps no workspace: calls on several streams may share a handle. LASER_E_LIMIT where M / 16 times N / 16 passes 2^25. */
+int laser_w8_matmul(const laser_w8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, void* stream);
+
 /* laser_verify_step (Eq. 3 / Eq. 6 forward, Eq. 4 / 7 / 8 acceptance, correction rule of Sec. 2.1).
  * For sequence b, rows r = 0..K hold the tokens [pending[b], drafts[b][0..K-1]] at positions
  * len+r; their keys/values go to cache slots len..len+K; row r attends to slots 0..len+r. The

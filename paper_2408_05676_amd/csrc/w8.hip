@@ -1,0 +1,164 @@
+// Products of rows in 8-bit codes with 8-bit weights: out[M][outs] = s_x[row] s_w[output] sum c_x c_w, plain or gated (silu(gate) up).
+#include <algorithm>
+
+#include "eight_bit.h"
+
+namespace laser {
+
+// Row of the handle's layout -> output of the caller's matrix, or -1.
+__device__ inline int w8_source(int row, int N, int gated) {
+    if (!gated) return row < N ? row : -1;
+    const int f = (row >> 5) * 16 + (row & 15), F = N / 2;
+    return f < F ? f + (row & 16 ? F : 0) : -1;
+}
+
+// A thread per 16 bytes: row and 16 of its inputs. Inputs beyond Kd and rows beyond N are zeros.
+__global__ __launch_bounds__(256) void w8_layout_kernel(const int8_t* codes, const float* scales, int N, int Kd, int gated, int rows, int Kp, uint8_t* out, float* out_scales) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t rc = i >> 2;
+    const int row = (int)(rc % rows), k = (int)(rc / rows) * 64 + 16 * (int)(i & 3);
+    if (k >= Kp) return;
+    const int n = w8_source(row, N, gated);
+    union { u32x4 v; int8_t b[16]; } t;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) t.b[j] = n >= 0 && k + j < Kd ? codes[(size_t)n * Kd + k + j] : (int8_t)0;
+    reinterpret_cast<u32x4*>(out)[i] = t.v;
+    if (k == 0) out_scales[row] = n >= 0 ? scales[n] : 0.f;
+}
+
+struct W8Args {
+    const uint8_t* w; const float* w_scales;
+    const int8_t* x; const float* x_scales;
+    void* out;
+    int64_t x_stride, out_stride;
+    int M, outs, rows, Kp;
+};
+
+__device__ inline float silu_times(float gate, float up) { return gate / (1.f + __expf(-gate)) * up; }
+
+// o[0..3]: results of outputs n .. n + 3
+template <int DT>
+__device__ inline void w8_store(const W8Args& a, int row, int n, const float (&o)[4]) {
+    const int64_t at = row * a.out_stride + n;
+    if (n + 4 <= a.outs) { store_elems<DT, 4>(a.out, at, o); return; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n + i < a.outs) {
+            if constexpr (DT == DT_F32) ((float*)a.out)[at + i] = o[i];
+            else ((uint16_t*)a.out)[at + i] = DT == DT_BF16 ? f32_to_bf16(o[i]) : f32_to_f16(o[i]);
+        }
+}
+
+// A wave per 16 rows and 16 outputs.
+template <int DT, bool GATED>
+__global__ __launch_bounds__(64) void w8_matmul_kernel(W8Args a) {
+    constexpr int NA = GATED ? 2 : 1;
+    const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
+    const int tiles = a.rows / (16 * NA), tile = blockIdx.x % tiles, row = blockIdx.x / tiles * 16 + r;
+    const int8_t* xp = a.x + (int64_t)min(row, a.M - 1) * a.x_stride + 16 * g;
+    const uint8_t* wp = a.w + (size_t)tile * NA * 1024 + r * 64 + 16 * g;
+    int4_t acc[NA] = {};
+    for (int k = 0; k < a.Kp; k += 64) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(xp + k);
+#pragma unroll
+        for (int j = 0; j < NA; ++j) acc[j] = mfma_i8(*reinterpret_cast<const u32x4*>(wp + (size_t)k * a.rows + j * 1024), x, acc[j]);
+    }
+    if (row >= a.M) return;
+    const float sx = a.x_scales[row];
+    float o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int n = tile * NA * 16 + 4 * g + i;
+        o[i] = (float)acc[0][i] * a.w_scales[n] * sx;           // (rows may be as large as fp32 goes, weights are not)
+        if constexpr (GATED) o[i] = silu_times(o[i], (float)acc[NA - 1][i] * a.w_scales[n + 16] * sx);
+    }
+    w8_store<DT>(a, row, tile * 16 + 4 * g, o);
+}
+
+template <int DT, bool GATED>
+static void launch_rows(const W8Args& a, hipStream_t stream) {
+    const long units = (long)(a.rows / (GATED ? 32 : 16)) * ((a.M + 15) / 16);
+    hipLaunchKernelGGL((w8_matmul_kernel<DT, GATED>), dim3((unsigned)units), dim3(64), 0, stream, a);
+}
+
+int launch_w8(const W8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, hipStream_t stream) {
+    LASER_REQUIRE((long)(w->rows / 16) * ((M + 15) / 16) < (1l << 25), LASER_E_LIMIT, "%d rows times %d outputs are too many for a launch", M, w->rows);
+    const W8Args a{w->codes, w->scales, x, x_scales, out, x_stride, out_stride, M, w->outs, w->rows, w->Kp};
+    auto go = [&](auto dt) {
+        if (w->gated) launch_rows<decltype(dt)::value, true>(a, stream);
+        else launch_rows<decltype(dt)::value, false>(a, stream);
+    };
+    if (dtype == DT_F32) go(std::integral_constant<int, DT_F32>{});
+    else if (dtype == DT_BF16) go(std::integral_constant<int, DT_BF16>{});
+    else go(std::integral_constant<int, DT_F16>{});
+    LASER_HIP_CHECK(hipGetLastError());
+    return LASER_OK;
+}
+
+}  // namespace laser
+
+using namespace laser;
+
+static int check_w8(int N, int Kd) {
+    LASER_REQUIRE(N > 0 && Kd > 0, LASER_E_INVALID_ARG, "N and Kd must be positive");
+    LASER_REQUIRE(Kd <= kQ8MaxK, LASER_E_LIMIT, "Kd %d: sums of more than %d products may pass 32 bits", Kd, kQ8MaxK);
+    LASER_REQUIRE(((long)N + 15) / 16 * (((long)Kd + 127) / 128) < (1l << 23), LASER_E_LIMIT, "matrix too large");       // (a launch has less than 2^32 threads)
+    return LASER_OK;
+}
+
+extern "C" int laser_w8_create(const int8_t* codes, const float* scales, int N, int Kd, int gated, void* stream, laser_w8** out) {
+    LASER_REQUIRE(codes && scales && out, LASER_E_INVALID_ARG, "NULL argument");
+    if (const int rc = check_w8(N, Kd)) return rc;
+    LASER_REQUIRE(gated == 0 || gated == 1, LASER_E_INVALID_ARG, "gated must be 0 or 1");
+    LASER_REQUIRE(!gated || N % 2 == 0, LASER_E_SHAPE, "a gated matrix has as many up as gate outputs: N %d is odd", N);
+    LASER_REQUIRE((uintptr_t)scales % 4 == 0, LASER_E_INVALID_ARG, "scales are not aligned to their elements");
+    const int outs = gated ? N / 2 : N, rows = (outs + 15) / 16 * 16 * (gated ? 2 : 1), Kp = (Kd + kQ8Pad - 1) / kQ8Pad * kQ8Pad;
+    W8* w = new W8{N, Kd, gated, outs, rows, Kp, nullptr, nullptr};
+    const size_t bytes = (size_t)rows * Kp;
+    auto fail = [&](hipError_t e, const char* what) {
+        set_error("%s: %s", what, hipGetErrorString(e));
+        laser_w8_destroy(reinterpret_cast<laser_w8*>(w));
+        return LASER_E_HIP;
+    };
+    hipError_t e = hipMalloc((void**)&w->codes, bytes + (size_t)rows * 4);
+    if (e != hipSuccess) return fail(e, "hipMalloc");
+    w->scales = reinterpret_cast<float*>(w->codes + bytes);
+    hipLaunchKernelGGL(w8_layout_kernel, dim3((unsigned)((bytes / 16 + 255) / 256)), dim3(256), 0, (hipStream_t)stream, codes, scales, N, Kd, gated, rows, Kp, w->codes, w->scales);
+    if ((e = hipGetLastError()) != hipSuccess) return fail(e, "w8_layout_kernel");
+    if ((e = hipStreamSynchronize((hipStream_t)stream)) != hipSuccess) return fail(e, "hipStreamSynchronize");
+    *out = reinterpret_cast<laser_w8*>(w);
+    return LASER_OK;
+}
+
+extern "C" int laser_w8_destroy(laser_w8* h) {
+    W8* w = reinterpret_cast<W8*>(h);
+    if (!w) return LASER_OK;
+    if (w->codes) (void)hipFree(w->codes);
+    delete w;
+    return LASER_OK;
+}
+
+extern "C" int laser_w8_quantize(const uint16_t* w, int N, int Kd, int8_t* codes, float* scales, void* stream) {
+    LASER_REQUIRE(w && codes && scales, LASER_E_INVALID_ARG, "NULL argument");
+    if (const int rc = check_w8(N, Kd)) return rc;
+    for (int n = 0; n < N; n += kQ8MaxRows)          // (a launch's rows)
+        if (const int rc = laser_q8_rows(w + (size_t)n * Kd, Kd, std::min(N - n, kQ8MaxRows), Kd, LASER_BF16, codes + (size_t)n * Kd, Kd, scales + n, stream)) return rc;
+    return LASER_OK;
+}
+
+extern "C" int laser_w8_matmul(const laser_w8* h, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, void* stream) {
+    const W8* w = reinterpret_cast<const W8*>(h);
+    LASER_REQUIRE(w != nullptr, LASER_E_INVALID_ARG, "w is NULL");
+    LASER_REQUIRE(dtype == LASER_F16 || dtype == LASER_BF16 || dtype == LASER_F32, LASER_E_INVALID_ARG, "dtype %d: LASER_F16, LASER_BF16 or LASER_F32", dtype);
+    LASER_REQUIRE(M >= 0 && M <= kQ8MaxRows, LASER_E_INVALID_ARG, "M %d out of range", M);
+    LASER_REQUIRE(x_stride % kQ8Pad == 0 && x_stride >= w->Kp && x_stride < (1ll << 32), LASER_E_INVALID_ARG, "x_stride %lld: a multiple of %d, at least %d", (long long)x_stride, kQ8Pad, w->Kp);
+    LASER_REQUIRE(out_stride >= w->outs && out_stride < (1ll << 32), LASER_E_INVALID_ARG, "rows of out overlap: stride %lld", (long long)out_stride);
+    if (M == 0) return LASER_OK;
+    LASER_REQUIRE(x && x_scales && out, LASER_E_INVALID_ARG, "NULL argument");
+    const int64_t e = (int64_t)dtype_bytes(dtype);
+    LASER_REQUIRE((uintptr_t)x % 16 == 0, LASER_E_INVALID_ARG, "x is not aligned to 16 bytes");
+    LASER_REQUIRE((uintptr_t)out % e == 0 && (uintptr_t)x_scales % 4 == 0, LASER_E_INVALID_ARG, "out or x_scales is not aligned to its elements");
+    LASER_REQUIRE(rows_apart(out, w->outs * e, out_stride * e, x, w->Kp, x_stride, M) && rows_apart(out, w->outs * e, out_stride * e, x_scales, 4, 4, M), LASER_E_INVALID_ARG,
+                  "out overlaps x or x_scales");
+    return launch_w8(w, x, x_stride, x_scales, M, dtype, out, out_stride, (hipStream_t)stream);
+}

@@ -1,0 +1,384 @@
+"""Rows and weights in 8-bit integers (rows, norm, read, quantised weights, products plain and gated) against plain 64-bit forms."""
+import pytest
+import torch
+
+import paper_2408_05676_amd as laser
+from tests import eight_bit_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, *dims, dtype=F32, scale=1.0):
+    return (torch.empty(dims, device="cuda").normal_(0, 1, generator=g) * scale).to(dtype)
+
+
+def activations(g, M, N, dtype):
+    return (normal(g, M, N) * torch.exp(0.6 * normal(g, N)) * torch.exp(0.3 * normal(g, M, 1))).to(dtype)
+
+
+def same(a, b):
+    return bool(((a == b) | (a.isnan() & b.isnan())).all()) if a.is_floating_point() else torch.equal(a, b)
+
+
+SHAPES = [(1, 1), (1, 2), (3, 7), (1, 64), (4, 100), (10, 256), (1, 4096), (33, 511), (72, 2048), (5, 2049), (64, 4096), (2, 5632), (3, 8192), (2, 8193), (1, 11008),
+          (300, 1000), (1, 16385), (2, 40001), (700, 130)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("M, N", SHAPES)
+def test_rows(M, N, dtype):
+    x = activations(gen(M + N), M, N, dtype)
+    codes, scales = laser.q8_rows(x)
+    c, s = ref.rows(x)
+    assert torch.equal(codes, c) and torch.equal(scales, s)
+    assert M == 1 or codes.stride(0) % laser.Q8_PAD == 0
+    for t in (F16, BF16, F32):
+        assert ref.values_close(laser.q8_read(codes, scales, dtype=t), codes, scales)
+
+
+@pytest.mark.parametrize("dtype, res", [(F16, None), (F16, F16), (F16, F32), (BF16, None), (BF16, BF16), (BF16, F32), (F32, None), (F32, F32)])
+@pytest.mark.parametrize("M, N", SHAPES)
+def test_norm(M, N, dtype, res):
+    g = gen(M + N + 1)
+    x, gain = activations(g, M, N, dtype), 1 + 0.1 * normal(g, N)
+    r = activations(g, M, N, res) if res else None
+    before = None if r is None else r.clone()
+    c, s, h = ref.norm(x, gain, 1e-6, r)
+    out = None if r is None else torch.empty_like(r)
+    codes, scales = laser.q8_norm(x, gain, 1e-6, residual=r, residual_out=out)
+    assert torch.equal(codes, c) and ref.scales_close(scales, s)
+    if r is not None:
+        assert torch.equal(out, h.float().to(res)) and torch.equal(r, before)
+        again, s2 = laser.q8_norm(x, gain, 1e-6, residual=r)               # in place
+        assert torch.equal(again, codes) and torch.equal(s2, scales) and torch.equal(r, out)
+
+
+def test_codes_half_way_between_two():
+    """Halves of a row's largest: 63.5 goes to 64, and so do all its odd 254ths to the even neighbour."""
+    x = torch.arange(-254, 255, device="cuda").float()[None]
+    codes, scales = laser.q8_rows(x)
+    want = (x.double() / 2).round().to(torch.int8)
+    assert torch.equal(codes, want) and float(scales[0]) == 2.0
+    for t in (F16, BF16):
+        y = torch.tensor([[1.0, 0.5, -0.5, 0.25, 3.0, 1.5, -3.0, 0.75]], device="cuda", dtype=t) * 1.25
+        assert torch.equal(laser.q8_rows(y)[0], ref.rows(y)[0])
+        gain = torch.full((8,), 1 / 3, device="cuda")
+        assert torch.equal(laser.q8_norm(y, gain)[0], ref.norm(y, gain, 1e-6, None)[0])
+
+
+@pytest.mark.parametrize("N", [5, 300, 4096, 9000])
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_zeros_extremes_and_numbers_that_are_not_finite(dtype, N):
+    top, least = torch.finfo(dtype).max, torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    x = activations(gen(N), 8, N, dtype)
+    x[0] = 0
+    x[1, N // 2] = float("nan")
+    x[2, 0] = float("inf")
+    x[3, N - 1] = -float("inf")
+    x[4] = top
+    x[5] = 0
+    x[5, N - 1] = least                                                    # the type's smallest number, alone in its row
+    x[6] = -top
+    codes, scales = laser.q8_rows(x)
+    c, s = ref.rows(x)
+    assert torch.equal(codes, c) and same(scales, s)
+    assert scales[0] == 0 and bool(scales[1:4].isnan().all()) and not codes[:4].any()
+    gain = torch.ones(N, device="cuda")
+    codes, scales = laser.q8_norm(x, gain, 0.0)
+    c, s, _ = ref.norm(x, gain, 0.0, None)
+    assert torch.equal(codes, c) and ref.scales_close(scales, s)
+    bad_gain = gain.clone()
+    bad_gain[N - 1] = float("inf")
+    codes, scales = laser.q8_norm(x, bad_gain)
+    assert bool(scales.isnan().all()) and not codes.any()                  # (a row of zeros too: 0 inf)
+    wc, ws = laser.w8_quantize(normal(gen(1), 16, N, dtype=BF16))
+    codes, scales = laser.q8_rows(x)
+    o = laser.w8_matmul(laser.W8(wc, ws), codes, scales, dtype=F32)
+    assert not o[0].any() and bool(o[1:4].isnan().all())
+    p, most = ref.product(codes[4:], scales[4:], wc, ws), torch.finfo(F32).max
+    inside = p.abs() < most * (1 - 2.0 ** -20)                             # some of the true results are beyond fp32: those are infinite
+    assert ref.product_close(torch.where(inside, o[4:], 0.0), torch.where(inside, p, 0.0))
+    assert bool(o[4:][p.abs() > most * (1 + 2.0 ** -20)].isinf().all())
+
+
+def test_layouts_of_rows():
+    """Rows apart from each other, columns of wider matrices, broadcast inputs, memory off the 16-byte grid; what lies between rows stays."""
+    g = gen(3)
+    M, N = 9, 333
+    wide = activations(g, M, 1000, F16)
+    gain = 1 + 0.1 * normal(g, N)
+    for x in (wide[:, 5:5 + N], wide[:1, 3:3 + N].expand(M, N), wide[:, 400:400 + N]):
+        assert torch.equal(laser.q8_rows(x)[0], ref.rows(x)[0])
+        buf, sc = torch.full((M, 700), 77, dtype=torch.int8, device="cuda"), torch.full((M + 2,), 7.0, device="cuda")
+        rb, rin = torch.full((M, 900), 5.0, dtype=F16, device="cuda"), activations(g, 1, N, F16).expand(M, N)
+        codes, scales = laser.q8_norm(x, gain, residual=rin, residual_out=rb[:, 201:201 + N], out=(buf[:, 11:11 + N], sc[1:M + 1]))
+        c, s, h = ref.norm(x, gain, 1e-6, rin)
+        assert torch.equal(codes, c) and ref.scales_close(scales, s) and torch.equal(rb[:, 201:201 + N], h.float().half())
+        assert bool((buf[:, :11] == 77).all()) and bool((buf[:, 11 + N:] == 77).all()) and sc[0] == 7 and sc[M + 1] == 7
+        assert bool((rb[:, :201] == 5).all()) and bool((rb[:, 201 + N:] == 5).all())
+        out = torch.full((M, 501), 3.0, dtype=BF16, device="cuda")
+        laser.q8_read(codes, scales, out=out[:, 7:7 + N])
+        assert ref.values_close(out[:, 7:7 + N], codes, scales)
+        assert bool((out[:, :7] == 3).all()) and bool((out[:, 7 + N:] == 3).all())
+    x = wide[:, :N].clone()                                                # the sum over x itself
+    r = activations(g, M, N, F16)
+    c, s, h = ref.norm(x, gain, 1e-6, r)
+    codes, _ = laser.q8_norm(x, gain, residual=r, residual_out=x)
+    assert torch.equal(codes, c) and torch.equal(x, h.float().half())
+
+
+def test_rows_and_residual_side_by_side():
+    """x and the residual as columns of one matrix: nothing is shared, though the memory they span is."""
+    g = gen(4)
+    both, gain = activations(g, 6, 256, F32), torch.ones(128, device="cuda")
+    c, _, h = ref.norm(both[:, :128], gain, 1e-6, both[:, 128:])
+    codes, _ = laser.q8_norm(both[:, :128], gain, residual=both[:, 128:])
+    assert torch.equal(codes, c) and torch.equal(both[:, 128:], h.float())
+    with pytest.raises(laser.LaserError, match="overlap"):
+        laser.q8_norm(both[:, :128], gain, residual=both[:, 64:192])
+
+
+def made(g, N, Kd, extremes=False):
+    w = torch.randint(-127, 128, (N, Kd), generator=g, device="cuda", dtype=torch.int16).to(torch.int8)
+    if extremes:
+        w.fill_(-128)
+    return w, torch.rand(N, generator=g, device="cuda") * 1e-3 + 1e-4
+
+
+def padded(codes, value=0):
+    t = torch.full((codes.shape[0], -(-codes.shape[1] // 128) * 128), value, dtype=torch.int8, device="cuda")
+    t[:, :codes.shape[1]] = codes
+    return t[:, :codes.shape[1]]
+
+
+# rows x outputs x inputs: ends of tiles, one row to many, one output to many, inputs off the 128
+PRODUCTS = [(1, 1, 1), (1, 16, 128), (2, 768, 256), (1, 4096, 4096), (3, 17, 129), (5, 100, 64), (9, 4096, 11008), (16, 1000, 1000), (17, 4096, 512), (31, 64, 640),
+            (33, 333, 333), (48, 2048, 384), (49, 130, 1024), (64, 4096, 4096), (72, 6144, 2048), (80, 1111, 777), (81, 512, 512), (96, 4096, 1024), (100, 5000, 130),
+            (128, 12288, 256), (136, 256, 4096), (200, 4100, 256), (249, 777, 1500), (256, 4096, 11008), (352, 4096, 512), (513, 2000, 640), (704, 1024, 1024),
+            (1000, 300, 300), (1025, 2048, 128), (2500, 130, 200)]
+
+
+@pytest.mark.parametrize("M, N, Kd", PRODUCTS)
+def test_products(M, N, Kd):
+    g = gen(M + N + Kd)
+    w, sw = made(g, N, Kd)
+    x, sx = made(g, M, Kd)
+    x = padded(x, 127)                                                     # what lies behind a row's codes does not count
+    p = ref.product(x, sx, w, sw)
+    h = laser.W8(w, sw)
+    for t in (F16, BF16, F32):
+        out = laser.w8_matmul(h, x, sx, dtype=t)
+        assert out.shape == (M, N) and ref.product_close(out, p), t
+        assert torch.equal(out, laser.w8_matmul(h, x, sx, dtype=t))
+
+
+@pytest.mark.parametrize("M, N, Kd", PRODUCTS)
+def test_gated_products(M, N, Kd):
+    g = gen(M + N + Kd + 1)
+    w, sw = made(g, 2 * N, Kd)
+    x, sx = made(g, M, Kd)
+    x, sx = padded(x, -128), sx * (3.0 / (Kd ** 0.5 * 73 * 73 * 5.5e-4 * 6e-4))  # gates of some units
+    o, before = ref.gated(x, sx, w, sw)
+    h = laser.W8(w, sw, gated=True)
+    for t in (F16, BF16, F32):
+        out = laser.w8_matmul(h, x, sx, dtype=t)
+        assert out.shape == (M, N) and ref.gated_close(out, o, before), t
+        assert torch.equal(out, laser.w8_matmul(h, x, sx, dtype=t))
+
+
+@pytest.mark.parametrize("M, N", [(1, 16), (20, 40), (100, 64), (300, 100)])
+def test_sums_at_the_edge_of_32_bits(M, N):
+    Kd = 2 ** 17 - 1
+    g = gen(M)
+    w, sw = made(g, N, Kd, extremes=True)
+    x, sx = made(g, M, Kd, extremes=True)
+    x[:, ::3] = 127
+    p = ref.product(padded(x), sx, w, sw)
+    assert ref.product_close(laser.w8_matmul(laser.W8(w, sw), padded(x), sx, dtype=F32), p)
+    x.fill_(-128)
+    p = ref.product(padded(x), sx, w, sw)
+    assert float((p / sx.double()[:, None] / sw.double()).max()) > 2.0 ** 31 - 2.0 ** 15
+    assert ref.product_close(laser.w8_matmul(laser.W8(w, sw), padded(x), sx, dtype=F32), p)
+
+
+def test_large_gates():
+    """Gates at which exp passes fp32 on either side."""
+    Kd, N = 128, 16
+    w = torch.ones((2 * N, Kd), dtype=torch.int8, device="cuda")
+    sw = torch.cat([torch.linspace(-3, 3, N, device="cuda"), torch.ones(N, device="cuda")])
+    x, sx = torch.full((4, Kd), 1, dtype=torch.int8, device="cuda"), torch.tensor([1e-3, 0.3, 1.0, 1e3], device="cuda")
+    o, before = ref.gated(x, sx, w, sw)
+    out = laser.w8_matmul(laser.W8(w, sw, gated=True), x, sx, dtype=F32)
+    assert bool(out.isfinite().all()) and ref.gated_close(out, o, before)
+
+
+@pytest.mark.parametrize("M", [1, 9, 40, 200])
+@pytest.mark.parametrize("gated", [False, True])
+def test_layouts_of_products(M, gated):
+    g = gen(M)
+    N, Kd = 90, 250
+    w, sw = made(g, N, Kd)
+    h = laser.W8(w, sw, gated=gated)
+    big, s = made(g, 2 * M + 3, 1152)
+    x = big[1:2 * M + 1:2, 512:512 + Kd]                                   # every other row, from a column on
+    sx = s[:M].contiguous()
+    want = laser.w8_matmul(h, padded(x), sx)
+    buf = torch.full((M + 2, 301), 9.0, dtype=F16, device="cuda")
+    out = buf[1:M + 1, 11:11 + h.outs]
+    laser.w8_matmul(h, x, sx, out=out)
+    assert torch.equal(out, want)
+    buf[1:M + 1, 11:11 + h.outs] = 9
+    assert bool((buf == 9).all())
+
+
+def test_a_scale_that_is_not_a_number_stays_in_its_place():
+    g = gen(8)
+    w, sw = made(g, 40, 256)
+    x, sx = made(g, 70, 256)
+    sx[3], sw[7] = float("nan"), float("nan")
+    out = laser.w8_matmul(laser.W8(w, sw), x, sx)
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[3], bad[:, 7] = True, True
+    assert torch.equal(out.isnan(), bad)
+
+
+@pytest.mark.parametrize("N, Kd", [(1, 1), (17, 333), (256, 4096), (1000, 128)])
+def test_weights_are_quantised_by_rows(N, Kd):
+    w = normal(gen(N), N, Kd, dtype=BF16, scale=0.02)
+    w[0, 0] = float("nan") if N > 16 else 1.0
+    codes, scales = laser.w8_quantize(w)
+    c, s = ref.rows(w)
+    assert torch.equal(codes, c) and same(scales, s)
+
+
+def test_refusals():
+    g = gen(9)
+    w, sw = made(g, 32, 200)
+    h = laser.W8(w, sw)
+    x, sx = made(g, 4, 200)
+    good = padded(x)
+    with pytest.raises(laser.LaserError, match="multiple"):
+        laser.w8_matmul(h, x, sx)                                          # rows 200 bytes apart
+    with pytest.raises(laser.LaserError, match="reach as far"):
+        laser.w8_matmul(h, torch.zeros(3 * 256 + 200, dtype=torch.int8, device="cuda").as_strided((4, 200), (256, 1)), sx)
+    with pytest.raises(laser.LaserError, match="16 bytes"):
+        laser.w8_matmul(h, torch.zeros((4, 384), dtype=torch.int8, device="cuda")[:, 8:208], sx)
+    with pytest.raises(laser.LaserError):
+        laser.w8_matmul(h, good[:, :199], sx)
+    with pytest.raises(laser.LaserError, match="scales"):
+        laser.w8_matmul(h, good, sx[:3])
+    with pytest.raises(laser.LaserError, match="scales"):
+        laser.w8_matmul(h, good, sx.double())
+    with pytest.raises(laser.LaserError, match="out"):
+        laser.w8_matmul(h, good, sx, out=torch.zeros((4, 33), device="cuda"))
+    with pytest.raises(laser.LaserError, match="overlap"):
+        laser.w8_matmul(h, good, sx, out=torch.zeros((1, 32), device="cuda").expand(4, 32))
+    with pytest.raises(laser.LaserError, match="overlap"):
+        flat = torch.zeros(4 * 1024, dtype=torch.int8, device="cuda")
+        laser.w8_matmul(h, flat.view(4, 1024)[:, :200], sx, out=flat.view(F16).view(4, 512)[:, 64:96])
+    with pytest.raises(laser.LaserError):
+        laser.W8(w[:31].contiguous(), sw[:31].contiguous(), gated=True)
+    closed = laser.W8(w, sw)
+    closed.close()
+    with pytest.raises(laser.LaserError, match="closed"):
+        laser.w8_matmul(closed, good, sx)
+    with pytest.raises(laser.LaserError, match="residual_out"):
+        laser.q8_norm(sx[:, None].half(), torch.ones(1, device="cuda"), residual_out=sx[:, None].half())
+    with pytest.raises(laser.LaserError, match="on device 1"):
+        gone = laser.W8(w, sw)
+        gone.device = 1
+        laser.w8_matmul(gone, good, sx)
+    assert laser.w8_matmul(h, good[:0], sx[:0]).shape == (0, 32)
+    assert laser.q8_rows(normal(g, 0, 64))[0].shape == (0, 64)
+
+
+def block(g, d, F):
+    """A feed-forward block's weights: gain, gated matrix, down matrix, and the three as the framework holds them."""
+    gain, wgu, wd = 1 + 0.1 * normal(g, d), normal(g, 2 * F, d, dtype=BF16, scale=d ** -0.5), normal(g, d, F, dtype=BF16, scale=F ** -0.5)
+    return gain, wgu, wd, laser.W8(*laser.w8_quantize(wgu), gated=True), laser.W8(*laser.w8_quantize(wd))
+
+
+def feed_forward(x, res, gain, gu, down, stream=None):
+    q = laser.q8_norm(x, gain, residual=res, stream=stream)
+    act = laser.w8_matmul(gu, *q, stream=stream)
+    return laser.w8_matmul(down, *laser.q8_rows(act, stream=stream), dtype=F32, stream=stream), q, act
+
+
+@pytest.mark.parametrize("M, d, F", [(1, 256, 1024), (9, 200, 333), (72, 512, 1408), (300, 256, 700)])
+def test_operators_together(M, d, F):
+    """norm -> gated product -> rows -> product, each against the 64-bit form of its own step's inputs, the whole against bf16 weights within
+    what three roundings to 8 bits leave."""
+    g = gen(M)
+    gain, wgu, wd, gu, down = block(g, d, F)
+    x, res = activations(g, M, d, F32), activations(g, M, d, F32)
+    c, s, h = ref.norm(x, gain, 1e-6, res)
+    out, q, act = feed_forward(x, res, gain, gu, down)
+    assert torch.equal(res, h.float()) and torch.equal(q[0], c) and ref.scales_close(q[1], s)
+    assert ref.gated_close(act, *ref.gated(*q, *laser.w8_quantize(wgu)))
+    cq, sq = ref.rows(act)
+    assert ref.product_close(out, ref.product(cq, sq, *laser.w8_quantize(wd)))
+    gate, up = ((h / (h.square().mean(-1, keepdim=True) + 1e-6).sqrt() * gain.double()) @ wgu.double().T.contiguous()).chunk(2, -1)
+    want = (gate * torch.sigmoid(gate) * up) @ wd.double().T.contiguous()
+    # rounding to a step of max / 127 is max / 127 / sqrt(12) rms: with maxima of 3 to 15 times the rms 0.7 to 3.4 % a tensor; five of them
+    assert float((out.double() - want).norm() / want.norm()) < 0.08
+
+
+def test_on_another_stream():
+    g = gen(11)
+    gain, _, _, gu, down = block(g, 256, 512)
+    x, res = activations(g, 20, 256, F32), activations(g, 20, 256, F32)
+    want, *_ = feed_forward(x, res.clone(), gain, gu, down)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, *_ = feed_forward(x, res.clone(), gain, gu, down, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_two_streams_share_a_matrix():
+    g = gen(12)
+    w, sw = made(g, 4096, 1024)
+    h = laser.W8(w, sw)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    rows = [tuple(made(g, M, 1024)) for M in (5, 300)]
+    want = [laser.w8_matmul(h, *r) for r in rows]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(sides):
+            outs[i].append(laser.w8_matmul(h, *rows[i], stream=s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in outs[i])
+
+
+@pytest.mark.parametrize("M", [1, 9, 72, 200])
+def test_captured_and_replayed(M):
+    """Two graphs of the same block and matrices, replayed in turn with eager calls between; inputs change from replay to replay."""
+    g = gen(M)
+    gain, _, _, gu, down = block(g, 512, 1408)
+    graphs = []
+    for _ in range(2):
+        x, res = activations(g, M, 512, F32), activations(g, M, 512, F32)
+        feed_forward(x, res.clone(), gain, gu, down)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out, *_ = feed_forward(x, res, gain, gu, down)
+        graphs.append((graph, x, res, out))
+    for _ in range(4):
+        for graph, x, res, out in graphs:
+            x.copy_(activations(g, M, 512, F32))
+            res.copy_(activations(g, M, 512, F32))
+            was = res.clone()
+            graph.replay()
+            torch.cuda.synchronize()
+            want, *_ = feed_forward(x, was, gain, gu, down)
+            assert torch.equal(out, want) and torch.equal(res, was)
