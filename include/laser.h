@@ -349,14 +349,14 @@ int laser_q8_read(const int8_t* codes, int64_t codes_stride, const float* scales
 
 /* laser_w8_quantize: codes [dev] int8[N][Kd] and scales [dev] float[N] of bf16 weights [N][Kd], a row of weights as a row above.
  * laser_w8_create lays them out for the products (the handle keeps its own copy; synchronises `stream`); codes may be -128 too. gated = 1: the first
- * N / 2 outputs are gates, the others the up projection. Kd below 2^17 (sums are 32-bit integers, exact), up to 2^23 blocks of 16 x 128 weights (LASER_E_LIMIT). */
+ * N / 2 outputs are gates, the others the up projection. Kd below 2^17 (sums are 32-bit integers, exact), N up to 2^25, up to 2^23 blocks of 16 x 128 weights (LASER_E_LIMIT). */
 typedef struct laser_w8 laser_w8;
 int laser_w8_create(const int8_t* codes, const float* scales, int N, int Kd, int gated, void* stream, laser_w8** out);
 int laser_w8_destroy(laser_w8* w);
 int laser_w8_quantize(const uint16_t* w, int N, int Kd, int8_t* codes, float* scales, void* stream);
 /* laser_w8_matmul: p[r][n] = x_scales[r] scales[n] sum over i of x[r][i] codes[n][i] for M rows (up to 65535 * 32); out[r][n] = p[r][n] for all N
  * outputs or, gated, p[r][n] / (1 + exp(-p[r][n])) p[r][n + N / 2] for N / 2. out in `dtype` (LASER_F16, LASER_BF16, LASER_F32), rows out_stride
- * elements apart, aligned to its elements; it must not overlap x. x [dev] int8 rows of Kd codes (laser_q8_rows, laser_q8_norm), x_stride bytes apart.
+ * elements apart, aligned to its elements; it must not overlap x. x [dev] int8 rows of Kd codes (laser_q8_rows, laser_q8_norm), x_stride < 2^22 bytes apart.
  * Keeps no workspace: calls on several streams may share a handle. LASER_E_LIMIT where M / 16 times N / 16 passes 2^25. */
 int laser_w8_matmul(const laser_w8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, void* stream);
 

@@ -1,7 +1,7 @@
 // Products of rows in 8-bit codes with 8-bit weights: out[M][outs] = s_x[row] s_w[output] sum c_x c_w, plain or gated (silu(gate) up).
 #include <algorithm>
 
-#include "eight_bit.h"
+#include "w8_tile.h"
 
 namespace laser {
 
@@ -12,11 +12,10 @@ __device__ inline int w8_source(int row, int N, int gated) {
     return f < F ? f + (row & 16 ? F : 0) : -1;
 }
 
-// A thread per 16 bytes: row and 16 of its inputs. Inputs beyond Kd and rows beyond N are zeros.
+// A thread per 16 bytes: an output and 16 of its inputs. Inputs beyond Kd and rows beyond N are zeros.
 __global__ __launch_bounds__(256) void w8_layout_kernel(const int8_t* codes, const float* scales, int N, int Kd, int gated, int rows, int Kp, uint8_t* out, float* out_scales) {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const size_t rc = i >> 2;
-    const int row = (int)(rc % rows), k = (int)(rc / rows) * 64 + 16 * (int)(i & 3);
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, frag = i >> 6;
+    const int tiles = rows / 16, row = (int)(frag % tiles) * 16 + (int)(i & 15), k = (int)(frag / tiles) * 64 + 16 * (int)(i >> 4 & 3);
     if (k >= Kp) return;
     const int n = w8_source(row, N, gated);
     union { u32x4 v; int8_t b[16]; } t;
@@ -26,29 +25,6 @@ __global__ __launch_bounds__(256) void w8_layout_kernel(const int8_t* codes, con
     if (k == 0) out_scales[row] = n >= 0 ? scales[n] : 0.f;
 }
 
-struct W8Args {
-    const uint8_t* w; const float* w_scales;
-    const int8_t* x; const float* x_scales;
-    void* out;
-    int64_t x_stride, out_stride;
-    int M, outs, rows, Kp;
-};
-
-__device__ inline float silu_times(float gate, float up) { return gate / (1.f + __expf(-gate)) * up; }
-
-// o[0..3]: results of outputs n .. n + 3
-template <int DT>
-__device__ inline void w8_store(const W8Args& a, int row, int n, const float (&o)[4]) {
-    const int64_t at = row * a.out_stride + n;
-    if (n + 4 <= a.outs) { store_elems<DT, 4>(a.out, at, o); return; }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (n + i < a.outs) {
-            if constexpr (DT == DT_F32) ((float*)a.out)[at + i] = o[i];
-            else ((uint16_t*)a.out)[at + i] = DT == DT_BF16 ? f32_to_bf16(o[i]) : f32_to_f16(o[i]);
-        }
-}
-
 // A wave per 16 rows and 16 outputs.
 template <int DT, bool GATED>
 __global__ __launch_bounds__(64) void w8_matmul_kernel(W8Args a) {
@@ -56,9 +32,9 @@ __global__ __launch_bounds__(64) void w8_matmul_kernel(W8Args a) {
     const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
     const int tiles = a.rows / (16 * NA), tile = blockIdx.x % tiles, row = blockIdx.x / tiles * 16 + r;
     const int8_t* xp = a.x + (int64_t)min(row, a.M - 1) * a.x_stride + 16 * g;
-    const uint8_t* wp = a.w + (size_t)tile * NA * 1024 + r * 64 + 16 * g;
+    const uint8_t* wp = a.w + (size_t)tile * NA * 1024 + lane * 16;
     int4_t acc[NA] = {};
-    for (int k = 0; k < a.Kp; k += 64) {
+    for (int k = 0; k < a.Kd; k += 64) {
         const u32x4 x = *reinterpret_cast<const u32x4*>(xp + k);
 #pragma unroll
         for (int j = 0; j < NA; ++j) acc[j] = mfma_i8(*reinterpret_cast<const u32x4*>(wp + (size_t)k * a.rows + j * 1024), x, acc[j]);
@@ -81,9 +57,29 @@ static void launch_rows(const W8Args& a, hipStream_t stream) {
     hipLaunchKernelGGL((w8_matmul_kernel<DT, GATED>), dim3((unsigned)units), dim3(64), 0, stream, a);
 }
 
+static int w8_shape(const W8Args& a, int ncu) {
+    int best = 0;
+    double best_cost = 1e300;
+    for (int v = 0; v < kW8Shapes_; ++v) {
+        const int bm = kW8Shapes[v].wm * 16, bn = kW8Shapes[v].wn * 64;
+        const long units = (long)((a.M + bm - 1) / bm) * ((a.rows + bn - 1) / bn), rounds = (units + ncu - 1) / ncu;
+        const double step = 2.0 * kW8Shapes[v].wm * kW8Shapes[v].wn * 16 + 5.0 * (bm + bn) / 8;
+        const double cost = (double)rounds * (a.Kp / 128 * step + 8000.0);
+        if (cost < best_cost) { best_cost = cost; best = v; }
+    }
+    return best;
+}
+
 int launch_w8(const W8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, hipStream_t stream) {
     LASER_REQUIRE((long)(w->rows / 16) * ((M + 15) / 16) < (1l << 25), LASER_E_LIMIT, "%d rows times %d outputs are too many for a launch", M, w->rows);
-    const W8Args a{w->codes, w->scales, x, x_scales, out, x_stride, out_stride, M, w->outs, w->rows, w->Kp};
+    const W8Args a{w->codes, w->scales, x, x_scales, out, x_stride, out_stride, M, w->outs, w->rows, w->Kd, w->Kp, dtype, 0, 0};
+    if (M > 16) {
+        const int v = w8_shape(a, 256);
+        if (w->gated) launch_w8_tile_gated(a, v, stream);
+        else launch_w8_tile_plain(a, v, stream);
+        LASER_HIP_CHECK(hipGetLastError());
+        return LASER_OK;
+    }
     auto go = [&](auto dt) {
         if (w->gated) launch_rows<decltype(dt)::value, true>(a, stream);
         else launch_rows<decltype(dt)::value, false>(a, stream);
@@ -102,7 +98,7 @@ using namespace laser;
 static int check_w8(int N, int Kd) {
     LASER_REQUIRE(N > 0 && Kd > 0, LASER_E_INVALID_ARG, "N and Kd must be positive");
     LASER_REQUIRE(Kd <= kQ8MaxK, LASER_E_LIMIT, "Kd %d: sums of more than %d products may pass 32 bits", Kd, kQ8MaxK);
-    LASER_REQUIRE(((long)N + 15) / 16 * (((long)Kd + 127) / 128) < (1l << 23), LASER_E_LIMIT, "matrix too large");       // (a launch has less than 2^32 threads)
+    LASER_REQUIRE(N <= (1 << 25) && ((long)N + 15) / 16 * (((long)Kd + 127) / 128) < (1l << 23), LASER_E_LIMIT, "matrix too large");   // (offsets of 32 bits; a launch has less than 2^32 threads)
     return LASER_OK;
 }
 
@@ -112,7 +108,7 @@ extern "C" int laser_w8_create(const int8_t* codes, const float* scales, int N, 
     LASER_REQUIRE(gated == 0 || gated == 1, LASER_E_INVALID_ARG, "gated must be 0 or 1");
     LASER_REQUIRE(!gated || N % 2 == 0, LASER_E_SHAPE, "a gated matrix has as many up as gate outputs: N %d is odd", N);
     LASER_REQUIRE((uintptr_t)scales % 4 == 0, LASER_E_INVALID_ARG, "scales are not aligned to their elements");
-    const int outs = gated ? N / 2 : N, rows = (outs + 15) / 16 * 16 * (gated ? 2 : 1), Kp = (Kd + kQ8Pad - 1) / kQ8Pad * kQ8Pad;
+    const int outs = gated ? N / 2 : N, rows = (outs + 15) / 16 * 16 * (gated ? 2 : 1), Kp = (Kd + 255) / 256 * 256;
     W8* w = new W8{N, Kd, gated, outs, rows, Kp, nullptr, nullptr};
     const size_t bytes = (size_t)rows * Kp;
     auto fail = [&](hipError_t e, const char* what) {
@@ -151,14 +147,14 @@ extern "C" int laser_w8_matmul(const laser_w8* h, const int8_t* x, int64_t x_str
     LASER_REQUIRE(w != nullptr, LASER_E_INVALID_ARG, "w is NULL");
     LASER_REQUIRE(dtype == LASER_F16 || dtype == LASER_BF16 || dtype == LASER_F32, LASER_E_INVALID_ARG, "dtype %d: LASER_F16, LASER_BF16 or LASER_F32", dtype);
     LASER_REQUIRE(M >= 0 && M <= kQ8MaxRows, LASER_E_INVALID_ARG, "M %d out of range", M);
-    LASER_REQUIRE(x_stride % kQ8Pad == 0 && x_stride >= w->Kp && x_stride < (1ll << 32), LASER_E_INVALID_ARG, "x_stride %lld: a multiple of %d, at least %d", (long long)x_stride, kQ8Pad, w->Kp);
+    LASER_REQUIRE(x_stride % kQ8Pad == 0 && x_stride >= w->Kd && x_stride < (1ll << 22), LASER_E_INVALID_ARG, "x_stride %lld: a multiple of %d below 2^22, at least %d", (long long)x_stride, kQ8Pad, w->Kd);
     LASER_REQUIRE(out_stride >= w->outs && out_stride < (1ll << 32), LASER_E_INVALID_ARG, "rows of out overlap: stride %lld", (long long)out_stride);
     if (M == 0) return LASER_OK;
     LASER_REQUIRE(x && x_scales && out, LASER_E_INVALID_ARG, "NULL argument");
     const int64_t e = (int64_t)dtype_bytes(dtype);
     LASER_REQUIRE((uintptr_t)x % 16 == 0, LASER_E_INVALID_ARG, "x is not aligned to 16 bytes");
     LASER_REQUIRE((uintptr_t)out % e == 0 && (uintptr_t)x_scales % 4 == 0, LASER_E_INVALID_ARG, "out or x_scales is not aligned to its elements");
-    LASER_REQUIRE(rows_apart(out, w->outs * e, out_stride * e, x, w->Kp, x_stride, M) && rows_apart(out, w->outs * e, out_stride * e, x_scales, 4, 4, M), LASER_E_INVALID_ARG,
+    LASER_REQUIRE(rows_apart(out, w->outs * e, out_stride * e, x, (w->Kd + kQ8Pad - 1) / kQ8Pad * kQ8Pad, x_stride, M) && rows_apart(out, w->outs * e, out_stride * e, x_scales, 4, 4, M), LASER_E_INVALID_ARG,
                   "out overlaps x or x_scales");
     return launch_w8(w, x, x_stride, x_scales, M, dtype, out, out_stride, (hipStream_t)stream);
 }

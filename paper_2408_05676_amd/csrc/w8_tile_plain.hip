@@ -1,0 +1,8 @@
+// The tiles of products with 8-bit weights: instantiations, plain.
+#include "w8_tile.h"
+
+namespace laser {
+
+void launch_w8_tile_plain(const W8Args& a, int v, hipStream_t stream) { go_w8_tile<false>(a, v, stream); }
+
+}  // namespace laser

@@ -63,8 +63,9 @@ def gated(x, sx, w, sw):
     gate, up = p.chunk(2, -1)
     o = gate * torch.sigmoid(gate) * up
     # gate and up are 3 roundings off; silu takes a relative change d of its argument g to at most d (1 + |g|). exp(-g) is 2^(-g log2 e): the product and the
-    # constant are a rounding each, absolute in the exponent (2 |g| roundings), its own error 2 more; a sum, a quotient and a product: 3.
-    return o, 2.0 ** -24 * (3 * (1 + gate.abs()) + 3 + 2 * gate.abs() + 2 + 3) * o.abs() + 2.0 ** -110 * up.abs()
+    # constant are a rounding each, absolute in the exponent (2 |g| roundings), its own error a last place, 2 more; a sum (1), a reciprocal within
+    # a last place (2), two products (2).
+    return o, 2.0 ** -24 * (3 * (1 + gate.abs()) + 3 + 2 * gate.abs() + 2 + 5) * o.abs() + 2.0 ** -110 * up.abs()
 
 
 def gated_close(got, o, before):
