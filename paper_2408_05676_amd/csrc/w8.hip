@@ -1,7 +1,7 @@
 // Products of rows in 8-bit codes with 8-bit weights: out[M][outs] = s_x[row] s_w[output] sum c_x c_w, plain or gated (silu(gate) up).
 #include <algorithm>
 
-#include "w8_tile.h"
+#include "w8_few.h"
 
 namespace laser {
 
@@ -25,47 +25,33 @@ __global__ __launch_bounds__(256) void w8_layout_kernel(const int8_t* codes, con
     if (k == 0) out_scales[row] = n >= 0 ? scales[n] : 0.f;
 }
 
-// A wave per 16 rows and 16 outputs.
-template <int DT, bool GATED>
-__global__ __launch_bounds__(64) void w8_matmul_kernel(W8Args a) {
-    constexpr int NA = GATED ? 2 : 1;
-    const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
-    const int tiles = a.rows / (16 * NA), tile = blockIdx.x % tiles, row = blockIdx.x / tiles * 16 + r;
-    const int8_t* xp = a.x + (int64_t)min(row, a.M - 1) * a.x_stride + 16 * g;
-    const uint8_t* wp = a.w + (size_t)tile * NA * 1024 + lane * 16;
-    int4_t acc[NA] = {};
-    for (int k = 0; k < a.Kd; k += 64) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(xp + k);
-#pragma unroll
-        for (int j = 0; j < NA; ++j) acc[j] = mfma_i8(*reinterpret_cast<const u32x4*>(wp + (size_t)k * a.rows + j * 1024), x, acc[j]);
-    }
-    if (row >= a.M) return;
-    const float sx = a.x_scales[row];
-    float o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int n = tile * NA * 16 + 4 * g + i;
-        o[i] = (float)acc[0][i] * a.w_scales[n] * sx;           // (rows may be as large as fp32 goes, weights are not)
-        if constexpr (GATED) o[i] = silu_times(o[i], (float)acc[NA - 1][i] * a.w_scales[n + 16] * sx);
-    }
-    w8_store<DT>(a, row, tile * 16 + 4 * g, o);
-}
-
-template <int DT, bool GATED>
-static void launch_rows(const W8Args& a, hipStream_t stream) {
-    const long units = (long)(a.rows / (GATED ? 32 : 16)) * ((a.M + 15) / 16);
-    hipLaunchKernelGGL((w8_matmul_kernel<DT, GATED>), dim3((unsigned)units), dim3(64), 0, stream, a);
-}
-
-static int w8_shape(const W8Args& a, int ncu) {
+// Which kernel a launch takes: 0 .. kW8FewN - 1 of w8_few.h, beyond of w8_tile.h.
+//
+// Up to 16 rows: one output fragment and eight waves where that is at most a workgroup for each of 256 compute units, else two and four (6144 outputs of 2048
+// inputs, one row 5.0 us, the other way 5.9; 4096 x 4096 6.1 and 6.2; 4096 x 11008 10.3 and 12.5).
+// More rows: the least of the microseconds below, which grow with the workgroups of a compute unit and their stages. Fitted by least squares to what every kernel within
+// 1.4 of the fastest took, at 17 to 1000 rows of ten matrices (256 x 768 to 4096 x 2 x 11008) and of 400 random ones: 3700 measurements. What it takes is 0.5 % slower
+// than the fastest on average at the ten, 1 % at the random ones, 26 % at worst (814 rows 768 -> 9443: 18.9 us of 15.1).
+static int w8_pick(const W8Args& a, bool gated) {
+    constexpr int cus = 256;
+    const int frags = a.rows / 16;
+    const double k = a.Kp / 1024.0, weights = 1e-6 * a.rows * a.Kp, results = 2e-6 * a.M * a.outs;
+    auto up = [](long a, long b) { return (a + b - 1) / b; };
+    if (a.M <= 16) return (a.M <= 4 ? 0 : 2) + (gated || frags > cus);
     int best = 0;
-    double best_cost = 1e300;
-    for (int v = 0; v < kW8Shapes_; ++v) {
-        const int bm = kW8Shapes[v].wm * 16, bn = kW8Shapes[v].wn * 64;
-        const long units = (long)((a.M + bm - 1) / bm) * ((a.rows + bn - 1) / bn), rounds = (units + ncu - 1) / ncu;
-        const double step = 2.0 * kW8Shapes[v].wm * kW8Shapes[v].wn * 16 + 5.0 * (bm + bn) / 8;
-        const double cost = (double)rounds * (a.Kp / 128 * step + 8000.0);
-        if (cost < best_cost) { best_cost = cost; best = v; }
+    double least = 1e300;
+    for (int v = 0; v < kW8FewN; ++v) {
+        const W8Few f = kW8Few[v];
+        if (f.mt == 0 || (gated && f.nt % 2)) continue;
+        const double each = (double)up(up(frags, f.nt) * up(a.M, 16 * f.mt), cus);
+        const double us = 3.02 + each * (k * (0.141 * f.nt + 0.161 * f.mt) + 0.122 + 0.0945 * f.nt * f.mt) + 0.102 * weights + 0.509 * results;
+        if (us < least) { least = us; best = v; }
+    }
+    for (int v = 0; v < kW8ShapeN; ++v) {
+        const W8Shape s = kW8Shapes[v];
+        const double each = (double)up(up(a.M, s.wm * 16) * up(a.rows, s.wn * 64), cus);
+        const double us = 3.35 + each * (k * (0.0817 * s.wm * s.wn + 0.0654 * s.wm + 0.406 * s.wn) + 0.1 * s.wm * s.wn) + 0.428 * k + 0.0903 * weights + 0.228 * results;
+        if (us < least) { least = us; best = kW8FewN + v; }
     }
     return best;
 }
@@ -73,20 +59,10 @@ static int w8_shape(const W8Args& a, int ncu) {
 int launch_w8(const W8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, hipStream_t stream) {
     LASER_REQUIRE((long)(w->rows / 16) * ((M + 15) / 16) < (1l << 25), LASER_E_LIMIT, "%d rows times %d outputs are too many for a launch", M, w->rows);
     const W8Args a{w->codes, w->scales, x, x_scales, out, x_stride, out_stride, M, w->outs, w->rows, w->Kd, w->Kp, dtype, 0, 0};
-    if (M > 16) {
-        const int v = w8_shape(a, 256);
-        if (w->gated) launch_w8_tile_gated(a, v, stream);
-        else launch_w8_tile_plain(a, v, stream);
-        LASER_HIP_CHECK(hipGetLastError());
-        return LASER_OK;
-    }
-    auto go = [&](auto dt) {
-        if (w->gated) launch_rows<decltype(dt)::value, true>(a, stream);
-        else launch_rows<decltype(dt)::value, false>(a, stream);
-    };
-    if (dtype == DT_F32) go(std::integral_constant<int, DT_F32>{});
-    else if (dtype == DT_BF16) go(std::integral_constant<int, DT_BF16>{});
-    else go(std::integral_constant<int, DT_F16>{});
+    const int v = w8_pick(a, w->gated);
+    if (v < kW8FewN) launch_w8_few(a, w->gated, v, stream);
+    else if (w->gated) launch_w8_tile_gated(a, v - kW8FewN, stream);
+    else launch_w8_tile_plain(a, v - kW8FewN, stream);
     LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
 }

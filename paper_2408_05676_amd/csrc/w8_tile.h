@@ -31,6 +31,13 @@ __device__ inline void w8_store(const W8Args& a, int row, int n, const float (&o
         }
 }
 
+// 16 bytes a lane from base + vo to LDS at `at`, lane after lane. m0 holds the address, one wait state before its use.
+__device__ inline void load_to_lds(uint64_t base, uint32_t vo, uint32_t at) {
+    const u32x4 srd{(uint32_t)base, (uint32_t)(base >> 32), 0xFFFFFFFFu, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" ::"v"(vo), "s"(at), "s"(srd) : "memory", "m0");
+}
+__device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+
 __device__ inline void mfma_i8_acc(const u32x4& w, const u32x4& x, int4_t& c) {
     asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
 }
@@ -69,14 +76,13 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
         voff[j] = (uint32_t)min(row, a.M - 1 - tm * BM) * (uint32_t)a.x_stride + (((lane & 7) ^ ((row >> 1) & 7)) * 16);
     }
     uint64_t xbase = (uint64_t)(uintptr_t)a.x + (uint64_t)tm * BM * a.x_stride;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
+    const uint32_t lds0 = lds_address(lds) + wave * 1024;
     const uint32_t last = lds0 + (PIECES - 1 - wave) * 1024;
     uint32_t lslot = 0;
     auto issue = [&](auto jc) {
         constexpr int j = decltype(jc)::value;
-        const u32x4 srd{(uint32_t)xbase, (uint32_t)(xbase >> 32), 0xFFFFFFFFu, 0x00020000u};
-        const uint32_t vo = voff[j], at = (PIECES % NW != 0 && j == LPS - 1 && wave + j * NW >= PIECES ? last : lds0 + j * NW * 1024) + lslot;
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" ::"v"(vo), "s"(at), "s"(srd) : "memory", "m0");
+        const uint32_t at = (PIECES % NW != 0 && j == LPS - 1 && wave + j * NW >= PIECES ? last : lds0 + j * NW * 1024) + lslot;
+        load_to_lds(xbase, voff[j], at);
     };
     int kreq = 0;
     auto next_stage = [&] {
@@ -104,7 +110,7 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
     const uint32_t touch = (uint32_t)(line / (WN * 8 * NW)) * (uint32_t)wstep + (uint32_t)min(line % (WN * 8 * NW), step_lines - 1) * 128;
     uint64_t tbase = (uint64_t)(uintptr_t)a.w + (uint64_t)tile0 * 64;
     int treq = 0;
-    const uint32_t junk = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + SBYTES * NS + wave * 256;
+    const uint32_t junk = lds_address(lds) + SBYTES * NS + wave * 256;
     auto touch_ahead = [&] {
         if (a.tiles_m > 1) {
             const u32x4 srd{(uint32_t)tbase, (uint32_t)(tbase >> 32), 0xFFFFFFFFu, 0x00020000u};
@@ -232,8 +238,8 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
 }
 
 struct W8Shape { int wm, wn; };
-constexpr W8Shape kW8Shapes[] = {{2, 2}, {3, 2}, {4, 2}, {5, 2}, {6, 2}, {8, 2}, {11, 2}, {3, 4}, {4, 4}, {5, 4}, {6, 4}, {8, 4}, {11, 4}, {6, 6}, {8, 6}, {11, 6}};
-constexpr int kW8Shapes_ = (int)(sizeof(kW8Shapes) / sizeof(kW8Shapes[0]));
+constexpr W8Shape kW8Shapes[] = {{2, 2}, {3, 2}, {4, 2}, {5, 2}, {6, 2}, {8, 2}, {5, 4}, {8, 4}, {6, 6}, {8, 6}, {11, 6}};
+constexpr int kW8ShapeN = (int)(sizeof(kW8Shapes) / sizeof(kW8Shapes[0]));
 
 template <int J, int N, class F>
 static void each(F&& f) {
@@ -242,7 +248,7 @@ static void each(F&& f) {
 
 template <bool GATED>
 inline void go_w8_tile(W8Args a, int v, hipStream_t stream) {
-    each<0, kW8Shapes_>([&](auto vc) {
+    each<0, kW8ShapeN>([&](auto vc) {
         if (decltype(vc)::value != v) return;
         constexpr int WM = kW8Shapes[decltype(vc)::value].wm, WN = kW8Shapes[decltype(vc)::value].wn;
         a.tiles_m = (a.M + WM * 16 - 1) / (WM * 16);
