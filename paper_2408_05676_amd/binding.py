@@ -584,90 +584,84 @@ def w4_matmul(w: W4, x: torch.Tensor, out=None, stream=None) -> torch.Tensor:
 Q8_PAD = 128                                                                     # rows of codes lie multiples of this many bytes apart
 
 
-def _rows(t: torch.Tensor, name: str, shape, dtype, dev: int) -> int:
-    """Checks a [M][N] tensor with contiguous rows; its row stride."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.shape != shape:
-        raise LaserError(f"{name} must be a CUDA tensor {list(shape)} of {dtype}")
+def _rows(t: torch.Tensor, name: str, M: int, N: int, dtype, dev: int) -> int:
+    """Checks a [M][N] tensor with contiguous rows on device dev; its row stride. (A call takes some microseconds on the device: few attributes are read.)"""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != (M, N):
+        raise LaserError(f"{name} must be a CUDA tensor [{M}][{N}] of {dtype}")
     if t.get_device() != dev:
         raise LaserError(f"{name} is on {t.device}, not on the current device")
-    if shape[1] > 1 and t.stride(1) != 1 and shape[0]:
+    step, one = t.stride()
+    if one != 1 and N > 1 and M:
         raise LaserError(f"{name} must have contiguous rows")
-    return t.stride(0) if shape[0] > 1 else -(-shape[1] // Q8_PAD) * Q8_PAD
+    return step if M > 1 else -(-N // Q8_PAD) * Q8_PAD
 
 
-def _q8_out(out, M: int, N: int, device, dev: int, stream):
-    """(codes, their stride, scales) of M rows of N."""
-    if out is None:
-        codes = _out((M, -(-N // Q8_PAD) * Q8_PAD), torch.int8, device, stream)[:, :N]
-        return codes, codes.stride(0), _out((M,), torch.float32, device, stream)
-    codes, scales = out
-    step = _rows(codes, "codes", (M, N), torch.int8, dev)
-    _q8_scales(scales, M, dev)
-    return codes, step, scales
+def _line(t: torch.Tensor, name: str, M: int, dev: int) -> int:
+    """Checks a contiguous float32 [M] on device dev; its address."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (M,) or not t.is_contiguous():
+        raise LaserError(f"{name} must be a contiguous CUDA tensor [{M}] of float32")
+    if t.get_device() != dev:
+        raise LaserError(f"{name}: on {t.device}, not on the current device")
+    return t.data_ptr()
 
 
-def _q8_scales(scales, M: int, dev: int) -> None:
-    if not isinstance(scales, torch.Tensor) or not scales.is_cuda or scales.dtype != torch.float32 or scales.shape != (M,) or not scales.is_contiguous():
-        raise LaserError(f"scales must be a contiguous CUDA tensor [{M}] of float32")
-    if scales.get_device() != dev:
-        raise LaserError(f"scales are on {scales.device}, not on the current device")
+def _two_dims(t, name: str, what: str):
+    """(device in use, M, N) of a CUDA tensor with two dimensions."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise LaserError(f"{name} must be a CUDA tensor [M][N] of {what}")
+    return (_device(), *t.shape)
 
 
-def _q8_in(x):
-    """(device, M, N, dtype code, row stride) of rows that go into 8 bits."""
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 2 or x.dtype not in _DTYPES:
-        raise LaserError("x must be a CUDA tensor [M][N] of float16, bfloat16 or float32")
-    dev = _device()
-    return (dev, *x.shape, _DTYPES[x.dtype], _rows(x, "x", x.shape, x.dtype, dev))
+def _float_code(t, name: str) -> int:
+    dt = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if dt is None:
+        raise LaserError(f"{name} must be of float16, bfloat16 or float32")
+    return dt
+
+
+def _q8_out(M: int, N: int, device, stream):
+    """Memory for the codes and scales of M rows of N."""
+    return _out((M, -(-N // Q8_PAD) * Q8_PAD), torch.int8, device, stream)[:, :N], _out((M,), torch.float32, device, stream)
 
 
 def q8_rows(x: torch.Tensor, out=None, stream=None):
     """laser_q8_rows: x [M][N] -> (codes int8 [M][N], scales float32 [M]). The codes' rows are Q8_PAD bytes' multiples apart, as w8_matmul wants them;
     out: two such tensors to write to (codes of any row stride, if they are for q8_read only)."""
-    dev, M, N, dt, step = _q8_in(x)
-    codes, cs, scales = _q8_out(out, M, N, x.device, dev, stream)
-    _check(lib().laser_q8_rows(x.data_ptr(), step, M, N, dt, codes.data_ptr(), cs, scales.data_ptr(), _on(stream, dev)), "laser_q8_rows")
+    dev, M, N = _two_dims(x, "x", "float16, bfloat16 or float32")
+    dt, step = _float_code(x, "x"), _rows(x, "x", M, N, x.dtype, dev)
+    codes, scales = _q8_out(M, N, x.device, stream) if out is None else out
+    _check(lib().laser_q8_rows(x.data_ptr(), step, M, N, dt, codes.data_ptr(), _rows(codes, "codes", M, N, torch.int8, dev), _line(scales, "scales", M, dev),
+                               _on(stream, dev)), "laser_q8_rows")
     return codes, scales
 
 
 def q8_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, residual=None, residual_out=None, out=None, stream=None):
     """laser_q8_norm: (codes, scales) of the root-mean-square norm of x + residual times gain (float32 [N]); the sum goes to residual_out (None: to
     residual itself). residual: float32 or x's type, or None."""
-    dev, M, N, dt, step = _q8_in(x)
-    if not isinstance(gain, torch.Tensor) or not gain.is_cuda or gain.dtype != torch.float32 or gain.shape != (N,) or not gain.is_contiguous():
-        raise LaserError(f"gain must be a contiguous CUDA tensor [{N}] of float32")
-    _here(gain, "gain", dev)
-    rp = rs = op = os_ = 0
-    rdt = dt
+    dev, M, N = _two_dims(x, "x", "float16, bfloat16 or float32")
+    dt, step = _float_code(x, "x"), _rows(x, "x", M, N, x.dtype, dev)
+    rp, rs, op, os_, rdt = None, 0, None, 0, dt
     if residual is not None:
-        if not isinstance(residual, torch.Tensor) or residual.dtype not in (x.dtype, torch.float32):
-            raise LaserError(f"residual must be a CUDA tensor [{M}][{N}] of {x.dtype} or float32")
+        rdt = _float_code(residual, "residual")
         if residual_out is None:
             residual_out = residual
-        rdt = _DTYPES[residual.dtype]
-        rs, os_ = _rows(residual, "residual", (M, N), residual.dtype, dev), _rows(residual_out, "residual_out", (M, N), residual.dtype, dev)
+        rs, os_ = _rows(residual, "residual", M, N, residual.dtype, dev), _rows(residual_out, "residual_out", M, N, residual.dtype, dev)
         rp, op = residual.data_ptr(), residual_out.data_ptr()
     elif residual_out is not None:
         raise LaserError("residual_out without a residual")
-    codes, cs, scales = _q8_out(out, M, N, x.device, dev, stream)
-    _check(lib().laser_q8_norm(x.data_ptr(), step, dt, rp, rs, op, os_, rdt, gain.data_ptr(), eps, M, N, codes.data_ptr(), cs, scales.data_ptr(),
-                               _on(stream, dev)), "laser_q8_norm")
+    codes, scales = _q8_out(M, N, x.device, stream) if out is None else out
+    _check(lib().laser_q8_norm(x.data_ptr(), step, dt, rp, rs, op, os_, rdt, _line(gain, "gain", N, dev), eps, M, N, codes.data_ptr(),
+                               _rows(codes, "codes", M, N, torch.int8, dev), _line(scales, "scales", M, dev), _on(stream, dev)), "laser_q8_norm")
     return codes, scales
 
 
 def q8_read(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.float16, out=None, stream=None) -> torch.Tensor:
     """laser_q8_read: what rows of codes stand for, [M][N] of dtype (or of out's)."""
-    if not isinstance(codes, torch.Tensor) or not codes.is_cuda or codes.dim() != 2:
-        raise LaserError("codes must be a CUDA tensor [M][N] of int8")
-    dev, (M, N) = _device(), codes.shape
-    step = _rows(codes, "codes", (M, N), torch.int8, dev)
-    _q8_scales(scales, M, dev)
+    dev, M, N = _two_dims(codes, "codes", "int8")
     if out is None:
         out = _out((M, N), dtype, codes.device, stream)
-    if not isinstance(out, torch.Tensor) or out.dtype not in _DTYPES:
-        raise LaserError("out must be of float16, bfloat16 or float32")
-    _check(lib().laser_q8_read(codes.data_ptr(), step, scales.data_ptr(), M, N, _DTYPES[out.dtype], out.data_ptr(), _rows(out, "out", (M, N), out.dtype, dev),
-                               _on(stream, dev)), "laser_q8_read")
+    _check(lib().laser_q8_read(codes.data_ptr(), _rows(codes, "codes", M, N, torch.int8, dev), _line(scales, "scales", M, dev), M, N, _float_code(out, "out"),
+                               out.data_ptr(), _rows(out, "out", M, N, out.dtype, dev), _on(stream, dev)), "laser_q8_read")
     return out
 
 
@@ -719,22 +713,17 @@ def w8_matmul(w: W8, x: torch.Tensor, scales: torch.Tensor, dtype=torch.float16,
     """laser_w8_matmul: rows of codes x int8 [M][Kd] with their scales (q8_rows, q8_norm) -> [M][w.outs] of dtype (or of out's)."""
     if not isinstance(w, W8) or not w._h:
         raise LaserError("w must be a W8 that has not been closed")
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 2:
-        raise LaserError(f"x must be a CUDA tensor [M][{w.Kd}] of int8")
-    dev, M, Kd = _device(), x.shape[0], w.Kd
+    dev, M, Kd = _two_dims(x, "x", "int8")
     if w.device != dev:
         raise LaserError(f"the weights are on device {w.device}, not on the current one")
-    step = _rows(x, "x", (M, Kd), torch.int8, dev)
+    step = _rows(x, "x", M, w.Kd, torch.int8, dev)
     # a row's bytes up to the next multiple of Q8_PAD are read
     if Kd % Q8_PAD and M and x.storage_offset() + (M - 1) * step + -(-Kd // Q8_PAD) * Q8_PAD > x.untyped_storage().nbytes():
         raise LaserError(f"rows of x must lie multiples of {Q8_PAD} bytes apart, and the memory of the last one reach as far")
-    _q8_scales(scales, M, dev)
     if out is None:
         out = _out((M, w.outs), dtype, x.device, stream)
-    if not isinstance(out, torch.Tensor) or out.dtype not in _DTYPES:
-        raise LaserError("out must be of float16, bfloat16 or float32")
-    _check(lib().laser_w8_matmul(w._h, x.data_ptr(), step, scales.data_ptr(), M, _DTYPES[out.dtype], out.data_ptr(), _rows(out, "out", (M, w.outs), out.dtype, dev),
-                                 _on(stream, dev)), "laser_w8_matmul")
+    _check(lib().laser_w8_matmul(w._h, x.data_ptr(), step, _line(scales, "scales", M, dev), M, _float_code(out, "out"), out.data_ptr(),
+                                 _rows(out, "out", M, w.outs, out.dtype, dev), _on(stream, dev)), "laser_w8_matmul")
     return out
 
 

@@ -3,7 +3,10 @@
 // h = x + res, u = h gain (u = x without the norm), m = max |u|: codes c = rint(127 u / m) and scale s = m / 127 / sqrt(mean h^2 + eps).
 // The root is the same for a row's elements, so codes need the extremes of h gain only. All in 64 bits, where x + res and the
 // products are exact: a code is the formula's whatever the order of operations, and squares of any fp32 rows have room. t = u (127 / m) is
-// off by some 2^-46; only where it is closer than 2^-30 to a half is the quotient itself taken.
+// off by some 2^-45; only where it is closer than 2^-30 to a half is the quotient itself taken.
+// Bound: a launch and one round trip to memory up to some hundred rows (1 x 4096 3.0 us, with the norm 3.7; an empty launch 2.3), then both and the vector
+// instructions of the codes: 704 x 11008 fp16 8.8 us (2.6 TB/s; a copy of as many bytes takes 4.6), the norm of 704 x 4096 with its residual in bf16 8.3 us (2.4 TB/s). Reading back 5.3 us
+// (704 x 11008, 4.4 TB/s).
 #include <algorithm>
 
 #include "eight_bit.h"
@@ -25,80 +28,300 @@ __device__ inline void store_elem(void* p, int64_t o, float x) {
     else ((uint16_t*)p)[o] = f32_to_f16(x);
 }
 
-struct RowStats { double m, ss, bad; };              // largest |u|, sum of h^2, not 0 (NaN) if some u is not finite
-
-__device__ inline RowStats wave_stats(RowStats s) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        s.m = fmax(s.m, __shfl_xor(s.m, o));
-        s.ss += __shfl_xor(s.ss, o);
-        s.bad += __shfl_xor(s.bad, o);
+// Eight elements of a row as they lie in memory
+template <int DT>
+struct Raw8 {
+    uint32_t w[DT == DT_F32 ? 8 : 4];
+    __device__ float get(int i) const {
+        if constexpr (DT == DT_F32) return __uint_as_float(w[i]);
+        else if constexpr (DT == DT_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        else return f16_to_f32((uint16_t)(w[i / 2] >> (16 * (i & 1))));
     }
-    return s;
+};
+template <int DT>
+__device__ inline void load8(Raw8<DT>& r, const void* p, int64_t o) {
+    if constexpr (DT == DT_F32) {
+        const f32x4_a4 *q = reinterpret_cast<const f32x4_a4*>((const float*)p + o), a = q[0], b = q[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { r.w[i] = __float_as_uint(a[i]); r.w[4 + i] = __float_as_uint(b[i]); }
+    } else {
+        const u32x4_a2 a = *reinterpret_cast<const u32x4_a2*>((const uint16_t*)p + o);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = a[i];
+    }
 }
+// The first `left` (1 .. 7) of them, zeros behind.
+template <int DT>
+__device__ inline void load_tail(Raw8<DT>& r, const void* p, int64_t o, int left) {
+#pragma unroll
+    for (uint32_t& w : r.w) w = 0;
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) {
+            if constexpr (DT == DT_F32) r.w[i] = ((const uint32_t*)p)[o + i];
+            else r.w[i / 2] |= (uint32_t)((const uint16_t*)p)[o + i] << (16 * (i & 1));
+        }
+}
+template <int DT>
+__device__ inline void store8(void* p, int64_t o, int left, const float (&x)[8]) {
+    if (left >= 8) { store_elems<DT, 8>(p, o, x); return; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < left) store_elem<DT>(p, o + i, x[i]);
+}
+typedef unsigned u32x2_a1 __attribute__((ext_vector_type(2), aligned(1)));
 
-__device__ inline int q8_code(double u, double inv, double m) {
+// rint(127 u / m) in the low byte; inv = 127 / m. Adding 1.5 2^52 rounds to nearest even and leaves the whole number in the low bits.
+__device__ inline uint32_t q8_code(double u, double inv, double m) {
+    constexpr double kWhole = 0x1.8p52;
     const double t = u * inv;
-    double c = rint(t);
-    if (fabs(t - c) > 0.5 - 0x1p-30) c = rint(127.0 * u / m);
-    return (int)c;
+    double c = t + kWhole;
+    if (fabs(t - (c - kWhole)) > 0.5 - 0x1p-30) c = 127.0 * u / m + kWhole;
+    return (uint32_t)__builtin_bit_cast(uint64_t, c);
 }
 
-template <int DT, int RT>
-__global__ __launch_bounds__(256) void q8_rows_kernel(Q8Args a) {
-    __shared__ RowStats sm[4];
+// x of another lane of the same sixteen (dpp control CTRL)
+template <int CTRL, class T>
+__device__ inline T row_move(T x) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+    else {
+        const uint64_t u = __builtin_bit_cast(uint64_t, x);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, true), hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xF, 0xF, true);
+        return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
+    }
+}
+// op over a wave, in every lane: pairs, fours, eights and sixteens by lane moves, then rows of sixteen
+template <class T, class F>
+__device__ inline T wave_fold(T x, F op) {
+    x = op(x, row_move<0xB1>(x));                    // lanes 1 0 3 2 of four
+    x = op(x, row_move<0x4E>(x));                    // lanes 2 3 0 1
+    x = op(x, row_move<0x141>(x));                   // eight lanes mirrored
+    x = op(x, row_move<0x140>(x));                   // sixteen mirrored
+    x = op(x, __shfl_xor(x, 16));
+    return op(x, __shfl_xor(x, 32));
+}
+__device__ inline double wave_max(double x) { return wave_fold(x, [](double a, double b) { return fmax(a, b); }); }
+__device__ inline float wave_max(float x) { return wave_fold(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ inline double wave_sum(double x) { return wave_fold(x, [](double a, double b) { return a + b; }); }
+
+// A row's scale. m: its largest |u|.
+template <bool NORM>
+__device__ inline float row_scale(double m, double ss, bool bad, int N, float eps) {
+    double d = 127.0;
+    if (NORM && m > 0) d *= sqrt(ss / N + (double)eps);
+    return bad ? __builtin_nanf("") : (float)(m / d);
+}
+
+// WPR waves a row (four rows a workgroup where that is one), NV times eight columns a thread: the row stays in registers between its statistics and its codes.
+//
+// Codes take 32-bit numbers wherever those decide: h, u, m, its reciprocal (two), 127 times that and t are a rounding each, so t is within 127 7 2^-24 < 2^-14
+// of the formula's (sums of two floats never lose a small part; a product that does is 2^-66 of m). Elements closer than that to a half take 64 bits, one
+// at a time: with all eight of a thread's where one is close, 704 rows of 11008 took 11.4 us, so 8.9.
+template <int DT, int RT, bool NORM, int WPR, int NV>
+__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Args a) {
+    __shared__ double sm_m[WPR], sm_ss[WPR];
+    __shared__ int sm_bad[WPR];
+    const int wave = threadIdx.x >> 6, t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t row = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+    if (WPR == 1 && row >= a.M) return;
+    constexpr bool RES = RT != kNoResidual;
+    Raw8<DT> x[NV];
+    Raw8<RES ? RT : DT_F16> r[RES ? NV : 1];
+    Raw8<DT_F32> g[NORM ? NV : 1];
+    // All loads go out together, without a branch: a row has eight elements at least, and behind its end its last eight come again.
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = min((v * WPR * 64 + t) * 8, a.N - 8);
+        load8<DT>(x[v], a.x, row * a.x_stride + c);
+        if constexpr (RES) load8<RT>(r[v], a.res, row * a.res_stride + c);
+        if constexpr (NORM) load8<DT_F32>(g[v], a.gain, c);
+    }
+    asm volatile("" ::: "memory");
+    if (a.N & 7)
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * WPR * 64 + t) * 8, left = a.N - c;
+            if (left > 0 && left < 8) {
+                load_tail<DT>(x[v], a.x, row * a.x_stride + c, left);
+                if constexpr (RES) load_tail<RT>(r[v], a.res, row * a.res_stride + c, left);
+                if constexpr (NORM) load_tail<DT_F32>(g[v], a.gain, c, left);
+            }
+        }
+    double m = 0, ss = 0;
+    float m32 = 0, z = 0;                                // z: NaN where x or the gain is not finite (the norm: where the gain is not)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int left = a.N - (v * WPR * 64 + t) * 8;
+        if (left <= 0) continue;
+        if constexpr (DT == DT_F32 && NORM)
+            for (int p = 1; p < a.n_part; ++p) {         // sums of reduction parts (of whole pieces: the library's own), added to the first in fp32
+                Raw8<DT_F32> q;
+                load8<DT_F32>(q, a.x, row * a.x_stride + a.N - left + p * a.part_stride);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[v].w[i] = __float_as_uint(x[v].get(i) + q.get(i));
+            }
+        if constexpr (NORM) {
+            float sum[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                double h = (double)x[v].get(i);
+                if constexpr (RES) h += (double)r[v].get(i);
+                m = fmax(m, fabs(h * (double)g[v].get(i)));
+                ss = fma(h, h, ss);
+                z = fmaf(g[v].get(i), 0.f, z);
+                sum[i] = (float)h;
+            }
+            if constexpr (RES) store8<RT>(a.res_out, row * a.res_out_stride + a.N - left, left, sum);
+        } else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                m32 = fmaxf(m32, fabsf(x[v].get(i)));
+                z = fmaf(x[v].get(i), 0.f, z);
+            }
+    }
+    if constexpr (NORM) { m = wave_max(m); ss = wave_sum(ss); }
+    else m = (double)wave_max(m32);
+    bool bad = __any(!(z == 0)) || !(ss < INFINITY);     // (squares of finite sums do not pass 64 bits)
+    if constexpr (WPR > 1) {
+        if ((t & 63) == 0) { sm_m[wave] = m; sm_ss[wave] = ss; sm_bad[wave] = bad; }
+        __syncthreads();
+        m = sm_m[0]; ss = sm_ss[0]; bad = sm_bad[0];
+#pragma unroll
+        for (int w = 1; w < WPR; ++w) { m = fmax(m, sm_m[w]); ss += sm_ss[w]; bad |= (bool)sm_bad[w]; }
+    }
+    const bool some = m > 0 && !bad, usual = m >= 0x1p-60 && m <= 0x1p60;
+    const float inv32 = 127.f * __builtin_amdgcn_rcpf((float)m);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = (v * WPR * 64 + t) * 8, left = a.N - c;
+        if (left <= 0) continue;
+        uint32_t w[2] = {0, 0};
+        if (some) {
+            uint32_t close = usual ? 0 : 255;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                constexpr float kWhole = 0x1.8p23f;      // as in q8_code
+                float u = x[v].get(i);
+                if constexpr (RES) u += r[v].get(i);
+                if constexpr (NORM) u *= g[v].get(i);
+                const float y = u * inv32, n = y + kWhole;
+                close |= !(fabsf(y - (n - kWhole)) <= 0.5f - 0x1p-14f) ? 1u << i : 0u;
+                w[i / 4] |= (__float_as_uint(n) & 255u) << (8 * (i & 3));
+            }
+            while (close) {
+                const int i = __ffs(close) - 1;
+                close &= close - 1;
+                auto pick = [&](const auto& q) {
+                    float e = q.get(0);
+                    static_for<1, 8>([&](auto k) { e = i == decltype(k)::value ? q.get(decltype(k)::value) : e; });
+                    return e;
+                };
+                double u = (double)pick(x[v]);
+                if constexpr (RES) u += (double)pick(r[v]);
+                if constexpr (NORM) u *= (double)pick(g[v]);
+                const uint32_t code = (q8_code(u, 127.0 / m, m) & 255u) << (8 * (i & 3)), keep = ~(255u << (8 * (i & 3)));
+                if (i < 4) w[0] = (w[0] & keep) | code;
+                else w[1] = (w[1] & keep) | code;
+            }
+        }
+        int8_t* to = a.codes + row * a.codes_stride + c;
+        if (left >= 8) *reinterpret_cast<u32x2_a1*>(to) = u32x2_a1{w[0], w[1]};
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) to[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
+    }
+    if (t == 0) a.scales[row] = row_scale<NORM>(m, ss, bad, a.N, a.eps);
+}
+
+// Rows of any length (a wave for those below eight elements): read twice, the sum written the second time (it may go where the residual came from).
+template <int DT, int RT, bool NORM>
+__global__ __launch_bounds__(1024) void q8_long_rows_kernel(Q8Args a) {
+    __shared__ double sm_m[16], sm_ss[16];
+    __shared__ int sm_bad[16];
     const int64_t row = blockIdx.x;
     const int t = threadIdx.x;
     double h = 0;
-    auto value = [&](int i) {                        // u of column i; h on the side
-        h = (double)load_elem<DT>(a.x, row * a.x_stride + i);
+    auto value = [&](int i) {
+        float x = load_elem<DT>(a.x, row * a.x_stride + i);
         if constexpr (DT == DT_F32)
-            for (int p = 1; p < a.n_part; ++p) h += (double)((const float*)a.x)[row * a.x_stride + i + p * a.part_stride];
+            for (int p = 1; p < a.n_part; ++p) x += ((const float*)a.x)[row * a.x_stride + i + p * a.part_stride];
+        h = (double)x;
         if constexpr (RT != kNoResidual) h += (double)load_elem<RT>(a.res, row * a.res_stride + i);
-        return a.gain ? h * (double)a.gain[i] : h;
+        return NORM ? h * (double)a.gain[i] : h;
     };
-    RowStats s{0, 0, 0};
-    for (int i = t; i < a.N; i += 256) {
+    double m = 0, ss = 0, z = 0;
+    for (int i = t; i < a.N; i += (int)blockDim.x) {
         const double u = value(i);
-        s.m = fmax(s.m, fabs(u));
-        s.ss = fma(h, h, s.ss);
-        s.bad = fma(u, 0.0, s.bad);
+        m = fmax(m, fabs(u));
+        ss = fma(h, h, ss);
+        z = fma(u, 0.0, fma(h, 0.0, z));
     }
-    s = wave_stats(s);
-    if ((t & 63) == 0) sm[t >> 6] = s;
+    m = wave_max(m);
+    ss = wave_sum(ss);
+    bool bad = __any(!(z == 0));
+    if ((t & 63) == 0) { sm_m[t >> 6] = m; sm_ss[t >> 6] = ss; sm_bad[t >> 6] = bad; }
     __syncthreads();
-    s = sm[0];
-    for (int w = 1; w < 4; ++w) { s.m = fmax(s.m, sm[w].m); s.ss += sm[w].ss; s.bad += sm[w].bad; }
-    const bool bad = !(s.bad == 0) || !__builtin_isfinite(s.ss);
-    const double inv = s.m > 0 && !bad ? 127.0 / s.m : 0.0;
-    for (int i = t; i < a.N; i += 256) {
+    m = sm_m[0]; ss = sm_ss[0]; bad = sm_bad[0];
+    for (int w = 1; w < (int)blockDim.x / 64; ++w) { m = fmax(m, sm_m[w]); ss += sm_ss[w]; bad |= (bool)sm_bad[w]; }
+    const double inv = m > 0 && !bad ? 127.0 / m : 0.0;
+    for (int i = t; i < a.N; i += (int)blockDim.x) {
         const double u = value(i);
-        a.codes[row * a.codes_stride + i] = inv > 0 ? (int8_t)q8_code(u, inv, s.m) : (int8_t)0;
+        a.codes[row * a.codes_stride + i] = inv > 0 ? (int8_t)q8_code(u, inv, m) : (int8_t)0;
         if constexpr (RT != kNoResidual) store_elem<RT>(a.res_out, row * a.res_out_stride + i, (float)h);
     }
-    if (t == 0) {
-        double scale = s.m / 127.0;
-        if (a.gain && s.m > 0) scale /= sqrt(s.ss / a.N + (double)a.eps);
-        a.scales[row] = bad ? __builtin_nanf("") : (float)scale;
-    }
+    if (t == 0) a.scales[row] = row_scale<NORM>(m, ss, bad, a.N, a.eps);
 }
 
+// Eight elements a thread.
 template <int DT>
 __global__ __launch_bounds__(256) void q8_read_kernel(const int8_t* codes, int64_t codes_stride, const float* scales, int N, void* out, int64_t out_stride) {
     const int64_t row = blockIdx.x;
     const float s = scales[row];
-    for (int i = threadIdx.x; i < N; i += 256) store_elem<DT>(out, row * out_stride + i, s * (float)codes[row * codes_stride + i]);
+    for (int64_t c = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * 8; c < N; c += (int64_t)gridDim.y * blockDim.x * 8) {
+        const int8_t* from = codes + row * codes_stride + c;
+        const int left = (int)(N - c);
+        union { u32x2_a1 v; int8_t b[8]; } q{};
+        if (left >= 8) q.v = *reinterpret_cast<const u32x2_a1*>(from);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < left) q.b[i] = from[i];
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = s * (float)q.b[i];
+        store8<DT>(out, row * out_stride + c, left, x);
+    }
+}
+
+template <int DT, int RT, bool NORM>
+static void launch_rows(const Q8Args& a, hipStream_t stream) {
+    const long pieces = (a.N + 7l) / 8;
+    auto go = [&](auto wprc, auto nvc) {
+        constexpr int WPR = decltype(wprc)::value, NV = decltype(nvc)::value;
+        hipLaunchKernelGGL((q8_rows_kernel<DT, RT, NORM, WPR, NV>), dim3(WPR == 1 ? (a.M + 3) / 4 : a.M), dim3(WPR == 1 ? 256 : WPR * 64), 0, stream, a);
+    };
+    using C1 = std::integral_constant<int, 1>;
+    using C2 = std::integral_constant<int, 2>;
+    using C4 = std::integral_constant<int, 4>;
+    using C8 = std::integral_constant<int, 8>;
+    using C16 = std::integral_constant<int, 16>;
+    if (a.N < 8) hipLaunchKernelGGL((q8_long_rows_kernel<DT, RT, NORM>), dim3(a.M), dim3(64), 0, stream, a);
+    else if (pieces <= 64) go(C1{}, C1{});
+    else if (pieces <= 256) go(C4{}, C1{});
+    else if (pieces <= 1024 && a.M <= 256) go(C16{}, C1{});
+    else if (pieces <= 512) go(C8{}, C1{});              // 704 rows of 4096 with a residual 8.3 us; four waves 8.7, two 11
+    else if (pieces <= 1024) go(C8{}, C2{});
+    else if (!NORM && pieces <= 1536 && a.M > 256) go(C8{}, std::integral_constant<int, NORM ? 2 : 3>{});
+    else if (pieces <= 2048) go(C16{}, C2{});
+    else if (!NORM && pieces <= 4096) go(C16{}, std::integral_constant<int, NORM ? 2 : 4>{});       // (the norm's rows would not fit the registers)
+    else hipLaunchKernelGGL((q8_long_rows_kernel<DT, RT, NORM>), dim3(a.M), dim3(1024), 0, stream, a);
 }
 
 int launch_q8(const Q8Args& a, int dtype, int res_dtype, hipStream_t stream) {
-    auto go = [&](auto dt, auto rt) {
-        hipLaunchKernelGGL((q8_rows_kernel<decltype(dt)::value, decltype(rt)::value>), dim3(a.M), dim3(256), 0, stream, a);
-    };
     auto with = [&](auto dt) {
-        using F32 = std::integral_constant<int, DT_F32>;
-        if (res_dtype == kNoResidual) go(dt, std::integral_constant<int, kNoResidual>{});
-        else if (res_dtype == DT_F32) go(dt, F32{});
-        else go(dt, dt);                             // (of x's type)
+        constexpr int DT = decltype(dt)::value;
+        if (!a.gain) launch_rows<DT, kNoResidual, false>(a, stream);
+        else if (res_dtype == kNoResidual) launch_rows<DT, kNoResidual, true>(a, stream);
+        else if (res_dtype == DT_F32) launch_rows<DT, DT_F32, true>(a, stream);
+        else launch_rows<DT, DT, true>(a, stream);   // (of x's type)
     };
     if (dtype == DT_F32) with(std::integral_constant<int, DT_F32>{});
     else if (dtype == DT_BF16) with(std::integral_constant<int, DT_BF16>{});
@@ -191,10 +414,10 @@ extern "C" int laser_q8_read(const int8_t* codes, int64_t codes_stride, const fl
     LASER_REQUIRE((uintptr_t)out % e == 0 && (uintptr_t)scales % 4 == 0, LASER_E_INVALID_ARG, "out or scales is not aligned to its elements");
     LASER_REQUIRE(rows_apart(out, N * e, out_stride * e, codes, N, codes_stride, M) && rows_apart(out, N * e, out_stride * e, scales, 4, 4, M), LASER_E_INVALID_ARG,
                   "out overlaps codes or scales");
-    hipStream_t s = (hipStream_t)stream;
-    if (dtype == LASER_F32) hipLaunchKernelGGL(q8_read_kernel<DT_F32>, dim3(M), dim3(256), 0, s, codes, codes_stride, scales, N, out, out_stride);
-    else if (dtype == LASER_BF16) hipLaunchKernelGGL(q8_read_kernel<DT_BF16>, dim3(M), dim3(256), 0, s, codes, codes_stride, scales, N, out, out_stride);
-    else hipLaunchKernelGGL(q8_read_kernel<DT_F16>, dim3(M), dim3(256), 0, s, codes, codes_stride, scales, N, out, out_stride);
+    const long pieces = (N + 7l) / 8;
+    const dim3 block(pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256), grid(M, (unsigned)std::min((pieces + block.x - 1) / block.x, 1024l));
+    const auto kernel = dtype == LASER_F32 ? q8_read_kernel<DT_F32> : dtype == LASER_BF16 ? q8_read_kernel<DT_BF16> : q8_read_kernel<DT_F16>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)stream, codes, codes_stride, scales, N, out, out_stride);
     LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
 }
