@@ -18,7 +18,7 @@
  *   - Token ids are int32 >= 0; -1 pads. bf16 / fp16 = bfloat16 / IEEE half bit patterns in uint16.
  *   - Numerics: weights bf16 as given; activations that feed matrix products and the KV cache are
  *     fp16; accumulation, softmax, norms and the residual stream are fp32. Weights and caches may be held in four bits instead
- *     (laser_w4_create, laser_kv_create_4bit).
+ *     (laser_w4_create, laser_kv_create_4bit), weights and the rows before them in 8-bit integers (laser_w8_create).
  *   - A handle must not be used from two streams or two host threads at the same time (the model
  *     handle owns activation workspace, the KV handle owns host-side page bookkeeping).
  */
@@ -359,6 +359,11 @@ int laser_w8_quantize(const uint16_t* w, int N, int Kd, int8_t* codes, float* sc
  * elements apart, aligned to its elements; it must not overlap x. x [dev] int8 rows of Kd codes (laser_q8_rows, laser_q8_norm), x_stride < 2^22 bytes apart.
  * Keeps no workspace: calls on several streams may share a handle. LASER_E_LIMIT where M / 16 times N / 16 passes 2^25. */
 int laser_w8_matmul(const laser_w8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, void* stream);
+
+/* laser_model_set_w8: laser_model_set_w4 with 8-bit weights (LASER_W_GU takes a gated matrix); a matrix is one or the other, the last one set. Rows enter these
+ * products in 8 bits: normed rows as laser_q8_norm makes them from the fp32 residual stream, the attention's result and the FFN activations, fp16 values, as
+ * laser_q8_rows does. The first call allocates max_rows * (max(d_model, ffn) + 4) bytes for them. */
+int laser_model_set_w8(laser_model* model, int layer, int which, const laser_w8* w);
 
 /* laser_verify_step (Eq. 3 / Eq. 6 forward, Eq. 4 / 7 / 8 acceptance, correction rule of Sec. 2.1).
  * For sequence b, rows r = 0..K hold the tokens [pending[b], drafts[b][0..K-1]] at positions

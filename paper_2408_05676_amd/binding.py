@@ -87,6 +87,7 @@ def lib():
         "laser_q8_rows": [vp, i64, i32, i32, i32, vp, i64, vp, vp],
         "laser_q8_norm": [vp, i64, i32, vp, i64, vp, i64, i32, vp, f32, i32, i32, vp, i64, vp, vp],
         "laser_q8_read": [vp, i64, vp, i32, i32, i32, vp, i64, vp],
+        "laser_model_set_w8": [vp, i32, i32, vp],
         "laser_w8_create": [vp, vp, i32, i32, i32, vp, C.POINTER(vp)],
         "laser_w8_destroy": [vp],
         "laser_w8_quantize": [vp, i32, i32, vp, vp, vp],
@@ -274,18 +275,25 @@ class Model:
     def set_w4(self, layer: int, name: str, w4) -> None:
         """laser_model_set_w4: name is wqkv, wo, wgu or wdown, w4 a W4 or None. A W4 is kept alive until this object is closed, also after
         another has taken its place: a captured graph may still read it."""
+        self._set(layer, name, w4, W4, lib().laser_model_set_w4)
+
+    def set_w8(self, layer: int, name: str, w8) -> None:
+        """laser_model_set_w8: the same with a W8 (wgu: a gated one)."""
+        self._set(layer, name, w8, W8, lib().laser_model_set_w8)
+
+    def _set(self, layer: int, name: str, w, kind, call) -> None:
         names = ("wqkv", "wo", "wgu", "wdown")
         if name not in names:
             raise LaserError(f"no matrix {name!r}: {', '.join(names)}")
-        if w4 is not None:
-            if not isinstance(w4, W4) or not w4._h:
-                raise LaserError("w4 must be a W4 that has not been closed, or None")
-            if w4.device != self.device:
-                raise LaserError(f"the matrix is on device {w4.device}, the model on {self.device}")
-        _check(lib().laser_model_set_w4(self._h, layer, names.index(name), w4._h if w4 is not None else None), "laser_model_set_w4")
-        if w4 is not None:
-            self._w4.add(w4)
-            w4._models.add(self)
+        if w is not None:
+            if not isinstance(w, kind) or not w._h:
+                raise LaserError(f"the matrix must be a {kind.__name__} that has not been closed, or None")
+            if w.device != self.device:
+                raise LaserError(f"the matrix is on device {w.device}, the model on {self.device}")
+        _check(call(self._h, layer, names.index(name), w._h if w is not None else None), call.__name__)
+        if w is not None:
+            self._w4.add(w)
+            w._models.add(self)
 
     def aborted(self, stream=None) -> bool:
         v = C.c_int()

@@ -5,7 +5,7 @@
 #include <string>
 #include <vector>
 
-#include "four_bit.h"
+#include "eight_bit.h"
 #include "gemm_tile_plan.h"
 #include "gemm_skinny.h"
 #include "gemm_mid.h"
@@ -780,6 +780,30 @@ static void copies_for_few_rows(Model* m, hipStream_t stream) {
 
 static const W4* w4_of(const Model* m, int layer, int which) { return m->w4.empty() ? nullptr : (const W4*)m->w4[4 * layer + which]; }
 
+static const W8* w8_of(const Model* m, int layer, int which) { return m->w8.empty() ? nullptr : (const W8*)m->w8[4 * layer + which]; }
+
+// The row before a product with 8-bit weights: the residual stream, with n_part parts of the product before it added to it (part: [n_part][M][d]), normed.
+static int q8_residual(Model* m, int M, const float* gain, const float* part, int n_part, hipStream_t stream) {
+    const int dm = m->d.d_model;
+    Q8Args a{};
+    a.x = n_part ? part : m->x; a.x_stride = dm;
+    a.n_part = std::max(1, n_part); a.part_stride = (int64_t)M * dm;
+    if (n_part) { a.res = a.res_out = m->x; a.res_stride = a.res_out_stride = dm; }
+    a.gain = gain; a.eps = m->d.eps;
+    a.codes = m->q8; a.codes_stride = dm; a.scales = m->q8_scales;
+    a.M = M; a.N = dm;
+    return launch_q8(a, DT_F32, n_part ? DT_F32 : -1, stream);
+}
+// rows [M][N] fp16 -> codes -> their product, as fp32 [M][outs]
+static int q8_product(Model* m, const W8* w, const uint16_t* rows, int M, float* out, hipStream_t stream) {
+    Q8Args a{};
+    a.x = rows; a.x_stride = w->Kd; a.n_part = 1;
+    a.codes = m->q8; a.codes_stride = w->Kd; a.scales = m->q8_scales;
+    a.M = M; a.N = w->Kd;
+    if (const int rc = launch_q8(a, DT_F16, -1, stream)) return rc;
+    return launch_w8(w, m->q8, w->Kd, m->q8_scales, M, DT_F32, out, w->outs, stream);
+}
+
 // A layer's rotary positions, cache write and attention on a 4-bit cache. The qkv rows (the sums of n_part arrays, see RopeArgs) go in as
 // fp32; rotated queries replace the first array's and are read back by the attention, whose result is split into two planes.
 static int four_bit_attention(Model* m, KV* kv, const int32_t* ids_dev, const RopeArgs& ra, int layer, int B, int R, int max_tokens, hipStream_t stream) {
@@ -823,8 +847,8 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
                        m->row_pos, m->row_slot, m->row_anc);
     hipLaunchKernelGGL(embed_rmsnorm_kernel, dim3(M), dim3(256), 0, stream, d.emb, d.g1, pending, drafts, draft_len,
                        R, dm, d.vocab, d.eps, m->x, m->xn, m->xn_lo);
-    const bool all_w4 = m->w4_set == 4 * d.n_layers;                // then no projection is read as bf16, and none is copied
-    if (M > kSkinnyMaxRows && m->f16_copies && !m->w16[0] && !all_w4) {
+    const bool none_bf16 = m->w4_set + m->w8_set == 4 * d.n_layers; // then no projection is read as bf16, and none is copied
+    if (M > kSkinnyMaxRows && m->f16_copies && !m->w16[0] && !none_bf16) {
         if (const int rc = widen_copies(m, kProjections, stream)) return rc;
     }
     if (M > 16 && !m->kpart) {
@@ -832,7 +856,8 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
         m->kpart_floats = (size_t)dm * std::max((size_t)d.max_rows * 8, (size_t)std::min(d.max_rows, kSkinnyMaxRows) * 12);
         LASER_HIP_CHECK(hipMalloc((void**)&m->kpart, m->kpart_floats * 4));
     }
-    int pend = 0;              // partial results of the last down projection still to be added to the residual
+    int pend = 0;              // partial results of the last down projection still to be added to the residual,
+    const float* pend_at = m->kpart;       // and where they are
     const int nqt = (R + 15) / 16;
     const int npages_ub = (max_len_ub + R + kPageSize - 1) / kPageSize;
     // With a (sequence, head, query tile) triple for every second compute unit the context is not split: no
@@ -854,13 +879,18 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
     }
     for (int l = 0; l < d.n_layers; ++l) {
         int rc;
-        if (l > 0)
-            launch_rmsnorm(M, stream, m->x, d.g1 + (size_t)l * dm, dm, d.eps, m->xn, m->xn_lo, (const float*)m->kpart, pend, (size_t)M * dm);
+        const W8 *w8_qkv = w8_of(m, l, 0), *w8_o = w8_of(m, l, 1), *w8_gu = w8_of(m, l, 2), *w8_down = w8_of(m, l, 3);
+        if (w8_qkv) {
+            if ((rc = q8_residual(m, M, d.g1 + (size_t)l * dm, pend_at, pend, stream))) return rc;
+        } else if (l > 0)
+            launch_rmsnorm(M, stream, m->x, d.g1 + (size_t)l * dm, dm, d.eps, m->xn, m->xn_lo, pend_at, pend, (size_t)M * dm);
         pend = 0;
         const bool many = M > 16 && m->w16[0];      // tiled path: weights from the fp16 copy (if kept)
         GemmArgs g{d.wqkv + (size_t)l * 3 * dm * dm, many ? m->w16[0] + (size_t)l * 3 * dm * dm : nullptr, m->xn, m->xn_lo, M, 3 * dm, dm, 1, m->qkv, nullptr};
         g.part = m->kpart; g.part_floats = m->kpart_floats; g.want_split = m->ksplit_opt[0]; g.mid_waves = m->mid_waves; g.want_tile = m->tile;
-        if (const W4* w = w4_of(m, l, 0)) {
+        if (w8_qkv) {
+            if ((rc = launch_w8(w8_qkv, m->q8, dm, m->q8_scales, M, DT_F32, m->qkv, 3 * dm, stream))) return rc;
+        } else if (const W4* w = w4_of(m, l, 0)) {
             g.n_part = 0;
             if ((rc = launch_w4(w, m->xn, dm, M, LASER_F16, W4_F32, m->qkv, 3 * dm, stream))) return rc;
         } else if ((rc = launch_gemm<EPI_F32>(g, stream))) return rc;
@@ -900,11 +930,18 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
         }
         GemmArgs go{d.wo + (size_t)l * dm * dm, many ? m->w16[1] + (size_t)l * dm * dm : nullptr, m->attn, m->attn_lo, M, dm, dm, 1, m->x, nullptr};
         go.part = m->kpart; go.part_floats = m->kpart_floats; go.want_split = m->ksplit_opt[1]; go.mid_waves = m->mid_waves; go.want_tile = m->tile;
-        if (const W4* w = w4_of(m, l, 1)) {
+        const float* o_part = m->kpart;
+        if (w8_o) {                                  // its result takes the place of the attention's inputs, and the norm adds it to the residual
+            if ((rc = q8_product(m, w8_o, m->attn, M, m->qkv, stream))) return rc;
+            go.n_part = 1;
+            o_part = m->qkv;
+        } else if (const W4* w = w4_of(m, l, 1)) {
             go.n_part = 0;
             if ((rc = launch_w4(w, m->attn, dm, M, LASER_F16, W4_ADD_F32, m->x, dm, stream))) return rc;
         } else if ((rc = launch_gemm<EPI_RESID>(go, stream))) return rc;
-        launch_rmsnorm(M, stream, m->x, d.g2 + (size_t)l * dm, dm, d.eps, m->xn, m->xn_lo, (const float*)m->kpart, go.n_part, (size_t)M * dm);
+        if (w8_gu) {
+            if ((rc = q8_residual(m, M, d.g2 + (size_t)l * dm, o_part, go.n_part, stream))) return rc;
+        } else launch_rmsnorm(M, stream, m->x, d.g2 + (size_t)l * dm, dm, d.eps, m->xn, m->xn_lo, o_part, go.n_part, (size_t)M * dm);
         // On the tiled many-row path a split operand doubles the matrix work; gate/up (45 % of the layer's
         // flops) takes the single fp16 rows there unless option "split_ffn" asks for the split (see set_option).
         const bool split_gu = M <= kSkinnyMaxRows || m->split_ffn;
@@ -912,19 +949,25 @@ static int forward(Model* m, KV* kv, const int32_t* ids_dev, const int32_t* pend
         gg.mid_waves = m->mid_waves; gg.want_tile = m->tile;
         const bool prof = m->prof_on && m->prof_n < m->prof_cap;
         if (prof) LASER_HIP_CHECK(hipEventRecord(m->prof_ev[2 * m->prof_n], stream));
-        if (const W4* w = w4_of(m, l, 2)) {
+        if (w8_gu) {
+            if ((rc = launch_w8(w8_gu, m->q8, dm, m->q8_scales, M, DT_F16, m->act, F, stream))) return rc;
+        } else if (const W4* w = w4_of(m, l, 2)) {
             if ((rc = launch_w4(w, m->xn, dm, M, LASER_F16, W4_SWIGLU, m->act, F, stream))) return rc;
         } else if ((rc = launch_gemm<EPI_SWIGLU>(gg, stream))) return rc;
         if (prof) { LASER_HIP_CHECK(hipEventRecord(m->prof_ev[2 * m->prof_n + 1], stream)); ++m->prof_n; }
         GemmArgs gd{d.wdown + (size_t)l * dm * F, many ? m->w16[3] + (size_t)l * dm * F : nullptr, m->act, nullptr, M, dm, F, 1, m->x, nullptr};
         gd.part = m->kpart; gd.part_floats = m->kpart_floats; gd.want_split = m->ksplit_opt[2]; gd.mid_waves = m->mid_waves; gd.want_tile = m->tile;
-        if (const W4* w = w4_of(m, l, 3)) {
+        if (w8_down) {
+            if ((rc = q8_product(m, w8_down, m->act, M, m->qkv, stream))) return rc;
+            gd.n_part = 1;
+        } else if (const W4* w = w4_of(m, l, 3)) {
             gd.n_part = 0;
             if ((rc = launch_w4(w, m->act, F, M, LASER_F16, W4_ADD_F32, m->x, dm, stream))) return rc;
         } else if ((rc = launch_gemm<EPI_RESID>(gd, stream))) return rc;
         pend = gd.n_part;        // added to the residual by the next norm (next layer's, or the final one)
+        pend_at = w8_down ? m->qkv : m->kpart;
     }
-    launch_rmsnorm(M, stream, m->x, d.gf, dm, d.eps, m->xn, nullptr, (const float*)m->kpart, pend, (size_t)M * dm);
+    launch_rmsnorm(M, stream, m->x, d.gf, dm, d.eps, m->xn, nullptr, pend_at, pend, (size_t)M * dm);
     LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
 }
@@ -936,7 +979,7 @@ using namespace laser;
 extern "C" int laser_model_destroy(laser_model* h) {
     if (!h) return LASER_OK;
     Model* m = reinterpret_cast<Model*>(h);
-    void* ptrs[] = {m->kpart, m->w16_mem[0], m->w16_mem[1], m->w16_mem[2], m->w16_mem[3], m->w16_mem[4], m->x, m->xn, m->q_lo, m->qkv, m->q, m->attn, m->act, m->row_pos, m->att_part, m->rope, m->hp_max,
+    void* ptrs[] = {m->kpart, m->q8, m->w16_mem[0], m->w16_mem[1], m->w16_mem[2], m->w16_mem[3], m->w16_mem[4], m->x, m->xn, m->q_lo, m->qkv, m->q, m->attn, m->act, m->row_pos, m->att_part, m->rope, m->hp_max,
                     m->hp_sum, m->hp_arg, m->hp_topv, m->hp_topi, m->cand_beg, m->cand_cnt, m->cand_x, m->node_cand, m->cand_lx, m->row_slot, m->row_anc,
                     m->row_mx, m->row_sum, m->row_arg, m->cand_rank};
     for (void* p : ptrs) if (p) (void)hipFree(p);
@@ -1059,8 +1102,8 @@ static int verify_impl(laser_model* mh, laser_kv* kh, const int32_t* seq_ids, co
     }
     const int32_t* ids_dev = nullptr;
     if ((rc = kv->stage_ids(seq_ids, B, stream, &ids_dev))) return rc;
-    const bool fused = m->use_fused && !kv->pages4 && m->w4_set == 0 && fused_supported(m, B, K, max_ub);
-    if (fused || (B * R > 16 && B * R <= kSkinnyMaxRows && m->w4_set < 4 * m->d.n_layers)) copies_for_few_rows(m, stream);
+    const bool fused = m->use_fused && !kv->pages4 && m->w4_set + m->w8_set == 0 && fused_supported(m, B, K, max_ub);
+    if (fused || (B * R > 16 && B * R <= kSkinnyMaxRows && m->w4_set + m->w8_set < 4 * m->d.n_layers)) copies_for_few_rows(m, stream);
     if (fused) {
         if (parent)          // token tree: positions (depth) and ancestor masks of the rows
             hipLaunchKernelGGL(rows_kernel, dim3((B * R + 255) / 256), dim3(256), 0, stream, parent, draft_len, ids_dev, kv->len, B, R,
@@ -1188,19 +1231,44 @@ extern "C" int laser_model_set_option(laser_model* mh, const char* name, int val
     return LASER_E_INVALID_ARG;
 }
 
-extern "C" int laser_model_set_w4(laser_model* mh, int layer, int which, const laser_w4* wh) {
-    Model* m = reinterpret_cast<Model*>(mh);
-    const W4* w = reinterpret_cast<const W4*>(wh);
+static int check_set(Model* m, int layer, int which, const void* w, int wN, int wKd) {
     LASER_REQUIRE(m != nullptr, LASER_E_INVALID_ARG, "model is NULL");
     LASER_REQUIRE(layer >= 0 && layer < m->d.n_layers, LASER_E_INVALID_ARG, "layer %d out of range", layer);
     LASER_REQUIRE(which >= 0 && which <= 3, LASER_E_INVALID_ARG, "matrix %d: LASER_W_QKV, LASER_W_O, LASER_W_GU or LASER_W_DOWN", which);
     const int dm = m->d.d_model, F = m->d.ffn;
     const int N = which == 0 ? 3 * dm : which == 2 ? 2 * F : dm, Kd = which == 3 ? F : dm;
-    LASER_REQUIRE(!w || (w->N == N && w->Kd == Kd), LASER_E_SHAPE, "the matrix is [%d][%d], not [%d][%d]", w ? w->N : 0, w ? w->Kd : 0, N, Kd);
-    if (m->w4.empty()) m->w4.assign((size_t)4 * m->d.n_layers, nullptr);
-    const void*& at = m->w4[4 * (size_t)layer + which];
-    m->w4_set += (w != nullptr) - (at != nullptr);
+    LASER_REQUIRE(!w || (wN == N && wKd == Kd), LASER_E_SHAPE, "the matrix is [%d][%d], not [%d][%d]", wN, wKd, N, Kd);
+    return LASER_OK;
+}
+// w in its place of one kind's list, and how many that has
+static void put(std::vector<const void*>& list, int& count, int n_layers, int layer, int which, const void* w) {
+    if (list.empty()) { if (!w) return; list.assign((size_t)4 * n_layers, nullptr); }
+    const void*& at = list[4 * (size_t)layer + which];
+    count += (w != nullptr) - (at != nullptr);
     at = w;
+}
+
+extern "C" int laser_model_set_w4(laser_model* mh, int layer, int which, const laser_w4* wh) {
+    Model* m = reinterpret_cast<Model*>(mh);
+    const W4* w = reinterpret_cast<const W4*>(wh);
+    if (const int rc = check_set(m, layer, which, w, w ? w->N : 0, w ? w->Kd : 0)) return rc;
+    put(m->w4, m->w4_set, m->d.n_layers, layer, which, w);
+    if (w) put(m->w8, m->w8_set, m->d.n_layers, layer, which, nullptr);
+    return LASER_OK;
+}
+
+extern "C" int laser_model_set_w8(laser_model* mh, int layer, int which, const laser_w8* wh) {
+    Model* m = reinterpret_cast<Model*>(mh);
+    const W8* w = reinterpret_cast<const W8*>(wh);
+    if (const int rc = check_set(m, layer, which, w, w ? w->N : 0, w ? w->Kd : 0)) return rc;
+    LASER_REQUIRE(!w || w->gated == (which == LASER_W_GU), LASER_E_SHAPE, "LASER_W_GU takes a gated matrix, the others a plain one");
+    if (w && !m->q8) {
+        const size_t R = (size_t)m->d.max_rows, bytes = R * std::max(m->d.d_model, m->d.ffn);    // (a multiple of 128)
+        LASER_HIP_CHECK(hipMalloc((void**)&m->q8, bytes + R * 4));
+        m->q8_scales = reinterpret_cast<float*>(m->q8 + bytes);
+    }
+    put(m->w8, m->w8_set, m->d.n_layers, layer, which, w);
+    if (w) put(m->w4, m->w4_set, m->d.n_layers, layer, which, nullptr);
     return LASER_OK;
 }
 

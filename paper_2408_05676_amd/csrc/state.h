@@ -109,6 +109,10 @@ struct Model {
     int f16_copies = 1;                // 0: the tiled kernels stream the bf16 weights and widen them in the loop (no copies)
     std::vector<const void*> w4;       // laser_model_set_w4: 4-bit matrices instead of wqkv, wo, wgu, wdown, four a layer; NULL: none. Empty: never set
     int w4_set = 0;                    // how many of them are not NULL
+    std::vector<const void*> w8;       // laser_model_set_w8: the same with 8-bit matrices; a matrix has at most one of the two
+    int w8_set = 0;
+    int8_t* q8 = nullptr;              // [max_rows][d or F] codes of the rows before a product with one, from the first such matrix on
+    float* q8_scales = nullptr;        // [max_rows], behind them in one allocation
     float* kpart = nullptr;            // partial results of reduction-split tiled GEMMs (many-row path), [parts][rows][N]
     size_t kpart_floats = 0;
     int ksplit_opt[3] = {0, 0, 0};     // forced reduction parts for QKV, O, down (0 = choose from the tile count)

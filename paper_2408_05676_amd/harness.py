@@ -32,13 +32,15 @@ class Engine:
     state (pending token, context tail) lives on the device."""
 
     def __init__(self, shape, weights: dict, batch: int, K: int, max_len: int, n_max: int = 3,
-                 prefill_chunk: int = 16, own_text_cap: int = 0, four_bit_cache: bool = False, w4_group: int = 0):
+                 prefill_chunk: int = 16, own_text_cap: int = 0, four_bit_cache: bool = False, w4_group: int = 0, w8: bool = False):
         """own_text_cap > 0: keep each sequence's own text (prompt + emitted tokens, the most recent own_text_cap of
         them) on the device and search it as a temporary branch at every retrieval (Sec. 3.2).
         four_bit_cache: keys and values in four bits. w4_group 32, 64 or 128: the projections in four bits, quantised here from the bf16 weights
         in groups of that many inputs, in memory of their own: `weights` stays as it is, and the embedding and the head are read from it.
         Either takes the steps off the persistent kernel, ms a step at the 7B shape as it is / four_bit_cache / w4_group=128 / both: one sequence of 9 rows
         behind 1024 tokens 3.5 / 4.8 / 2.6 / 2.3, one row behind 8000 4.8 / 4.3 / 3.3 / 2.3, 64 sequences of 11 rows behind 512 17.1 / 14.5 / 21.7 / 19.4."""
+        if w4_group and w8:
+            raise L.LaserError("w4_group or w8, not both")
         self.shape, self.B, self.K, self.n_max = shape, batch, K, n_max
         R = max(K + 1, prefill_chunk)
         pages_per_seq = (max_len + 15) // 16 + 1
@@ -49,6 +51,10 @@ class Engine:
             for l in range(shape.n_layers):
                 for name in ("wqkv", "wo", "wgu", "wdown"):
                     self.model.set_w4(l, name, L.W4(*L.w4_quantize(weights[name][l], w4_group)))
+        if w8:
+            for l in range(shape.n_layers):
+                for name in ("wqkv", "wo", "wgu", "wdown"):
+                    self.model.set_w8(l, name, L.W8(*L.w8_quantize(weights[name][l]), gated=name == "wgu"))
         cache = L.KVCache4 if four_bit_cache else L.KVCache
         self.kv = cache(shape.n_layers, shape.n_heads, shape.head_dim, n_pages=batch * pages_per_seq,
                         max_seqs=batch, max_pages_per_seq=pages_per_seq)
