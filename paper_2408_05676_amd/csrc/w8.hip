@@ -30,8 +30,9 @@ __global__ __launch_bounds__(256) void w8_layout_kernel(const int8_t* codes, con
 // Up to 16 rows: one output fragment and eight waves where that is at most a workgroup for each of 256 compute units, else two and four (6144 outputs of 2048
 // inputs, one row 5.0 us, the other way 5.9; 4096 x 4096 6.1 and 6.2; 4096 x 11008 10.3 and 12.5).
 // More rows: the least of the microseconds below, which grow with the workgroups of a compute unit and their stages. Fitted by least squares to what every kernel within
-// 1.4 of the fastest took, at 17 to 1000 rows of ten matrices (256 x 768 to 4096 x 2 x 11008) and of 400 random ones: 3700 measurements. What it takes is 0.5 % slower
-// than the fastest on average at the ten, 1 % at the random ones, 26 % at worst (814 rows 768 -> 9443: 18.9 us of 15.1).
+// 1.25 of the fastest took, at 17 to 1000 rows of ten matrices (256 x 768 to 4096 x 2 x 11008) and of 400 random ones: 2600 measurements. What it takes is 0.5 % slower
+// than the fastest on average at the ten, 0.8 % at the random ones, 21 % at worst (520 rows 3712 -> 238: 6.7 us of 5.5). Epilogues of tiles that leave a compute unit to one
+// workgroup, by their registers, stand behind nothing else's products.
 static int w8_pick(const W8Args& a, bool gated) {
     constexpr int cus = 256;
     const int frags = a.rows / 16;
@@ -44,13 +45,14 @@ static int w8_pick(const W8Args& a, bool gated) {
         const W8Few f = kW8Few[v];
         if (f.mt == 0 || (gated && f.nt % 2)) continue;
         const double each = (double)up(up(frags, f.nt) * up(a.M, 16 * f.mt), cus);
-        const double us = 3.02 + each * (k * (0.141 * f.nt + 0.161 * f.mt) + 0.122 + 0.0945 * f.nt * f.mt) + 0.102 * weights + 0.509 * results;
+        const double us = 3.07 + each * (k * (0.141 * f.nt + 0.169 * f.mt) + 0.052 + 0.0914 * f.nt * f.mt) + 0.0979 * weights + 0.568 * results;
         if (us < least) { least = us; best = v; }
     }
     for (int v = 0; v < kW8ShapeN; ++v) {
         const W8Shape s = kW8Shapes[v];
         const double each = (double)up(up(a.M, s.wm * 16) * up(a.rows, s.wn * 64), cus);
-        const double us = 3.35 + each * (k * (0.0817 * s.wm * s.wn + 0.0654 * s.wm + 0.406 * s.wn) + 0.1 * s.wm * s.wn) + 0.428 * k + 0.0903 * weights + 0.228 * results;
+        const double end = s.wm * s.wn >= 32 ? (gated ? 0.103 : 0.0838) : gated ? 0.0616 : 0.0547;
+        const double us = 3.3 + each * (k * (0.071 * s.wm * s.wn + 0.109 * s.wm + 0.352 * s.wn) + end * s.wm * s.wn) + 0.466 * k + 0.0877 * weights + 0.328 * results;
         if (us < least) { least = us; best = kW8FewN + v; }
     }
     return best;

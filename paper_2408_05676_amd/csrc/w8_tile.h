@@ -38,11 +38,16 @@ __device__ inline void load_to_lds(uint64_t base, uint32_t vo, uint32_t at) {
 }
 __device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
+// Accumulators are pinned to the accumulation registers by assembly (V: to vector registers, where those are full): left to itself the compiler moves them between the two.
+template <bool V>
 __device__ inline void mfma_i8_acc(const u32x4& w, const u32x4& x, int4_t& c) {
-    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
+    if constexpr (V) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+v"(c) : "v"(w), "v"(x));
+    else asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x));
 }
-__device__ inline void mfma_i8_acc_v(const u32x4& w, const u32x4& x, int4_t& c) {
-    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+v"(c) : "v"(w), "v"(x));
+template <bool V>
+__device__ inline void mfma_i8_first(const u32x4& w, const u32x4& x, int4_t& c) {
+    if constexpr (V) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=&v"(c) : "v"(w), "v"(x));
+    else asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=&a"(c) : "v"(w), "v"(x));
 }
 
 constexpr int kW8Waves = 4;
@@ -100,11 +105,14 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
     const uint64_t wstep = (uint64_t)a.rows * 64;
     int wreq = 0;
     u32x4 fw[WD][WN];
-    auto load_w = [&](auto sc, auto jc) { fw[decltype(sc)::value][decltype(jc)::value] = *reinterpret_cast<const u32x4*>(wbase + wo[decltype(jc)::value]); };
+    auto load_w = [&](auto sc, auto jc) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wbase), (short)0, -1, 0x00020000);
+        fw[decltype(sc)::value][decltype(jc)::value] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, wo[decltype(jc)::value], 0, 0);
+    };
     auto next_w = [&] { ++wreq; wbase += wreq < 2 * nk ? wstep : 0; };
 
     // The workgroups of a column of tiles walk the same weights together. Each touches its share of the lines PD stages ahead.
-    constexpr int PD = 5;
+    constexpr int PD = 3;
     const int line = min(tm + a.tiles_m * (wave * 64 + lane), WN * 16 * NW - 1);       // of a stage: 64-byte rows in pairs, step by step
     const int tile0 = tn * NW * WN * 16, step_lines = min(NW * WN * 16, a.rows - tile0) / 2;
     const uint32_t touch = (uint32_t)(line / (WN * 8 * NW)) * (uint32_t)wstep + (uint32_t)min(line % (WN * 8 * NW), step_lines - 1) * 128;
@@ -120,11 +128,7 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
         tbase += treq < nk ? 2 * wstep : 0;
     };
 
-    int4_t acc[WN][WM];
-#pragma unroll
-    for (int j = 0; j < WN; ++j)
-#pragma unroll
-        for (int i = 0; i < WM; ++i) acc[j][i] = int4_t{0, 0, 0, 0};
+    int4_t acc[WN][WM];                                             // (the first step writes it: zeros would be up to 264 writes before it)
     u32x4 fx[2][WM];
     uint32_t ox[2];
 #pragma unroll
@@ -135,15 +139,15 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
     };
     // Multiplies step s of a stage (weights in ring slot q), reads the rows' fragments of the other step from rslot meanwhile, requests the weights
     // WD steps on, and the loads L0 .. L1 - 1 of a later stage's rows.
-    auto multiply = [&](auto sc, auto qc, int rslot, auto l0c, auto l1c) {
+    auto multiply = [&](auto firstc, auto sc, auto qc, int rslot, auto l0c, auto l1c) __attribute__((always_inline)) {
         constexpr int s = decltype(sc)::value, q = decltype(qc)::value, L0 = decltype(l0c)::value, L1 = decltype(l1c)::value, NMUL = WM * WN;
         static_for<0, NMUL>([&](auto mc) {
             constexpr int m = decltype(mc)::value, j = m / WM, i = m % WM;
             static_for<m * WM / NMUL, (m + 1) * WM / NMUL>([&](auto ic) { read_x(std::integral_constant<int, 1 - s>{}, ic, rslot); });
             constexpr int l0 = L0 + (2 * m * (L1 - L0) + NMUL) / (2 * NMUL), l1 = L0 + (2 * (m + 1) * (L1 - L0) + NMUL) / (2 * NMUL);
             static_for<l0, l1>([&](auto jc) { issue(jc); });
-            if constexpr (m >= 64) mfma_i8_acc_v(fw[q][j], fx[s][i], acc[j][i]);
-            else mfma_i8_acc(fw[q][j], fx[s][i], acc[j][i]);
+            if constexpr (decltype(firstc)::value) mfma_i8_first<(m >= 64)>(fw[q][j], fx[s][i], acc[j][i]);
+            else mfma_i8_acc<(m >= 64)>(fw[q][j], fx[s][i], acc[j][i]);
             if constexpr (i == WM - 1) load_w(qc, std::integral_constant<int, j>{});
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -170,17 +174,20 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
     asm volatile("" ::: "memory");
     static_for<0, WM>([&](auto ic) { read_x(C0{}, ic, 0); });
     int slot = 0;
-    for (int kt0 = 0; kt0 < nk; kt0 += WD / 2)
+    auto two_stages = [&](auto firstc) __attribute__((always_inline)) {                            // (nk is even: there is no way out between them, past which the accumulators would be copied)
         static_for<0, WD / 2>([&](auto uc) {
             constexpr int u = decltype(uc)::value;
             const int nslot = slot + 1 < NS ? slot + 1 : 0;
             touch_ahead();
-            multiply(C0{}, std::integral_constant<int, 2 * u>{}, slot, LH{}, LA{});
+            multiply(std::bool_constant<decltype(firstc)::value && u == 0>{}, C0{}, std::integral_constant<int, 2 * u>{}, slot, LH{}, LA{});
             next_stage();
             sync();
-            multiply(C1{}, std::integral_constant<int, 2 * u + 1>{}, nslot, C0{}, LH{});
+            multiply(std::false_type{}, C1{}, std::integral_constant<int, 2 * u + 1>{}, nslot, C0{}, LH{});
             slot = nslot;
         });
+    };
+    two_stages(std::true_type{});
+    for (int kt0 = WD / 2; kt0 < nk; kt0 += WD / 2) two_stages(std::false_type{});
     // The surplus requests must not land in a later workgroup's LDS; the last matrix instructions must have written.
     asm volatile("s_waitcnt vmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
     static_for<0, WM * WN>([&](auto mc) {
