@@ -592,39 +592,41 @@ def w4_matmul(w: W4, x: torch.Tensor, out=None, stream=None) -> torch.Tensor:
 Q8_PAD = 128                                                                     # rows of codes lie multiples of this many bytes apart
 
 
-def _rows(t: torch.Tensor, name: str, M: int, N: int, dtype, dev: int) -> int:
-    """Checks a [M][N] tensor with contiguous rows on device dev; its row stride. (A call takes some microseconds on the device: few attributes are read.)"""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != (M, N):
-        raise LaserError(f"{name} must be a CUDA tensor [{M}][{N}] of {dtype}")
-    if t.get_device() != dev:
+# A small call takes less than the checks of its arguments would attribute by attribute: the helpers below read each of a tensor's once.
+def _matrix(t, name: str, types):
+    """(device, M, N, types[its dtype], row stride, address) of a [M][N] tensor with contiguous rows on the current device."""
+    try:
+        (M, N), (step, one), dt, dev = t.shape, t.stride(), types[t.dtype], t.get_device()
+    except (AttributeError, ValueError, KeyError, TypeError):
+        raise LaserError(f"{name} must be a CUDA tensor [M][N] of {', '.join(str(k)[6:] for k in types)}") from None
+    if dev < 0 or dev != _device():
         raise LaserError(f"{name} is on {t.device}, not on the current device")
-    step, one = t.stride()
     if one != 1 and N > 1 and M:
         raise LaserError(f"{name} must have contiguous rows")
-    return step if M > 1 else -(-N // Q8_PAD) * Q8_PAD
+    return dev, M, N, dt, step if M > 1 else -(-N // Q8_PAD) * Q8_PAD, t.data_ptr()
 
 
-def _line(t: torch.Tensor, name: str, M: int, dev: int) -> int:
-    """Checks a contiguous float32 [M] on device dev; its address."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (M,) or not t.is_contiguous():
-        raise LaserError(f"{name} must be a contiguous CUDA tensor [{M}] of float32")
-    if t.get_device() != dev:
-        raise LaserError(f"{name}: on {t.device}, not on the current device")
+def _like(t, name: str, M: int, N: int, types, dev: int):
+    """(types[its dtype], row stride, address) of a [M][N] tensor with contiguous rows on device dev."""
+    try:
+        dt, shape, (step, one), on = types[t.dtype], t.shape, t.stride(), t.get_device()
+    except (AttributeError, ValueError, KeyError, TypeError):
+        shape = None
+    if shape != (M, N) or on != dev:
+        raise LaserError(f"{name} must be a tensor [{M}][{N}] of {', '.join(str(k)[6:] for k in types)} on the current device")
+    if one != 1 and N > 1 and M:
+        raise LaserError(f"{name} must have contiguous rows")
+    return dt, step if M > 1 else -(-N // Q8_PAD) * Q8_PAD, t.data_ptr()
+
+
+def _line(t, name: str, M: int, dev: int) -> int:
+    """The address of a contiguous float32 [M] on device dev."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != (M,) or t.get_device() != dev or not t.is_contiguous():
+        raise LaserError(f"{name} must be a contiguous tensor [{M}] of float32 on the current device")
     return t.data_ptr()
 
 
-def _two_dims(t, name: str, what: str):
-    """(device in use, M, N) of a CUDA tensor with two dimensions."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
-        raise LaserError(f"{name} must be a CUDA tensor [M][N] of {what}")
-    return (_device(), *t.shape)
-
-
-def _float_code(t, name: str) -> int:
-    dt = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
-    if dt is None:
-        raise LaserError(f"{name} must be of float16, bfloat16 or float32")
-    return dt
+_CODES = {torch.int8: 0}
 
 
 def _q8_out(M: int, N: int, device, stream):
@@ -635,41 +637,39 @@ def _q8_out(M: int, N: int, device, stream):
 def q8_rows(x: torch.Tensor, out=None, stream=None):
     """laser_q8_rows: x [M][N] -> (codes int8 [M][N], scales float32 [M]). The codes' rows are Q8_PAD bytes' multiples apart, as w8_matmul wants them;
     out: two such tensors to write to (codes of any row stride, if they are for q8_read only)."""
-    dev, M, N = _two_dims(x, "x", "float16, bfloat16 or float32")
-    dt, step = _float_code(x, "x"), _rows(x, "x", M, N, x.dtype, dev)
+    dev, M, N, dt, step, xp = _matrix(x, "x", _DTYPES)
     codes, scales = _q8_out(M, N, x.device, stream) if out is None else out
-    _check(lib().laser_q8_rows(x.data_ptr(), step, M, N, dt, codes.data_ptr(), _rows(codes, "codes", M, N, torch.int8, dev), _line(scales, "scales", M, dev),
-                               _on(stream, dev)), "laser_q8_rows")
+    _, cs, cp = _like(codes, "codes", M, N, _CODES, dev)
+    _check(lib().laser_q8_rows(xp, step, M, N, dt, cp, cs, _line(scales, "scales", M, dev), _on(stream, dev)), "laser_q8_rows")
     return codes, scales
 
 
 def q8_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, residual=None, residual_out=None, out=None, stream=None):
     """laser_q8_norm: (codes, scales) of the root-mean-square norm of x + residual times gain (float32 [N]); the sum goes to residual_out (None: to
     residual itself). residual: float32 or x's type, or None."""
-    dev, M, N = _two_dims(x, "x", "float16, bfloat16 or float32")
-    dt, step = _float_code(x, "x"), _rows(x, "x", M, N, x.dtype, dev)
-    rp, rs, op, os_, rdt = None, 0, None, 0, dt
+    dev, M, N, dt, step, xp = _matrix(x, "x", _DTYPES)
+    rs, rp, os_, op, rdt = 0, None, 0, None, dt
     if residual is not None:
-        rdt = _float_code(residual, "residual")
-        if residual_out is None:
-            residual_out = residual
-        rs, os_ = _rows(residual, "residual", M, N, residual.dtype, dev), _rows(residual_out, "residual_out", M, N, residual.dtype, dev)
-        rp, op = residual.data_ptr(), residual_out.data_ptr()
+        rdt, rs, rp = _like(residual, "residual", M, N, _DTYPES, dev)
+        odt, os_, op = (rdt, rs, rp) if residual_out is None else _like(residual_out, "residual_out", M, N, _DTYPES, dev)
+        if odt != rdt:
+            raise LaserError("residual_out is not of residual's type")
     elif residual_out is not None:
         raise LaserError("residual_out without a residual")
     codes, scales = _q8_out(M, N, x.device, stream) if out is None else out
-    _check(lib().laser_q8_norm(x.data_ptr(), step, dt, rp, rs, op, os_, rdt, _line(gain, "gain", N, dev), eps, M, N, codes.data_ptr(),
-                               _rows(codes, "codes", M, N, torch.int8, dev), _line(scales, "scales", M, dev), _on(stream, dev)), "laser_q8_norm")
+    _, cs, cp = _like(codes, "codes", M, N, _CODES, dev)
+    _check(lib().laser_q8_norm(xp, step, dt, rp, rs, op, os_, rdt, _line(gain, "gain", N, dev), eps, M, N, cp, cs, _line(scales, "scales", M, dev),
+                               _on(stream, dev)), "laser_q8_norm")
     return codes, scales
 
 
 def q8_read(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.float16, out=None, stream=None) -> torch.Tensor:
     """laser_q8_read: what rows of codes stand for, [M][N] of dtype (or of out's)."""
-    dev, M, N = _two_dims(codes, "codes", "int8")
+    dev, M, N, _, cs, cp = _matrix(codes, "codes", _CODES)
     if out is None:
         out = _out((M, N), dtype, codes.device, stream)
-    _check(lib().laser_q8_read(codes.data_ptr(), _rows(codes, "codes", M, N, torch.int8, dev), _line(scales, "scales", M, dev), M, N, _float_code(out, "out"),
-                               out.data_ptr(), _rows(out, "out", M, N, out.dtype, dev), _on(stream, dev)), "laser_q8_read")
+    dt, os_, op = _like(out, "out", M, N, _DTYPES, dev)
+    _check(lib().laser_q8_read(cp, cs, _line(scales, "scales", M, dev), M, N, dt, op, os_, _on(stream, dev)), "laser_q8_read")
     return out
 
 
@@ -721,17 +721,16 @@ def w8_matmul(w: W8, x: torch.Tensor, scales: torch.Tensor, dtype=torch.float16,
     """laser_w8_matmul: rows of codes x int8 [M][Kd] with their scales (q8_rows, q8_norm) -> [M][w.outs] of dtype (or of out's)."""
     if not isinstance(w, W8) or not w._h:
         raise LaserError("w must be a W8 that has not been closed")
-    dev, M, Kd = _two_dims(x, "x", "int8")
-    if w.device != dev:
-        raise LaserError(f"the weights are on device {w.device}, not on the current one")
-    step = _rows(x, "x", M, w.Kd, torch.int8, dev)
+    dev, M, Kd, _, step, xp = _matrix(x, "x", _CODES)
+    if w.device != dev or w.Kd != Kd:
+        raise LaserError(f"the weights are [{w.N}][{w.Kd}] on device {w.device}, the rows [{M}][{Kd}] on {dev}")
     # a row's bytes up to the next multiple of Q8_PAD are read
     if Kd % Q8_PAD and M and x.storage_offset() + (M - 1) * step + -(-Kd // Q8_PAD) * Q8_PAD > x.untyped_storage().nbytes():
         raise LaserError(f"rows of x must lie multiples of {Q8_PAD} bytes apart, and the memory of the last one reach as far")
     if out is None:
         out = _out((M, w.outs), dtype, x.device, stream)
-    _check(lib().laser_w8_matmul(w._h, x.data_ptr(), step, _line(scales, "scales", M, dev), M, _float_code(out, "out"), out.data_ptr(),
-                                 _rows(out, "out", M, w.outs, out.dtype, dev), _on(stream, dev)), "laser_w8_matmul")
+    dt, os_, op = _like(out, "out", M, w.outs, _DTYPES, dev)
+    _check(lib().laser_w8_matmul(w._h, xp, step, _line(scales, "scales", M, dev), M, dt, op, os_, _on(stream, dev)), "laser_w8_matmul")
     return out
 
 

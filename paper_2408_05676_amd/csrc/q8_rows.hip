@@ -296,14 +296,14 @@ static void launch_rows(const Q8Args& a, hipStream_t stream) {
     const long pieces = (a.N + 7l) / 8;
     auto go = [&](auto wprc, auto nvc) {
         constexpr int WPR = decltype(wprc)::value, NV = decltype(nvc)::value;
-        hipLaunchKernelGGL((q8_rows_kernel<DT, RT, NORM, WPR, NV>), dim3(WPR == 1 ? (a.M + 3) / 4 : a.M), dim3(WPR == 1 ? 256 : WPR * 64), 0, stream, a);
+        launch(q8_rows_kernel<DT, RT, NORM, WPR, NV>, dim3(WPR == 1 ? (a.M + 3) / 4 : a.M), dim3(WPR == 1 ? 256 : WPR * 64), stream, a);
     };
     using C1 = std::integral_constant<int, 1>;
     using C2 = std::integral_constant<int, 2>;
     using C4 = std::integral_constant<int, 4>;
     using C8 = std::integral_constant<int, 8>;
     using C16 = std::integral_constant<int, 16>;
-    if (a.N < 8) hipLaunchKernelGGL((q8_long_rows_kernel<DT, RT, NORM>), dim3(a.M), dim3(64), 0, stream, a);
+    if (a.N < 8) launch(q8_long_rows_kernel<DT, RT, NORM>, dim3(a.M), dim3(64), stream, a);
     else if (pieces <= 64) go(C1{}, C1{});
     else if (pieces <= 256) go(C4{}, C1{});
     else if (pieces <= 1024 && a.M <= 256) go(C16{}, C1{});
@@ -312,7 +312,7 @@ static void launch_rows(const Q8Args& a, hipStream_t stream) {
     else if (!NORM && pieces <= 1536 && a.M > 256) go(C8{}, std::integral_constant<int, NORM ? 2 : 3>{});
     else if (pieces <= 2048) go(C16{}, C2{});
     else if (!NORM && pieces <= 4096) go(C16{}, std::integral_constant<int, NORM ? 2 : 4>{});       // (the norm's rows would not fit the registers)
-    else hipLaunchKernelGGL((q8_long_rows_kernel<DT, RT, NORM>), dim3(a.M), dim3(1024), 0, stream, a);
+    else launch(q8_long_rows_kernel<DT, RT, NORM>, dim3(a.M), dim3(1024), stream, a);
 }
 
 int launch_q8(const Q8Args& a, int dtype, int res_dtype, hipStream_t stream) {
@@ -417,7 +417,7 @@ extern "C" int laser_q8_read(const int8_t* codes, int64_t codes_stride, const fl
     const long pieces = (N + 7l) / 8;
     const dim3 block(pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256), grid(M, (unsigned)std::min((pieces + block.x - 1) / block.x, 1024l));
     const auto kernel = dtype == LASER_F32 ? q8_read_kernel<DT_F32> : dtype == LASER_BF16 ? q8_read_kernel<DT_BF16> : q8_read_kernel<DT_F16>;
-    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)stream, codes, codes_stride, scales, N, out, out_stride);
+    launch(kernel, grid, block, (hipStream_t)stream, codes, codes_stride, scales, N, out, out_stride);
     LASER_HIP_CHECK(hipGetLastError());
     return LASER_OK;
 }

@@ -157,8 +157,8 @@ inline void launch_w8_few(W8Args a, bool gated, int v, hipStream_t stream) {
         a.tiles_n = (a.rows / 16 + F.nt - 1) / F.nt;
         const dim3 grid(8u * (unsigned)((a.tiles_m * a.tiles_n + 7) / 8));
         if constexpr (F.nt % 2 == 0)
-            if (gated) hipLaunchKernelGGL((w8_few_kernel<F.mt, F.nt, F.wk, true>), grid, dim3(64 * F.wk), 0, stream, a);
-        if (!gated) hipLaunchKernelGGL((w8_few_kernel<F.mt, F.nt, F.wk, false>), grid, dim3(64 * F.wk), 0, stream, a);
+            if (gated) launch(w8_few_kernel<F.mt, F.nt, F.wk, true>, grid, dim3(64 * F.wk), stream, a);
+        if (!gated) launch(w8_few_kernel<F.mt, F.nt, F.wk, false>, grid, dim3(64 * F.wk), stream, a);
     });
 }
 

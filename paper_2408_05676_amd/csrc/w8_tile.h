@@ -261,7 +261,7 @@ inline void go_w8_tile(W8Args a, int v, hipStream_t stream) {
         a.tiles_m = (a.M + WM * 16 - 1) / (WM * 16);
         a.tiles_n = (a.rows + WN * 64 - 1) / (WN * 64);
         const unsigned grid = 8u * (unsigned)((a.tiles_m * a.tiles_n + 7) / 8);
-        hipLaunchKernelGGL((w8_gemm_tile_kernel<WM, WN, GATED>), dim3(grid), dim3(64 * kW8Waves), 0, stream, a);
+        launch(w8_gemm_tile_kernel<WM, WN, GATED>, dim3(grid), dim3(64 * kW8Waves), stream, a);
     });
 }
 void launch_w8_tile_plain(const W8Args& a, int v, hipStream_t stream);
