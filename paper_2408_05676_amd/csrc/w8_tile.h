@@ -143,7 +143,8 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
         constexpr int s = decltype(sc)::value, q = decltype(qc)::value, L0 = decltype(l0c)::value, L1 = decltype(l1c)::value, NMUL = WM * WN;
         static_for<0, NMUL>([&](auto mc) {
             constexpr int m = decltype(mc)::value, j = m / WM, i = m % WM;
-            static_for<m * WM / NMUL, (m + 1) * WM / NMUL>([&](auto ic) { read_x(std::integral_constant<int, 1 - s>{}, ic, rslot); });
+            constexpr int r0 = 2 * m * WM / NMUL, r1 = 2 * (m + 1) * WM / NMUL;              // (in the first half: the wait behind the step finds them done)
+            static_for<(r0 < WM ? r0 : WM), (r1 < WM ? r1 : WM)>([&](auto ic) { read_x(std::integral_constant<int, 1 - s>{}, ic, rslot); });
             constexpr int l0 = L0 + (2 * m * (L1 - L0) + NMUL) / (2 * NMUL), l1 = L0 + (2 * (m + 1) * (L1 - L0) + NMUL) / (2 * NMUL);
             static_for<l0, l1>([&](auto jc) { issue(jc); });
             if constexpr (decltype(firstc)::value) mfma_i8_first<(m >= 64)>(fw[q][j], fx[s][i], acc[j][i]);
