@@ -5,7 +5,7 @@
 // products are exact: a code is the formula's whatever the order of operations, and squares of any fp32 rows have room. t = u (127 / m) is
 // off by some 2^-45; only where it is closer than 2^-30 to a half is the quotient itself taken.
 // Bound: a launch and one round trip to memory up to some hundred rows (1 x 4096 3.0 us, with the norm 3.7; an empty launch 2.3), then both and the vector
-// instructions of the codes: 704 x 11008 fp16 8.8 us (2.6 TB/s; a copy of as many bytes takes 4.6), the norm of 704 x 4096 with its residual in bf16 8.3 us (2.4 TB/s). Reading back 5.3 us
+// instructions of the codes: 704 x 11008 fp16 8.1 us (2.9 TB/s; a copy of as many bytes takes 4.6), the norm of 704 x 4096 with its residual in bf16 8.3 us (2.4 TB/s). Reading back 5.3 us
 // (704 x 11008, 4.4 TB/s).
 #include <algorithm>
 
@@ -68,6 +68,7 @@ __device__ inline void store8(void* p, int64_t o, int left, const float (&x)[8])
 #pragma unroll
     for (int i = 0; i < 8; ++i) if (i < left) store_elem<DT>(p, o + i, x[i]);
 }
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2_a1 __attribute__((ext_vector_type(2), aligned(1)));
 
 // rint(127 u / m) in the low byte; inv = 127 / m. Adding 1.5 2^52 rounds to nearest even and leaves the whole number in the low bits.
@@ -100,7 +101,7 @@ __device__ inline T wave_fold(T x, F op) {
     return op(x, __shfl_xor(x, 32));
 }
 __device__ inline double wave_max(double x) { return wave_fold(x, [](double a, double b) { return fmax(a, b); }); }
-__device__ inline float wave_max(float x) { return wave_fold(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ inline uint32_t wave_max(uint32_t x) { return wave_fold(x, [](uint32_t a, uint32_t b) { return max(a, b); }); }
 __device__ inline double wave_sum(double x) { return wave_fold(x, [](double a, double b) { return a + b; }); }
 
 // A row's scale. m: its largest |u|.
@@ -113,9 +114,9 @@ __device__ inline float row_scale(double m, double ss, bool bad, int N, float ep
 
 // WPR waves a row (four rows a workgroup where that is one), NV times eight columns a thread: the row stays in registers between its statistics and its codes.
 //
-// Codes take 32-bit numbers wherever those decide: h, u, m, its reciprocal (two), 127 times that and t are a rounding each, so t is within 127 7 2^-24 < 2^-14
+// Codes take 32-bit numbers wherever those decide: h, u, m, its reciprocal (two) and 127 times that are a rounding each, so t (never rounded itself) is within 127 6 2^-24 < 2^-14
 // of the formula's (sums of two floats never lose a small part; a product that does is 2^-66 of m). Elements closer than that to a half take 64 bits, one
-// at a time: with all eight of a thread's where one is close, 704 rows of 11008 took 11.4 us, so 8.9.
+// at a time: with all eight of a thread's where one is close, 704 rows of 11008 took 11.4 us, so 8.9 (8.1 since packed bytes and the largest by bits).
 template <int DT, int RT, bool NORM, int WPR, int NV>
 __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Args a) {
     __shared__ double sm_m[WPR], sm_ss[WPR];
@@ -147,7 +148,9 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Ar
             }
         }
     double m = 0, ss = 0;
-    float m32 = 0, z = 0;                                // z: NaN where x or the gain is not finite (the norm: where the gain is not)
+    float z = 0;                                         // NaN where the gain is not finite
+    uint32_t top = 0;                                    // without the norm: the largest |x| as its bits, which are in the order of the numbers, past the infinity's if one is
+    u16x2 top2 = {0, 0};                                 // not a number; 16-bit elements in pairs
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int left = a.N - (v * WPR * 64 + t) * 8;
@@ -173,14 +176,22 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Ar
             if constexpr (RES) store8<RT>(a.res_out, row * a.res_out_stride + a.N - left, left, sum);
         } else
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                m32 = fmaxf(m32, fabsf(x[v].get(i)));
-                z = fmaf(x[v].get(i), 0.f, z);
+            for (const uint32_t w : x[v].w) {
+                if constexpr (DT == DT_F32) top = max(top, w & 0x7FFFFFFFu);
+                else top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
             }
     }
-    if constexpr (NORM) { m = wave_max(m); ss = wave_sum(ss); }
-    else m = (double)wave_max(m32);
-    bool bad = __any(!(z == 0)) || !(ss < INFINITY);     // (squares of finite sums do not pass 64 bits)
+    bool bad;
+    if constexpr (NORM) {
+        m = wave_max(m);
+        ss = wave_sum(ss);
+        bad = __any(!(z == 0)) || !(ss < INFINITY);      // (squares of finite sums do not pass 64 bits)
+    } else {
+        if constexpr (DT != DT_F32) top = max(top2[0], top2[1]);
+        top = wave_max(top);
+        bad = top >= (DT == DT_F32 ? 0x7F800000u : DT == DT_BF16 ? 0x7F80u : 0x7C00u);
+        m = DT == DT_F32 ? (double)__uint_as_float(top) : DT == DT_BF16 ? (double)bf16_to_f32((uint16_t)top) : (double)f16_to_f32((uint16_t)top);
+    }
     if constexpr (WPR > 1) {
         if ((t & 63) == 0) { sm_m[wave] = m; sm_ss[wave] = ss; sm_bad[wave] = bad; }
         __syncthreads();
@@ -196,17 +207,26 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Ar
         if (left <= 0) continue;
         uint32_t w[2] = {0, 0};
         if (some) {
-            uint32_t close = usual ? 0 : 255;
+            constexpr float kWhole = 0x1.8p23f, kFar = 0.5f - 0x1p-14f;      // as in q8_code
+            float u[8], n[8];
+            uint32_t far = 0;                            // bits of the largest distance from a whole number: one that is not a number is beyond all
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                constexpr float kWhole = 0x1.8p23f;      // as in q8_code
-                float u = x[v].get(i);
-                if constexpr (RES) u += r[v].get(i);
-                if constexpr (NORM) u *= g[v].get(i);
-                const float y = u * inv32, n = y + kWhole;
-                close |= !(fabsf(y - (n - kWhole)) <= 0.5f - 0x1p-14f) ? 1u << i : 0u;
-                w[i / 4] |= (__float_as_uint(n) & 255u) << (8 * (i & 3));
+                u[i] = x[v].get(i);
+                if constexpr (RES) u[i] += r[v].get(i);
+                if constexpr (NORM) u[i] *= g[v].get(i);
+                n[i] = fmaf(u[i], inv32, kWhole);
+                far = max(far, __float_as_uint(fmaf(u[i], inv32, kWhole - n[i])) & 0x7FFFFFFFu);
             }
+            static_for<0, 2>([&](auto hc) {
+                constexpr int h = decltype(hc)::value * 4;
+                auto bits = [&](int i) { return __float_as_uint(n[h + i]); };
+                w[h / 4] = __builtin_amdgcn_perm(bits(1), bits(0), 0x0C0C0400u) | __builtin_amdgcn_perm(bits(3), bits(2), 0x04000C0Cu);
+            });
+            uint32_t close = usual ? 0 : 255;
+            if (far > __float_as_uint(kFar))
+#pragma unroll
+                for (int i = 0; i < 8; ++i) close |= !(fabsf(fmaf(u[i], inv32, kWhole - n[i])) <= kFar) ? 1u << i : 0u;
             while (close) {
                 const int i = __ffs(close) - 1;
                 close &= close - 1;

@@ -382,3 +382,19 @@ def test_captured_and_replayed(M):
             torch.cuda.synchronize()
             want, *_ = feed_forward(x, was, gain, gu, down)
             assert torch.equal(out, want) and torch.equal(res, was)
+
+
+def test_sums_that_pass_fp32_beside_small_gains():
+    """h beyond fp32's largest number, products with the gain of ordinary size: codes are the 64-bit formula's all the same, the sum itself is infinite."""
+    g = gen(21)
+    N = 96
+    x, res = normal(g, 4, N), normal(g, 4, N)
+    x[1, 5] = res[1, 5] = 3e38
+    x[2] = res[2] = 2.5e38
+    gain = 1 + 0.1 * normal(g, N)
+    gain[5] = 1e-38
+    c, s, h = ref.norm(x, gain, 1e-6, res)
+    out = torch.empty_like(x)
+    codes, scales = laser.q8_norm(x, gain, residual=res, residual_out=out)
+    assert torch.equal(codes, c) and ref.scales_close(scales, s) and torch.equal(out, h.float())
+    assert bool(out[1, 5].isinf()) and bool(out[2].isinf().all()) and bool(scales.isfinite().all())
