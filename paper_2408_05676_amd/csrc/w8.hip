@@ -44,7 +44,9 @@ static int w8_pick(const W8Args& a, bool gated) {
     for (int v = 0; v < kW8FewN; ++v) {
         const W8Few f = kW8Few[v];
         if (f.mt == 0 || (gated && f.nt % 2)) continue;
-        const double each = (double)up(up(frags, f.nt) * up(a.M, 16 * f.mt), cus);
+        const long units = up(frags, f.nt) * up(a.M, 16 * f.mt);
+        if (units * 64 * f.wk >= (1l << 32)) continue;           // (a launch's threads)
+        const double each = (double)up(units, cus);
         const double us = 3.07 + each * (k * (0.141 * f.nt + 0.169 * f.mt) + 0.052 + 0.0914 * f.nt * f.mt) + 0.0979 * weights + 0.568 * results;
         if (us < least) { least = us; best = v; }
     }

@@ -1,4 +1,10 @@
 // Products of few rows in 8-bit codes with 8-bit weights (see eight_bit.h): the waves of a workgroup share the inputs of its outputs.
+//
+// out[r][n] = s_x[r] s_w[n] sum of c_x c_w. A wave takes its share of the inputs of 16 NT outputs and 16 MT rows, weights a kilobyte a load straight into registers; the
+// waves' sums meet in LDS. Every workgroup reads its rows whole, from L2: with few outputs (one layer's 4096) that is as much as the weights from some 30 rows on.
+//
+// Bound: the weights' way from memory (one row gated 4096 -> 2 x 11008 90 MB in 18.3 us, 4.9 TB/s where a long read reaches 5.5; 4096 -> 12288 12.3 us, 11008 -> 4096 10.4 us, nine rows
+// 11.0), with more rows theirs through LDS too (72 rows 11008 -> 4096 16.6 us, 2048 -> 6144 7.6 us: start 0.7, stages 3.9, sums 1, launch 2).
 #pragma once
 
 #include "w8_tile.h"
@@ -29,6 +35,8 @@ __global__ __launch_bounds__(64 * WK) void w8_few_kernel(W8Args a) {
     const int nst = a.Kp / 128, nx = (a.Kd + 127) / 128;             // stages of 128 inputs; nst is even, where nx is odd the last stage of weights is zeros
     const int k0 = (int)((long)nst * wave / WK), k1 = (int)((long)nst * (wave + 1) / WK);
 
+    // The scales' lines are asked for now: behind the last product they would be a round trip to memory.
+    const float touch_w = a.w_scales[min(tile0 * 16 + (int)threadIdx.x, a.rows - 1)], touch_x = a.x_scales[min(row0 + (int)threadIdx.x, a.M - 1)];
     int4_t acc[NT][MT];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -112,6 +120,7 @@ __global__ __launch_bounds__(64 * WK) void w8_few_kernel(W8Args a) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");               // surplus rows must not land in what follows
     }
 
+    asm volatile("" ::"v"(touch_w), "v"(touch_x));
     // ---- the waves' sums; a thread adds up, scales and stores four outputs of a row, threads side by side the next ones
     __syncthreads();
     int4_t* const sums = reinterpret_cast<int4_t*>(lds);             // [wave][output fragment][row][four outputs]

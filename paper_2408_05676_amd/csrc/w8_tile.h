@@ -1,4 +1,14 @@
 // Products of many rows in 8-bit codes with 8-bit weights (see eight_bit.h): a tile of rows by four waves' columns a workgroup.
+//
+// out[r][n] = s_x[r] s_w[n] sum of c_x c_w: integers, so the order of the sums does not matter and nothing is rounded before the scales.
+// All four waves multiply the same WM x 16 rows, each with WN x 16 columns of its own: rows come through LDS, once a workgroup, and weights straight into the registers of the
+// one wave that needs them, in the order its lanes hold them. At 11 x 6 fragments a wave a stage (128 inputs) takes 110 KB through LDS, in and out, where waves arranged 2 x 2
+// with both operands in it would take 212, and 70 KB from L2, 34 bytes a clock of its matrix instructions.
+//
+// Bound: few hundred rows, the weights' way from memory and the two ends of a launch (249 rows gated 2048 -> 2 x 5632, 128 x 128 tiles on 176 compute units: start 1.3 us, 16 stages 7.1, results
+// 2.1, launch 2); many rows, the matrix instructions at the clock that the card holds under them (704 rows gated 4096 -> 2 x 11008, 176 x 384 tiles: start 3.6, 32 stages of 1.3 us,
+// results 8.6; a stage's matrix instructions alone 0.90 us, all of it with zeros as data 1.15). 704 rows, weights from memory: 4096 -> 12288 40 us (1.77 POP/s), gated
+// 4096 -> 2 x 11008 60 us (2.1), 11008 -> 4096 41 us, 4096 -> 4096 18 us; a library's int8 products of these sizes without the epilogue 64, 90 and 55 us (8192 cubed: 2.04 POP/s).
 #pragma once
 
 #include "eight_bit.h"
@@ -35,6 +45,10 @@ __device__ inline void w8_store(const W8Args& a, int row, int n, const float (&o
 __device__ inline void load_to_lds(uint64_t base, uint32_t vo, uint32_t at) {
     const u32x4 srd{(uint32_t)base, (uint32_t)(base >> 32), 0xFFFFFFFFu, 0x00020000u};
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" ::"v"(vo), "s"(at), "s"(srd) : "memory", "m0");
+}
+__device__ inline void load_dword_to_lds(uint64_t base, uint32_t vo, uint32_t at) {          // four bytes a lane
+    const u32x4 srd{(uint32_t)base, (uint32_t)(base >> 32), 0xFFFFFFFFu, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %0, %2, 0 offen lds" ::"v"(vo), "s"(at), "s"(srd) : "memory", "m0");
 }
 __device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
@@ -111,7 +125,8 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
     };
     auto next_w = [&] { ++wreq; wbase += wreq < 2 * nk ? wstep : 0; };
 
-    // The workgroups of a column of tiles walk the same weights together. Each touches its share of the lines PD stages ahead.
+    // The workgroups of a column of tiles walk the same weights together. Each touches its share of their lines PD stages ahead, so that the others find them in L2: 704 rows of
+    // 16384 -> 12288 129 -> 115 us with zeros as data, a few per cent with others (5 or 9 stages ahead no better).
     constexpr int PD = 3;
     const int line = min(tm + a.tiles_m * (wave * 64 + lane), WN * 16 * NW - 1);       // of a stage: 64-byte rows in pairs, step by step
     const int tile0 = tn * NW * WN * 16, step_lines = min(NW * WN * 16, a.rows - tile0) / 2;
@@ -120,10 +135,7 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
     int treq = 0;
     const uint32_t junk = lds_address(lds) + SBYTES * NS + wave * 256;
     auto touch_ahead = [&] {
-        if (a.tiles_m > 1) {
-            const u32x4 srd{(uint32_t)tbase, (uint32_t)(tbase >> 32), 0xFFFFFFFFu, 0x00020000u};
-            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %0, %2, 0 offen lds" ::"v"(touch), "s"(junk), "s"(srd) : "memory", "m0");
-        }
+        if (a.tiles_m > 1) load_dword_to_lds(tbase, touch, junk);
         ++treq;
         tbase += treq < nk ? 2 * wstep : 0;
     };
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(64 * kW8Waves, 1) void w8_gemm_tile_kernel(W8Args a
     });
 
     // ---- results: a lane holds columns 4 lg .. 4 lg + 3 of every fragment, row lr of every 16. They leave by way of LDS, so that threads side by
-    // side store whole lines.
+    // side store whole lines (in pieces of eight bytes 17 MB took 10 us, so 4). Sums put there as integers and scaled by the threads that store them: 704 rows gated 61 -> 66 us.
     auto store = [&](auto dt) {
         constexpr int DT = decltype(dt)::value, OC = (GATED ? WN / 2 : WN) * 16, ES = DT == DT_F32 ? 4 : 2;      // columns of a wave, bytes
         constexpr int PITCH = OC * NW * ES + 16, PPR = OC * NW * ES / 16, EPP = 16 / ES;                         // pieces of 16 bytes of a row

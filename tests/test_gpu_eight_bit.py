@@ -398,3 +398,53 @@ def test_sums_that_pass_fp32_beside_small_gains():
     codes, scales = laser.q8_norm(x, gain, residual=res, residual_out=out)
     assert torch.equal(codes, c) and ref.scales_close(scales, s) and torch.equal(out, h.float())
     assert bool(out[1, 5].isinf()) and bool(out[2].isinf().all()) and bool(scales.isfinite().all())
+
+
+def test_sizes_past_32_bits():
+    """Results, rows and weights of more than 4 GiB: their last rows and outputs."""
+    g = gen(30)
+    w, sw = made(g, 32800, 64)
+    h = laser.W8(w, sw)
+    M = 70000                                                              # 70000 x 32800 fp16: 4.6 GB
+    x = torch.randint(-127, 128, (M, 128), generator=g, device="cuda", dtype=torch.int16).to(torch.int8)[:, :64]
+    sx = torch.rand(M, generator=g, device="cuda")
+    out = laser.w8_matmul(h, x, sx)
+    for at in (slice(0, 3), slice(65530, 65540), slice(M - 3, M)):
+        assert ref.product_close(out[at], ref.product(x[at], sx[at], w, sw))
+    del out
+    big = torch.empty((300000, 8192), dtype=BF16, device="cuda").normal_(0, 1, generator=g)          # 4.9 GB
+    codes, scales = laser.q8_rows(big)
+    for at in (slice(0, 2), slice(299990, 300000)):
+        c, s = ref.rows(big[at])
+        assert torch.equal(codes[at], c) and torch.equal(scales[at], s)
+    gain = 1 + 0.1 * normal(g, 8192)
+    normed, _ = laser.q8_norm(big, gain, residual=big)
+    tail = big[-3:].clone()
+    values = laser.q8_read(codes, scales, dtype=BF16, out=big)
+    assert ref.values_close(values[-3:], codes[-3:], scales[-3:])
+    del big, values
+    h, out = None, None
+    N, Kd = 540000, 8192                                                   # 4.4 GB of weights
+    wide = torch.randint(-128, 128, (N, Kd), generator=g, device="cuda", dtype=torch.int8)
+    sw = torch.rand(N, generator=g, device="cuda")
+    for M in (3, 20, 200):
+        x, sx = made(g, M, Kd)
+        if h is None:
+            h = laser.W8(wide, sw)
+        out = laser.w8_matmul(h, x, sx, dtype=F32)
+        for at in (slice(0, 40), slice(N - 40, N)):
+            assert ref.product_close(out[:, at], ref.product(x, sx, wide[at], sw[at]))
+    assert tail.isfinite().all() and normed.shape == codes.shape
+
+
+def test_a_broadcast_residual_is_not_written_to():
+    g = gen(31)
+    x, res, gain = normal(g, 5, 64), normal(g, 1, 64).expand(5, 64), torch.ones(64, device="cuda")
+    with pytest.raises(laser.LaserError, match="overlap"):
+        laser.q8_norm(x, gain, residual=res)
+    out = torch.empty_like(x)
+    c, _, h = ref.norm(x, gain, 1e-6, res)
+    codes, _ = laser.q8_norm(x, gain, residual=res, residual_out=out)
+    assert torch.equal(codes, c) and torch.equal(out, h.float())
+    with pytest.raises(laser.LaserError, match="type"):
+        laser.q8_norm(x.half(), gain, residual=res, residual_out=out.half())
