@@ -290,7 +290,8 @@ class Model:
                 raise LaserError(f"the matrix must be a {kind.__name__} that has not been closed, or None")
             if w.device != self.device:
                 raise LaserError(f"the matrix is on device {w.device}, the model on {self.device}")
-        _check(call(self._h, layer, names.index(name), w._h if w is not None else None), call.__name__)
+        with torch.cuda.device(self.device):                                     # (the first W8 allocates)
+            _check(call(self._h, layer, names.index(name), w._h if w is not None else None), call.__name__)
         if w is not None:
             self._w4.add(w)
             w._models.add(self)

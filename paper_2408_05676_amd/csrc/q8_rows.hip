@@ -1,11 +1,10 @@
 // Rows into 8-bit codes with one scale each, alone or behind the residual's addition and the root-mean-square norm, and back.
 //
 // h = x + res, u = h gain (u = x without the norm), m = max |u|: codes c = rint(127 u / m) and scale s = m / 127 / sqrt(mean h^2 + eps).
-// The root is the same for a row's elements, so codes need the extremes of h gain only. All in 64 bits, where x + res and the
-// products are exact: a code is the formula's whatever the order of operations, and squares of any fp32 rows have room. t = u (127 / m) is
-// off by some 2^-45; only where it is closer than 2^-30 to a half is the quotient itself taken.
-// Bound: a launch and one round trip to memory up to some hundred rows (1 x 4096 3.0 us, with the norm 3.7; an empty launch 2.3), then both and the vector
-// instructions of the codes: 704 x 11008 fp16 8.1 us (2.9 TB/s; a copy of as many bytes takes 4.6), the norm of 704 x 4096 with its residual in bf16 8.3 us (2.4 TB/s). Reading back 5.3 us
+// The root is the same for a row's elements, so codes need the extremes of h gain only. h, u and 127 u are 64-bit numbers, of which a code is the formula's exactly, and
+// squares of any fp32 rows have room.
+// Bound: a launch and one round trip to memory up to some hundred rows (1 x 4096 2.4 us, with the norm 3.6; an empty launch 2.3), then both and the vector
+// instructions of the codes: 704 x 11008 fp16 7.1 us (3.3 TB/s; a copy of as many bytes takes 4.6), the norm of 704 x 4096 with its residual in bf16 7.7 us (2.6 TB/s). Reading back 5.3 us
 // (704 x 11008, 4.4 TB/s).
 #include <algorithm>
 
@@ -37,6 +36,14 @@ struct Raw8 {
         else if constexpr (DT == DT_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
         else return f16_to_f32((uint16_t)(w[i / 2] >> (16 * (i & 1))));
     }
+    __device__ float pick(int i) const {                 // the same for an i that is known at run time only
+        auto two = [&](uint32_t a, uint32_t b, int bit) { return i & bit ? b : a; };
+        if constexpr (DT == DT_F32) return __uint_as_float(two(two(two(w[0], w[1], 1), two(w[2], w[3], 1), 2), two(two(w[4], w[5], 1), two(w[6], w[7], 1), 2), 4));
+        else {
+            const uint16_t h = (uint16_t)(two(two(w[0], w[1], 2), two(w[2], w[3], 2), 4) >> (16 * (i & 1)));
+            return DT == DT_BF16 ? bf16_to_f32(h) : f16_to_f32(h);
+        }
+    }
 };
 template <int DT>
 __device__ inline void load8(Raw8<DT>& r, const void* p, int64_t o) {
@@ -50,18 +57,6 @@ __device__ inline void load8(Raw8<DT>& r, const void* p, int64_t o) {
         for (int i = 0; i < 4; ++i) r.w[i] = a[i];
     }
 }
-// The first `left` (1 .. 7) of them, zeros behind.
-template <int DT>
-__device__ inline void load_tail(Raw8<DT>& r, const void* p, int64_t o, int left) {
-#pragma unroll
-    for (uint32_t& w : r.w) w = 0;
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (i < left) {
-            if constexpr (DT == DT_F32) r.w[i] = ((const uint32_t*)p)[o + i];
-            else r.w[i / 2] |= (uint32_t)((const uint16_t*)p)[o + i] << (16 * (i & 1));
-        }
-}
 template <int DT>
 __device__ inline void store8(void* p, int64_t o, int left, const float (&x)[8]) {
     if (left >= 8) { store_elems<DT, 8>(p, o, x); return; }
@@ -71,13 +66,13 @@ __device__ inline void store8(void* p, int64_t o, int left, const float (&x)[8])
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2_a1 __attribute__((ext_vector_type(2), aligned(1)));
 
-// rint(127 u / m) in the low byte; inv = 127 / m. Adding 1.5 2^52 rounds to nearest even and leaves the whole number in the low bits.
-__device__ inline uint32_t q8_code(double u, double inv, double m) {
+// rint(127 u / m) in the low byte; rcp is 1 / m to a few places, so that c is the code or its neighbour, and what is left of 127 u tells which: it is exact, as c m has fewer
+// bits than the fused product keeps. Adding 1.5 2^52 rounds to nearest even and leaves the whole number in the low bits.
+__device__ inline uint32_t q8_code(double u, double rcp, double m) {
     constexpr double kWhole = 0x1.8p52;
-    const double t = u * inv;
-    double c = t + kWhole;
-    if (fabs(t - (c - kWhole)) > 0.5 - 0x1p-30) c = 127.0 * u / m + kWhole;
-    return (uint32_t)__builtin_bit_cast(uint64_t, c);
+    const double p = 127.0 * u, n = fma(p, rcp, kWhole), e = fma(kWhole - n, m, p), twice = fabs(e) + fabs(e);
+    const uint32_t c = (uint32_t)__builtin_bit_cast(uint64_t, n);
+    return twice > m || (twice == m && (c & 1)) ? c + (e > 0 ? 1u : ~0u) : c;
 }
 
 // x of another lane of the same sixteen (dpp control CTRL)
@@ -90,15 +85,35 @@ __device__ inline T row_move(T x) {
         return __builtin_bit_cast(T, (uint64_t)hi << 32 | lo);
     }
 }
-// op over a wave, in every lane: pairs, fours, eights and sixteens by lane moves, then rows of sixteen
+// op(a, b) of the sixteens (HALVES: halves) of a wave that lie side by side, in both: swapping x's odd ones with the even ones of a copy leaves all the even ones in one
+// register and all the odd ones in the other.
+template <bool HALVES, class T, class F>
+__device__ inline T fold_sides(T x, F op) {
+    auto swap = [](uint32_t a, uint32_t& even, uint32_t& odd) {
+        if constexpr (HALVES) { const auto r = __builtin_amdgcn_permlane32_swap(a, a, false, false); even = r[0]; odd = r[1]; }
+        else { const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false); even = r[0]; odd = r[1]; }
+    };
+    if constexpr (sizeof(T) == 4) {
+        uint32_t a, b;
+        swap(__builtin_bit_cast(uint32_t, x), a, b);
+        return op(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b));
+    } else {
+        const uint64_t u = __builtin_bit_cast(uint64_t, x);
+        uint32_t al, bl, ah, bh;
+        swap((uint32_t)u, al, bl);
+        swap((uint32_t)(u >> 32), ah, bh);
+        return op(__builtin_bit_cast(T, (uint64_t)ah << 32 | al), __builtin_bit_cast(T, (uint64_t)bh << 32 | bl));
+    }
+}
+// op over a wave, in every lane
 template <class T, class F>
 __device__ inline T wave_fold(T x, F op) {
     x = op(x, row_move<0xB1>(x));                    // lanes 1 0 3 2 of four
     x = op(x, row_move<0x4E>(x));                    // lanes 2 3 0 1
     x = op(x, row_move<0x141>(x));                   // eight lanes mirrored
     x = op(x, row_move<0x140>(x));                   // sixteen mirrored
-    x = op(x, __shfl_xor(x, 16));
-    return op(x, __shfl_xor(x, 32));
+    x = fold_sides<false>(x, op);
+    return fold_sides<true>(x, op);
 }
 __device__ inline double wave_max(double x) { return wave_fold(x, [](double a, double b) { return fmax(a, b); }); }
 __device__ inline uint32_t wave_max(uint32_t x) { return wave_fold(x, [](uint32_t a, uint32_t b) { return max(a, b); }); }
@@ -113,14 +128,18 @@ __device__ inline float row_scale(double m, double ss, bool bad, int N, float ep
 }
 
 // WPR waves a row (four rows a workgroup where that is one), NV times eight columns a thread: the row stays in registers between its statistics and its codes.
+// Behind the end of a row there are no elements: a thread that would pass it takes the last eight, some of them a second time (results are stored behind the barrier, when
+// all have been read; only the squares leave the others' out).
 //
-// Codes take 32-bit numbers wherever those decide: h, u, m, its reciprocal (two) and 127 times that are a rounding each, so t (never rounded itself) is within 127 6 2^-24 < 2^-14
-// of the formula's (sums of two floats never lose a small part; a product that does is 2^-66 of m). Elements closer than that to a half take 64 bits, one
-// at a time: with all eight of a thread's where one is close, 704 rows of 11008 took 11.4 us, so 8.9 (8.1 since packed bytes and the largest by bits).
+// Codes take 32-bit numbers wherever those decide. inv is 127 / m with one rounding, u has one of the sum and one of the product with the gain (neither without the norm),
+// t = u inv is never rounded itself and its distance from a whole number by 2^-25 at most: together less than 127 2^-24 + 2^-25 < 1.0625 2^-17, with the norm
+// 3 127 2^-24 + 2^-25 < 1.5625 2^-16. (Sums of two floats never lose a small part; a product that does is 2^-66 of m.) Elements closer than that to a half take 64 bits, one at a time.
+// A launch of some hundred rows has such elements somewhere, and waits for them: what costs is the way through instructions that no other wave has fetched, so they are few. 704 rows of
+// 11008: all eight of a thread's in 64 bits 11.4 us; one at a time, with two divisions in the way 8.1 (with limits of 2^-14 as of 2^-22), without 7.1, not at all 6.1.
 template <int DT, int RT, bool NORM, int WPR, int NV>
 __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Args a) {
-    __shared__ double sm_m[WPR], sm_ss[WPR];
-    __shared__ int sm_bad[WPR];
+    __shared__ __attribute__((aligned(16))) double sm_m[WPR], sm_ss[WPR];
+    __shared__ __attribute__((aligned(16))) uint32_t sm_top[WPR];
     const int wave = threadIdx.x >> 6, t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
     const int64_t row = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
     if (WPR == 1 && row >= a.M) return;
@@ -128,7 +147,7 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Ar
     Raw8<DT> x[NV];
     Raw8<RES ? RT : DT_F16> r[RES ? NV : 1];
     Raw8<DT_F32> g[NORM ? NV : 1];
-    // All loads go out together, without a branch: a row has eight elements at least, and behind its end its last eight come again.
+    // All loads go out together, without a branch: a row has eight elements at least.
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = min((v * WPR * 64 + t) * 8, a.N - 8);
@@ -137,16 +156,6 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Ar
         if constexpr (NORM) load8<DT_F32>(g[v], a.gain, c);
     }
     asm volatile("" ::: "memory");
-    if (a.N & 7)
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int c = (v * WPR * 64 + t) * 8, left = a.N - c;
-            if (left > 0 && left < 8) {
-                load_tail<DT>(x[v], a.x, row * a.x_stride + c, left);
-                if constexpr (RES) load_tail<RT>(r[v], a.res, row * a.res_stride + c, left);
-                if constexpr (NORM) load_tail<DT_F32>(g[v], a.gain, c, left);
-            }
-        }
     double m = 0, ss = 0;
     float z = 0;                                         // NaN where the gain is not finite
     uint32_t top = 0;                                    // without the norm: the largest |x| as its bits, which are in the order of the numbers, past the infinity's if one is
@@ -163,17 +172,24 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Ar
                 for (int i = 0; i < 8; ++i) x[v].w[i] = __float_as_uint(x[v].get(i) + q.get(i));
             }
         if constexpr (NORM) {
-            float sum[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            auto sum = [&](int i) {
                 double h = (double)x[v].get(i);
                 if constexpr (RES) h += (double)r[v].get(i);
+                return h;
+            };
+            const double before = ss;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double h = sum(i);
                 m = fmax(m, fabs(h * (double)g[v].get(i)));
                 ss = fma(h, h, ss);
                 z = fmaf(g[v].get(i), 0.f, z);
-                sum[i] = (float)h;
             }
-            if constexpr (RES) store8<RT>(a.res_out, row * a.res_out_stride + a.N - left, left, sum);
+            if (left < 8) {
+                ss = before;
+#pragma unroll
+                for (int i = 1; i < 8; ++i) ss = i >= 8 - left ? fma(sum(i), sum(i), ss) : ss;
+            }
         } else
 #pragma unroll
             for (const uint32_t w : x[v].w) {
@@ -181,73 +197,83 @@ __global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void q8_rows_kernel(Q8Ar
                 else top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
             }
     }
-    bool bad;
+    // An infinite m stands for a row that is not finite: products of two floats stay below it. Only the first thread needs the squares.
     if constexpr (NORM) {
+        if (!(z == 0) || !(ss < INFINITY)) m = INFINITY;     // (squares of finite sums do not pass 64 bits)
         m = wave_max(m);
         ss = wave_sum(ss);
-        bad = __any(!(z == 0)) || !(ss < INFINITY);      // (squares of finite sums do not pass 64 bits)
+        if constexpr (WPR > 1) {
+            if ((t & 63) == 0) { sm_m[wave] = m; sm_ss[wave] = ss; }
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WPR; ++w) m = fmax(m, sm_m[w]);
+            if (t == 0)
+#pragma unroll
+                for (int w = 1; w < WPR; ++w) ss += sm_ss[w];
+        }
     } else {
         if constexpr (DT != DT_F32) top = max(top2[0], top2[1]);
         top = wave_max(top);
-        bad = top >= (DT == DT_F32 ? 0x7F800000u : DT == DT_BF16 ? 0x7F80u : 0x7C00u);
-        m = DT == DT_F32 ? (double)__uint_as_float(top) : DT == DT_BF16 ? (double)bf16_to_f32((uint16_t)top) : (double)f16_to_f32((uint16_t)top);
-    }
-    if constexpr (WPR > 1) {
-        if ((t & 63) == 0) { sm_m[wave] = m; sm_ss[wave] = ss; sm_bad[wave] = bad; }
-        __syncthreads();
-        m = sm_m[0]; ss = sm_ss[0]; bad = sm_bad[0];
+        if constexpr (WPR > 1) {
+            if ((t & 63) == 0) sm_top[wave] = top;
+            __syncthreads();
 #pragma unroll
-        for (int w = 1; w < WPR; ++w) { m = fmax(m, sm_m[w]); ss += sm_ss[w]; bad |= (bool)sm_bad[w]; }
+            for (int w = 0; w < WPR; ++w) top = max(top, sm_top[w]);
+        }
+        if (top >= (DT == DT_F32 ? 0x7F800000u : DT == DT_BF16 ? 0x7F80u : 0x7C00u)) m = INFINITY;
+        else m = DT == DT_F32 ? (double)__uint_as_float(top) : DT == DT_BF16 ? (double)bf16_to_f32((uint16_t)top) : (double)f16_to_f32((uint16_t)top);
     }
-    const bool some = m > 0 && !bad, usual = m >= 0x1p-60 && m <= 0x1p60;
-    const float inv32 = 127.f * __builtin_amdgcn_rcpf((float)m);
+    const uint32_t m_high = __builtin_amdgcn_readfirstlane((uint32_t)(__builtin_bit_cast(uint64_t, m) >> 32));     // (all lanes' is the same)
+    const bool bad = m_high == 0x7FF00000u, some = m_high != 0 && !bad;      // (a product of two floats that is not 0 is 2^-298 at least)
+    const bool usual = m_high - 0x3C300000u <= 0x43B00000u - 0x3C300000u;    // 2^-60 .. 2^60
+    const float mh = (float)m, rcp = __builtin_amdgcn_rcpf(mh), inv0 = 127.f * rcp, rest = fmaf(-mh, inv0, 127.f);
+    const float inv = fmaf(NORM ? fmaf(-(float)(m - (double)mh), inv0, rest) : rest, rcp, inv0);
+    constexpr float kWhole = 0x1.8p23f, kFar = 0.5f - (NORM ? 0x1.9p-16f : 0x1.1p-17f);              // the first as in q8_code
+    const float least_far = usual ? kFar : some ? -1.f : INFINITY;
+    int8_t* const to = a.codes + row * a.codes_stride;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int c = (v * WPR * 64 + t) * 8, left = a.N - c;
-        if (left <= 0) continue;
+        const int c = (v * WPR * 64 + t) * 8, at = min(c, a.N - 8);
+        if (c >= a.N) continue;
         uint32_t w[2] = {0, 0};
-        if (some) {
-            constexpr float kWhole = 0x1.8p23f, kFar = 0.5f - 0x1p-14f;      // as in q8_code
-            float u[8], n[8];
-            uint32_t far = 0;                            // bits of the largest distance from a whole number: one that is not a number is beyond all
+        float sum[8];
+        if (some || RES) {
+            float n[8], d[8], far = 0;                       // the largest distance from a whole number; not a number where one is
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                u[i] = x[v].get(i);
-                if constexpr (RES) u[i] += r[v].get(i);
-                if constexpr (NORM) u[i] *= g[v].get(i);
-                n[i] = fmaf(u[i], inv32, kWhole);
-                far = max(far, __float_as_uint(fmaf(u[i], inv32, kWhole - n[i])) & 0x7FFFFFFFu);
+                sum[i] = x[v].get(i);
+                if constexpr (RES) sum[i] += r[v].get(i);
+                const float u = NORM ? sum[i] * g[v].get(i) : sum[i];
+                n[i] = fmaf(u, inv, kWhole);
+                d[i] = fabsf(fmaf(u, inv, kWhole - n[i]));
+                far = __builtin_elementwise_maximum(far, d[i]);
             }
             static_for<0, 2>([&](auto hc) {
                 constexpr int h = decltype(hc)::value * 4;
                 auto bits = [&](int i) { return __float_as_uint(n[h + i]); };
                 w[h / 4] = __builtin_amdgcn_perm(bits(1), bits(0), 0x0C0C0400u) | __builtin_amdgcn_perm(bits(3), bits(2), 0x04000C0Cu);
             });
-            uint32_t close = usual ? 0 : 255;
-            if (far > __float_as_uint(kFar))
+            if (!(far <= least_far)) {
+                uint32_t close = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) close |= !(fabsf(fmaf(u[i], inv32, kWhole - n[i])) <= kFar) ? 1u << i : 0u;
-            while (close) {
-                const int i = __ffs(close) - 1;
-                close &= close - 1;
-                auto pick = [&](const auto& q) {
-                    float e = q.get(0);
-                    static_for<1, 8>([&](auto k) { e = i == decltype(k)::value ? q.get(decltype(k)::value) : e; });
-                    return e;
-                };
-                double u = (double)pick(x[v]);
-                if constexpr (RES) u += (double)pick(r[v]);
-                if constexpr (NORM) u *= (double)pick(g[v]);
-                const uint32_t code = (q8_code(u, 127.0 / m, m) & 255u) << (8 * (i & 3)), keep = ~(255u << (8 * (i & 3)));
-                if (i < 4) w[0] = (w[0] & keep) | code;
-                else w[1] = (w[1] & keep) | code;
+                for (int i = 0; i < 8; ++i) close |= !(d[i] <= least_far) ? 1u << i : 0u;
+                double mm = m;
+                asm volatile("" : "+v"(mm));                 // (what follows from it is for these elements only)
+                do {
+                    const int i = __ffs(close) - 1, shift = 8 * (i & 3);
+                    close &= close - 1;
+                    double u = (double)x[v].pick(i);
+                    if constexpr (RES) u += (double)r[v].pick(i);
+                    if constexpr (NORM) u *= (double)g[v].pick(i);
+                    const uint32_t code = (q8_code(u, __builtin_amdgcn_rcp(mm), mm) & 255u) << shift, keep = ~(255u << shift);
+                    if (i < 4) w[0] = (w[0] & keep) | code;
+                    else w[1] = (w[1] & keep) | code;
+                } while (close);
             }
+            if (!some) w[0] = w[1] = 0;
         }
-        int8_t* to = a.codes + row * a.codes_stride + c;
-        if (left >= 8) *reinterpret_cast<u32x2_a1*>(to) = u32x2_a1{w[0], w[1]};
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) if (i < left) to[i] = (int8_t)(w[i / 4] >> (8 * (i & 3)));
+        if constexpr (RES) store_elems<RT, 8>(a.res_out, row * a.res_out_stride + at, sum);
+        *reinterpret_cast<u32x2_a1*>(to + at) = u32x2_a1{w[0], w[1]};
     }
     if (t == 0) a.scales[row] = row_scale<NORM>(m, ss, bad, a.N, a.eps);
 }
@@ -282,10 +308,10 @@ __global__ __launch_bounds__(1024) void q8_long_rows_kernel(Q8Args a) {
     __syncthreads();
     m = sm_m[0]; ss = sm_ss[0]; bad = sm_bad[0];
     for (int w = 1; w < (int)blockDim.x / 64; ++w) { m = fmax(m, sm_m[w]); ss += sm_ss[w]; bad |= (bool)sm_bad[w]; }
-    const double inv = m > 0 && !bad ? 127.0 / m : 0.0;
+    const double rcp = m > 0 && !bad ? __builtin_amdgcn_rcp(m) : 0.0;
     for (int i = t; i < a.N; i += (int)blockDim.x) {
         const double u = value(i);
-        a.codes[row * a.codes_stride + i] = inv > 0 ? (int8_t)q8_code(u, inv, m) : (int8_t)0;
+        a.codes[row * a.codes_stride + i] = rcp > 0 ? (int8_t)q8_code(u, rcp, m) : (int8_t)0;
         if constexpr (RT != kNoResidual) store_elem<RT>(a.res_out, row * a.res_out_stride + i, (float)h);
     }
     if (t == 0) a.scales[row] = row_scale<NORM>(m, ss, bad, a.N, a.eps);
@@ -327,7 +353,7 @@ static void launch_rows(const Q8Args& a, hipStream_t stream) {
     else if (pieces <= 64) go(C1{}, C1{});
     else if (pieces <= 256) go(C4{}, C1{});
     else if (pieces <= 1024 && a.M <= 256) go(C16{}, C1{});
-    else if (pieces <= 512) go(C8{}, C1{});              // 704 rows of 4096 with a residual 8.3 us; four waves 8.7, two 11
+    else if (pieces <= 512) go(C8{}, C1{});              // 704 rows of 4096 with a residual 7.7 us; four waves 7.9, two 9.8
     else if (pieces <= 1024) go(C8{}, C2{});
     else if (!NORM && pieces <= 1536 && a.M > 256) go(C8{}, std::integral_constant<int, NORM ? 2 : 3>{});
     else if (pieces <= 2048) go(C16{}, C2{});

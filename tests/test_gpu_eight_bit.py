@@ -72,6 +72,38 @@ def test_codes_half_way_between_two():
         assert torch.equal(laser.q8_norm(y, gain)[0], ref.norm(y, gain, 1e-6, None)[0])
 
 
+@pytest.mark.parametrize("N", [7, 300, 4096, 9000, 17000])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -90, 2.0 ** 90, 2.0 ** -120])
+def test_codes_nearly_half_way_between_two(N, size):
+    """Elements within two steps of fp32 of where a code changes: halves, or off them by some 2^-30, which is far more than steps of 64 bits."""
+    m = (1 + torch.rand(5, 1, generator=gen(N), device="cuda")) * size
+    k = torch.randint(0, 127, (5, N), generator=gen(N + 1), device="cuda")
+    x = (m.double() * (k + 0.5) / 127).float()
+    x = (x.view(torch.int32) + torch.randint(-2, 3, (5, N), generator=gen(N + 2), device="cuda", dtype=torch.int32)).view(F32)
+    x *= 1 - 2 * torch.randint(0, 2, (5, N), generator=gen(N + 3), device="cuda")
+    x[:, N // 3] = m[:, 0]
+    codes, scales = laser.q8_rows(x)
+    c, s = ref.rows(x)
+    assert torch.equal(codes, c) and same(scales, s)
+    gain = torch.ones(N, device="cuda")
+    assert torch.equal(laser.q8_norm(x, gain)[0], c)
+    assert torch.equal(laser.q8_norm(x, gain, residual=-x * 0.5)[0], ref.norm(x, gain, 1e-6, -x * 0.5)[0])
+
+
+@pytest.mark.parametrize("N", [9, 15, 505, 513, 519, 2049, 4095, 4097, 8193, 12290])
+@pytest.mark.parametrize("dtype, res", [(F16, F16), (BF16, F32), (F32, F32)])
+def test_odd_rows_in_place(N, dtype, res):
+    """The sum in the residual's place and in x's, where a row ends inside a thread's eight elements."""
+    x, r = activations(gen(N), 90, N, dtype), activations(gen(N + 1), 90, N, res)
+    gain = torch.rand(N, generator=gen(N + 2), device="cuda") + 0.5
+    want = ref.norm(x, gain, 1e-6, r)[0]
+    total = (x.double() + r.double()).float().to(res)
+    for to in ("r", "x") if dtype == res else ("r",):
+        x2, r2 = x.clone(), r.clone()
+        codes, _ = laser.q8_norm(x2, gain, 1e-6, residual=r2, residual_out=r2 if to == "r" else x2)
+        assert torch.equal(codes, want) and torch.equal(r2 if to == "r" else x2, total) and torch.equal(x2 if to == "r" else r2, x if to == "r" else r)
+
+
 @pytest.mark.parametrize("N", [5, 300, 4096, 9000])
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 def test_zeros_extremes_and_numbers_that_are_not_finite(dtype, N):
