@@ -714,7 +714,7 @@ class W8:
 
     def __del__(self):
         # at interpreter shutdown the HIP runtime may already be gone; the process frees everything
-        if not sys.is_finalizing():
+        if sys is not None and not sys.is_finalizing():
             self._free()
 
 

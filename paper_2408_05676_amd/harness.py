@@ -39,8 +39,8 @@ class Engine:
         in groups of that many inputs, in memory of their own: `weights` stays as it is, and the embedding and the head are read from it.
         Either takes the steps off the persistent kernel, ms a step at the 7B shape as it is / four_bit_cache / w4_group=128 / both: one sequence of 9 rows
         behind 1024 tokens 3.5 / 4.8 / 2.6 / 2.3, one row behind 8000 4.8 / 4.3 / 3.3 / 2.3, 64 sequences of 11 rows behind 512 17.1 / 14.5 / 21.7 / 19.4.
-        w8: the projections in 8-bit integers instead, likewise; ms a step as it is / w8 / w8 and four_bit_cache: 9 rows behind 1024 3.5 / 3.2 / 2.9, eight sequences
-        of 9 rows 5.0 / 4.2 / 4.0, 64 of 11 rows behind 512 16.6 / 11.9 / 9.1."""
+        w8: the projections in 8-bit integers instead, likewise; ms a step as it is / w8 / w8 and four_bit_cache: 9 rows behind 1024 3.5 / 3.1 / 2.8, eight sequences
+        of 9 rows 5.1 / 4.1 / 3.9, 64 of 11 rows behind 512 16.8 / 11.8 / 8.9."""
         if w4_group and w8:
             raise L.LaserError("w4_group or w8, not both")
         self.shape, self.B, self.K, self.n_max = shape, batch, K, n_max
