@@ -593,14 +593,17 @@ def w4_matmul(w: W4, x: torch.Tensor, out=None, stream=None) -> torch.Tensor:
 Q8_PAD = 128                                                                     # rows of codes lie multiples of this many bytes apart
 
 
-# A small call takes less than the checks of its arguments would attribute by attribute: the helpers below read each of a tensor's once.
+# A small call takes less than the checks of its arguments would attribute by attribute: the helpers below read each of a tensor's once, and calls in between are left out.
+_current, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _matrix(t, name: str, types):
     """(device, M, N, types[its dtype], row stride, address) of a [M][N] tensor with contiguous rows on the current device."""
     try:
         (M, N), (step, one), dt, dev = t.shape, t.stride(), types[t.dtype], t.get_device()
     except (AttributeError, ValueError, KeyError, TypeError):
         raise LaserError(f"{name} must be a CUDA tensor [M][N] of {', '.join(str(k)[6:] for k in types)}") from None
-    if dev < 0 or dev != _device():
+    if dev < 0 or dev != _current_device():
         raise LaserError(f"{name} is on {t.device}, not on the current device")
     if one != 1 and N > 1 and M:
         raise LaserError(f"{name} must have contiguous rows")
@@ -641,7 +644,9 @@ def q8_rows(x: torch.Tensor, out=None, stream=None):
     dev, M, N, dt, step, xp = _matrix(x, "x", _DTYPES)
     codes, scales = _q8_out(M, N, x.device, stream) if out is None else out
     _, cs, cp = _like(codes, "codes", M, N, _CODES, dev)
-    _check(lib().laser_q8_rows(xp, step, M, N, dt, cp, cs, _line(scales, "scales", M, dev), _on(stream, dev)), "laser_q8_rows")
+    rc = lib().laser_q8_rows(xp, step, M, N, dt, cp, cs, _line(scales, "scales", M, dev), _current(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc, "laser_q8_rows")
     return codes, scales
 
 
@@ -659,8 +664,10 @@ def q8_norm(x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-6, residual=Non
         raise LaserError("residual_out without a residual")
     codes, scales = _q8_out(M, N, x.device, stream) if out is None else out
     _, cs, cp = _like(codes, "codes", M, N, _CODES, dev)
-    _check(lib().laser_q8_norm(xp, step, dt, rp, rs, op, os_, rdt, _line(gain, "gain", N, dev), eps, M, N, cp, cs, _line(scales, "scales", M, dev),
-                               _on(stream, dev)), "laser_q8_norm")
+    rc = lib().laser_q8_norm(xp, step, dt, rp, rs, op, os_, rdt, _line(gain, "gain", N, dev), eps, M, N, cp, cs, _line(scales, "scales", M, dev),
+                             _current(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc, "laser_q8_norm")
     return codes, scales
 
 
@@ -670,7 +677,9 @@ def q8_read(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.float16, out=
     if out is None:
         out = _out((M, N), dtype, codes.device, stream)
     dt, os_, op = _like(out, "out", M, N, _DTYPES, dev)
-    _check(lib().laser_q8_read(cp, cs, _line(scales, "scales", M, dev), M, N, dt, op, os_, _on(stream, dev)), "laser_q8_read")
+    rc = lib().laser_q8_read(cp, cs, _line(scales, "scales", M, dev), M, N, dt, op, os_, _current(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc, "laser_q8_read")
     return out
 
 
@@ -731,7 +740,9 @@ def w8_matmul(w: W8, x: torch.Tensor, scales: torch.Tensor, dtype=torch.float16,
     if out is None:
         out = _out((M, w.outs), dtype, x.device, stream)
     dt, os_, op = _like(out, "out", M, w.outs, _DTYPES, dev)
-    _check(lib().laser_w8_matmul(w._h, xp, step, _line(scales, "scales", M, dev), M, dt, op, os_, _on(stream, dev)), "laser_w8_matmul")
+    rc = lib().laser_w8_matmul(w._h, xp, step, _line(scales, "scales", M, dev), M, dt, op, os_, _current(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc, "laser_w8_matmul")
     return out
 
 
