@@ -355,7 +355,8 @@ int laser_w8_create(const int8_t* codes, const float* scales, int N, int Kd, int
 int laser_w8_destroy(laser_w8* w);
 int laser_w8_quantize(const uint16_t* w, int N, int Kd, int8_t* codes, float* scales, void* stream);
 /* laser_w8_matmul: p[r][n] = x_scales[r] scales[n] sum over i of x[r][i] codes[n][i] for M rows (up to 65535 * 32); out[r][n] = p[r][n] for all N
- * outputs or, gated, p[r][n] / (1 + exp(-p[r][n])) p[r][n + N / 2] for N / 2. out in `dtype` (LASER_F16, LASER_BF16, LASER_F32), rows out_stride
+ * outputs or, gated, p[r][n] / (1 + exp(-p[r][n])) p[r][n + N / 2] for N / 2, from p in fp32 (beyond its largest number infinite, and a gate of -infinity
+ * makes NaN; a factor 1 / (1 + exp(-p)) below 2^-126 may be 0). Weights' scales outside 2^-126 .. 2^97 make products of many rows take up to 2.3 times as long. out in `dtype` (LASER_F16, LASER_BF16, LASER_F32), rows out_stride
  * elements apart, aligned to its elements; it must not overlap x. x [dev] int8 rows of Kd codes (laser_q8_rows, laser_q8_norm), x_stride < 2^22 bytes apart.
  * Keeps no workspace: calls on several streams may share a handle. LASER_E_LIMIT where M / 16 times N / 16 passes 2^25. */
 int laser_w8_matmul(const laser_w8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, void* stream);

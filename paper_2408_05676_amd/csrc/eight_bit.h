@@ -47,7 +47,7 @@ int launch_q8(const Q8Args& a, int dtype, int res_dtype, hipStream_t stream);
 // A matrix of 8-bit weights: fragments of 16 outputs x 64 inputs, a kilobyte each as the lanes of a wave hold it (16 bytes of lane 0, of lane 1, ..),
 // [Kp / 64][rows / 16], Kp = Kd rounded up to 256; then the scales of the rows. Rows are outputs, up to a multiple of 16 with zeros; of a gated
 // matrix 16 gate outputs, the 16 up outputs that belong to them, and so on.
-struct W8 { int N, Kd, gated, outs, rows, Kp; uint8_t* codes; float* scales; };   // outs: columns of a result
+struct W8 { int N, Kd, gated, outs, rows, Kp; uint8_t* codes; float* scales; int far; };   // outs: columns of a result; far: see w8_few.h
 // dtype: of the results, [M][outs]
 int launch_w8(const W8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, hipStream_t stream);
 

@@ -1,5 +1,8 @@
 // Products of rows in 8-bit codes with 8-bit weights: out[M][outs] = s_x[row] s_w[output] sum c_x c_w, plain or gated (silu(gate) up).
 #include <algorithm>
+#include <cmath>
+#include <memory>
+#include <new>
 
 #include "w8_few.h"
 
@@ -63,8 +66,9 @@ static int w8_pick(const W8Args& a, bool gated) {
 int launch_w8(const W8* w, const int8_t* x, int64_t x_stride, const float* x_scales, int M, int dtype, void* out, int64_t out_stride, hipStream_t stream) {
     LASER_REQUIRE((long)(w->rows / 16) * ((M + 15) / 16) < (1l << 25), LASER_E_LIMIT, "%d rows times %d outputs are too many for a launch", M, w->rows);
     const W8Args a{w->codes, w->scales, x, x_scales, out, x_stride, out_stride, M, w->outs, w->rows, w->Kd, w->Kp, dtype, 0, 0};
-    const int v = w8_pick(a, w->gated);
-    if (v < kW8FewN) launch_w8_few(a, w->gated, v, stream);
+    const int v = w->far ? -1 : w8_pick(a, w->gated);
+    if (v < 0) launch_w8_far(a, w->gated, stream);
+    else if (v < kW8FewN) launch_w8_few(a, w->gated, v, stream);
     else if (w->gated) launch_w8_tile_gated(a, v - kW8FewN, stream);
     else launch_w8_tile_plain(a, v - kW8FewN, stream);
     LASER_HIP_CHECK(hipGetLastError());
@@ -89,7 +93,7 @@ extern "C" int laser_w8_create(const int8_t* codes, const float* scales, int N, 
     LASER_REQUIRE(!gated || N % 2 == 0, LASER_E_SHAPE, "a gated matrix has as many up as gate outputs: N %d is odd", N);
     LASER_REQUIRE((uintptr_t)scales % 4 == 0, LASER_E_INVALID_ARG, "scales are not aligned to their elements");
     const int outs = gated ? N / 2 : N, rows = (outs + 15) / 16 * 16 * (gated ? 2 : 1), Kp = (Kd + 255) / 256 * 256;
-    W8* w = new W8{N, Kd, gated, outs, rows, Kp, nullptr, nullptr};
+    W8* w = new W8{N, Kd, gated, outs, rows, Kp, nullptr, nullptr, 0};
     const size_t bytes = (size_t)rows * Kp;
     auto fail = [&](hipError_t e, const char* what) {
         set_error("%s: %s", what, hipGetErrorString(e));
@@ -101,7 +105,14 @@ extern "C" int laser_w8_create(const int8_t* codes, const float* scales, int N, 
     w->scales = reinterpret_cast<float*>(w->codes + bytes);
     hipLaunchKernelGGL(w8_layout_kernel, dim3((unsigned)((bytes / 16 + 255) / 256)), dim3(256), 0, (hipStream_t)stream, codes, scales, N, Kd, gated, rows, Kp, w->codes, w->scales);
     if ((e = hipGetLastError()) != hipSuccess) return fail(e, "w8_layout_kernel");
+    const std::unique_ptr<float[]> held(new (std::nothrow) float[rows]);
+    if (!held) return fail(hipErrorOutOfMemory, "memory for the scales");
+    if ((e = hipMemcpyAsync(held.get(), w->scales, (size_t)rows * 4, hipMemcpyDeviceToHost, (hipStream_t)stream)) != hipSuccess) return fail(e, "hipMemcpyAsync");
     if ((e = hipStreamSynchronize((hipStream_t)stream)) != hipSuccess) return fail(e, "hipStreamSynchronize");
+    for (int i = 0; i < rows; ++i) {
+        const float s = std::fabs(held[i]);
+        w->far |= std::isfinite(s) && s != 0 && (s < 0x1p-126f || s >= 0x1p97f);
+    }
     *out = reinterpret_cast<laser_w8*>(w);
     return LASER_OK;
 }

@@ -20,7 +20,17 @@ constexpr int w8_few_lds(W8Few f) {
     return ring > sums ? ring : sums;
 }
 
-template <int MT_, int NT, int WK, bool GATED>
+// sum s_w s_x. FAR: some weights' scales are not within 2^-126 .. 2^97, so that a sum times one may pass fp32 or lose bits below its normal numbers where the product with both
+// scales does not; it goes through their mantissas. In between the bits are the same. Such matrices have kernels of their own at any number of rows (704 rows gated 4096 -> 2 x 11008 135 us of 60):
+// in the tiles, whose epilogue is a seventh of a launch, mantissas took 256 rows of that product from 35.7 to 36.4 us, a branch past them 704 rows of 4096 -> 12288 from 40.1 to 41.6,
+// and a branch here 72 rows of 2048 -> 6144 from 7.7 to 8.0.
+template <bool FAR>
+__device__ inline float w8_scaled(int sum, float sw, float sx) {
+    if constexpr (!FAR) return (float)sum * sw * sx;
+    else return __builtin_ldexpf((float)sum * __builtin_amdgcn_frexp_mantf(sw) * __builtin_amdgcn_frexp_mantf(sx), __builtin_amdgcn_frexp_expf(sw) + __builtin_amdgcn_frexp_expf(sx));
+}
+
+template <int MT_, int NT, int WK, bool GATED, bool FAR = false>
 __global__ __launch_bounds__(64 * WK) void w8_few_kernel(W8Args a) {
     constexpr W8Few F{MT_, NT, WK};
     constexpr bool DIRECT = MT_ == 0;
@@ -142,7 +152,7 @@ __global__ __launch_bounds__(64 * WK) void w8_few_kernel(W8Args a) {
                 for (int w = 1; w < WK; ++w) v += sums[(w * NT + j + h) * MT * 64 + at];
                 const float4_t sw = *reinterpret_cast<const float4_t*>(a.w_scales + n + 16 * h);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[h][e] = (float)v[e] * sw[e] * a.x_scales[row];
+                for (int e = 0; e < 4; ++e) o[h][e] = w8_scaled<FAR>(v[e], sw[e], a.x_scales[row]);
             }
             if constexpr (GATED)
 #pragma unroll
@@ -158,17 +168,26 @@ __global__ __launch_bounds__(64 * WK) void w8_few_kernel(W8Args a) {
 constexpr W8Few kW8Few[] = {{0, 1, 8}, {0, 2, 4}, {1, 1, 8}, {1, 2, 4}, {2, 2, 4}, {2, 4, 4}, {3, 2, 4}, {3, 4, 4}, {4, 4, 4}};
 constexpr int kW8FewN = (int)(sizeof(kW8Few) / sizeof(kW8Few[0]));
 
-inline void launch_w8_few(W8Args a, bool gated, int v, hipStream_t stream) {
+template <int V, bool GATED, bool FAR>
+inline void go_w8_few(W8Args a, hipStream_t stream) {
+    constexpr W8Few F = kW8Few[V];
+    a.tiles_m = (a.M + (F.mt ? F.mt : 1) * 16 - 1) / ((F.mt ? F.mt : 1) * 16);
+    a.tiles_n = (a.rows / 16 + F.nt - 1) / F.nt;
+    launch(w8_few_kernel<F.mt, F.nt, F.wk, GATED, FAR>, dim3(8u * (unsigned)((a.tiles_m * a.tiles_n + 7) / 8)), dim3(64 * F.wk), stream, a);
+}
+inline void launch_w8_few(const W8Args& a, bool gated, int v, hipStream_t stream) {
     each<0, kW8FewN>([&](auto vc) {
-        if (decltype(vc)::value != v) return;
-        constexpr W8Few F = kW8Few[decltype(vc)::value];
-        a.tiles_m = (a.M + (F.mt ? F.mt : 1) * 16 - 1) / ((F.mt ? F.mt : 1) * 16);
-        a.tiles_n = (a.rows / 16 + F.nt - 1) / F.nt;
-        const dim3 grid(8u * (unsigned)((a.tiles_m * a.tiles_n + 7) / 8));
-        if constexpr (F.nt % 2 == 0)
-            if (gated) launch(w8_few_kernel<F.mt, F.nt, F.wk, true>, grid, dim3(64 * F.wk), stream, a);
-        if (!gated) launch(w8_few_kernel<F.mt, F.nt, F.wk, false>, grid, dim3(64 * F.wk), stream, a);
+        constexpr int V = decltype(vc)::value;
+        if (V != v) return;
+        if constexpr (kW8Few[V].nt % 2 == 0)
+            if (gated) go_w8_few<V, true, false>(a, stream);
+        if (!gated) go_w8_few<V, false, false>(a, stream);
     });
+}
+inline void launch_w8_far(const W8Args& a, bool gated, hipStream_t stream) {
+    constexpr int ONE = 3, MANY = kW8FewN - 1;                       // {1, 2, 4}, {4, 4, 4}
+    if (a.M <= 16) gated ? go_w8_few<ONE, true, true>(a, stream) : go_w8_few<ONE, false, true>(a, stream);
+    else gated ? go_w8_few<MANY, true, true>(a, stream) : go_w8_few<MANY, false, true>(a, stream);
 }
 
 }  // namespace laser
