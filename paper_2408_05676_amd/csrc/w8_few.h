@@ -3,8 +3,8 @@
 // out[r][n] = s_x[r] s_w[n] sum of c_x c_w. A wave takes its share of the inputs of 16 NT outputs and 16 MT rows, weights a kilobyte a load straight into registers; the
 // waves' sums meet in LDS. Every workgroup reads its rows whole, from L2: with few outputs (one layer's 4096) that is as much as the weights from some 30 rows on.
 //
-// Bound: the weights' way from memory (one row gated 4096 -> 2 x 11008 90 MB in 18.3 us, 4.9 TB/s where a long read reaches 5.5; 4096 -> 12288 12.3 us, 11008 -> 4096 10.4 us, nine rows
-// 11.0), with more rows theirs through LDS too (72 rows 11008 -> 4096 16.6 us, 2048 -> 6144 7.6 us: start 0.7, stages 3.9, sums 1, launch 2).
+// Bound: the weights' way from memory (in a graph of twenty launches, six matrices in turn: one row gated 4096 -> 2 x 11008 90 MB in 20.2 us, 4.5 TB/s where a long read reaches 5.5; nine rows
+// 4096 -> 12288 13.7 us, 11008 -> 4096 10.6; with three matrices in turn, which the last-level cache holds in part, 16.0 us for the first), with more rows theirs through LDS too (72 rows 11008 -> 4096 16.6 us, 2048 -> 6144 7.6 us: start 0.7, stages 3.9, sums 1, launch 2).
 #pragma once
 
 #include "w8_tile.h"

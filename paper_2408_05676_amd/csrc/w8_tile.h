@@ -7,8 +7,8 @@
 //
 // Bound: few hundred rows, the weights' way from memory and the two ends of a launch (249 rows gated 2048 -> 2 x 5632, 128 x 128 tiles on 176 compute units: start 1.3 us, 16 stages 7.1, results
 // 2.1, launch 2); many rows, the matrix instructions at the clock that the card holds under them (704 rows gated 4096 -> 2 x 11008, 176 x 384 tiles: start 3.6, 32 stages of 1.3 us,
-// results 8.6; a stage's matrix instructions alone 0.90 us, all of it with zeros as data 1.15). 704 rows, weights from memory: 4096 -> 12288 40 us (1.77 POP/s), gated
-// 4096 -> 2 x 11008 60 us (2.1), 11008 -> 4096 41 us, 4096 -> 4096 18 us; a library's int8 products of these sizes without the epilogue 64, 90 and 55 us (8192 cubed: 2.04 POP/s).
+// results 8.6; a stage's matrix instructions alone 0.90 us, all of it with zeros as data 1.15). 704 rows, six matrices in turn: 4096 -> 12288 39 us (1.8 POP/s), gated
+// 4096 -> 2 x 11008 59 to 67 us (2.1 to 1.9, as the card's clock is), 11008 -> 4096 42 us, 4096 -> 4096 18 us (fp32 results 43, 44 and 20); three in turn 36 and 57; a library's int8 products of these sizes without the epilogue 64, 90 and 55 us (8192 cubed: 2.04 POP/s).
 #pragma once
 
 #include "eight_bit.h"
